@@ -12,9 +12,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtsq.so")
-SOURCES = ["tsq_api.hip", "tsq_kernels.hip", "tsq_fused.hip", "tsq_direct.hip", "tsq_entropy.hip", "tsq_rans.hip", "tsq_link.cpp"]
-HEADERS = ["tsq_internal.hpp", "tsq_device.hpp", "tsq_pass.hpp", "tsq_ranges.hpp"] + \
-    [os.path.join(ROOT, "include", h) for h in ("tsq.h", "tsq_measure.h", "tsq_ranges.h")]
+SOURCES = ["tsq_api.hip", "tsq_kernels.hip", "tsq_fused.hip", "tsq_direct.hip", "tsq_entropy.hip", "tsq_rans.hip", "tsq_link.cpp",
+           "tsq_cache_api.hip", "tsq_cache_rows.hip", "tsq_attend.hip"]
+HEADERS = ["tsq_internal.hpp", "tsq_device.hpp", "tsq_pass.hpp", "tsq_ranges.hpp", "tsq_cache_internal.hpp"] + \
+    [os.path.join(ROOT, "include", h) for h in ("tsq.h", "tsq_measure.h", "tsq_ranges.h", "tsq_cache.h")]
 
 # -ffp-contract=off: the quantizer's multiply and every fp64 product of the budget test must
 #   stay single IEEE operations; -packed-fp32-ops off: scalar fp32 code is not merged into

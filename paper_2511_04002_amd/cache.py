@@ -1,0 +1,329 @@
+"""Binding of the serving operators (include/tsq_cache.h): a key/value cache held in 8 bits and what fills and
+reads it.  Argument marshalling and checks only; every step runs in the HIP kernels of libtsq.so.
+
+A step of one layer, for requests of any lengths, new or going on:
+
+    c = Cache(blocks, 16, q_heads, kv_heads, head_dim, "bf16", max_blocks)
+    memory, table = c.new_memory(), c.new_table(requests)
+    ring, counters, lengths = c.new_ring(), c.new_counters(), c.new_lengths(requests)
+    s = c.schedule(new, lengths, table, ring, counters, c.new_schedule(requests, tokens))
+    q, k = c.norm_rotate(q, k, s.positions, angles, q_weight, k_weight)
+    c.append(memory, k, v, s.slots)
+    out = c.attend(memory, q, table, s.starts, s.lengths, max_new, max_length)
+    lengths, counters = s.lengths, s.counters         # what the next step begins with
+
+All calls run on torch's current stream.  A tensor that is left out is allocated on it.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+from . import tsq
+from .tsq import TSQ_OK, TsqError
+
+TSQ_PAIRS_HALVES, TSQ_PAIRS_NEIGHBOURS = 0, 1
+
+EXPORTS = ("tsq_cache_create", "tsq_cache_destroy", "tsq_cache_memory_sizes", "tsq_cache_schedule", "tsq_cache_norm_rotate",
+           "tsq_cache_append", "tsq_cache_gather", "tsq_cache_attend", "tsq_cache_attend_workspace_bytes")
+
+
+class tsq_cache_config(C.Structure):
+    _fields_ = [("blocks", C.c_uint32), ("block_tokens", C.c_uint32), ("q_heads", C.c_uint32), ("kv_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("dtype", C.c_int32), ("max_blocks", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class tsq_cache_memory(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_k", "d_v", "d_k_scale", "d_v_scale")]
+
+
+class tsq_cache_sizes(C.Structure):
+    _fields_ = [("code_bytes", C.c_uint64), ("scale_bytes", C.c_uint64)]
+
+
+_lib = None
+
+
+def lib():
+    """libtsq.so with the argument types of tsq_cache.h set.  Raises if it has not been built."""
+    global _lib
+    if _lib is None:
+        L = tsq.lib()
+        vp, u32, i32, u64, f32, st = C.c_void_p, C.c_uint32, C.c_int32, C.c_uint64, C.c_float, C.c_int
+        mem = C.POINTER(tsq_cache_memory)
+        for name, res, args in (
+                ("tsq_cache_create", st, [C.POINTER(tsq_cache_config), C.POINTER(vp)]),
+                ("tsq_cache_destroy", None, [vp]),
+                ("tsq_cache_memory_sizes", st, [vp, C.POINTER(tsq_cache_sizes)]),
+                ("tsq_cache_schedule", st, [vp, u32, vp, vp, vp, vp, vp, u32, vp, vp, vp, vp, vp, vp, vp]),
+                ("tsq_cache_norm_rotate", st, [vp, u32, vp, u64, vp, u64, vp, vp, u32, u32, i32, vp, vp, f32, vp, u64, vp, u64, vp]),
+                ("tsq_cache_append", st, [vp, mem, u32, vp, u64, vp, u64, vp, vp]),
+                ("tsq_cache_gather", st, [vp, mem, u32, vp, vp, vp, u32, vp, u64, vp, u64, vp]),
+                ("tsq_cache_attend", st, [vp, mem, u32, vp, vp, vp, u32, u32, u32, vp, u64, f32, i32, u32, vp, u64, vp, vp, vp]),
+                ("tsq_cache_attend_workspace_bytes", C.c_size_t, [vp, u32, u32, u32, u32, u32])):
+            getattr(L, name).restype = res
+            getattr(L, name).argtypes = args
+        _lib = L
+    return _lib
+
+
+# ------------------------------------------------------------------ the C entry points, same names
+
+def _done(status: int, what: str) -> None:
+    if status != TSQ_OK:
+        raise TsqError(status, what)
+
+
+def tsq_cache_create(cfg: tsq_cache_config) -> int:
+    """-> opaque handle (int).  Raises TsqError on a rejected configuration."""
+    h = C.c_void_p()
+    _done(lib().tsq_cache_create(C.byref(cfg), C.byref(h)), "tsq_cache_create")
+    return h.value
+
+
+def tsq_cache_destroy(cache: int) -> None:
+    lib().tsq_cache_destroy(cache)
+
+
+def tsq_cache_memory_sizes(cache: int) -> tsq_cache_sizes:
+    out = tsq_cache_sizes()
+    _done(lib().tsq_cache_memory_sizes(cache, C.byref(out)), "tsq_cache_memory_sizes")
+    return out
+
+
+def tsq_cache_schedule(*args) -> None:
+    _done(lib().tsq_cache_schedule(*args), "tsq_cache_schedule")
+
+
+def tsq_cache_norm_rotate(*args) -> None:
+    _done(lib().tsq_cache_norm_rotate(*args), "tsq_cache_norm_rotate")
+
+
+def tsq_cache_append(*args) -> None:
+    _done(lib().tsq_cache_append(*args), "tsq_cache_append")
+
+
+def tsq_cache_gather(*args) -> None:
+    _done(lib().tsq_cache_gather(*args), "tsq_cache_gather")
+
+
+def tsq_cache_attend(*args) -> None:
+    _done(lib().tsq_cache_attend(*args), "tsq_cache_attend")
+
+
+def tsq_cache_attend_workspace_bytes(cache: int, requests: int, tokens: int, max_new: int, max_length: int, window: int = 0) -> int:
+    return int(lib().tsq_cache_attend_workspace_bytes(cache, requests, tokens, max_new, max_length, window))
+
+
+# ------------------------------------------------------------------ convenience over torch tensors
+
+class Memory:
+    """The four tensors of one cache, and the C structure that holds their pointers."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.c = tsq_cache_memory(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.ref = C.byref(self.c)
+
+
+class Schedule:
+    """What one step's schedule is written to (see tsq_cache_schedule)."""
+
+    def __init__(self, lengths, counters, starts, positions, slots, status):
+        self.lengths, self.counters, self.starts = lengths, counters, starts
+        self.positions, self.slots, self.status = positions, slots, status
+
+    def check(self) -> None:
+        """Raises TsqError if the step could not be taken.  Synchronizes."""
+        _done(int(self.status.item()), "tsq_cache_schedule")
+
+
+def _refuse(what: str):
+    raise ValueError(what)
+
+
+class Cache:
+    """One tsq_cache plus helpers that allocate torch buffers, check them and pass their pointers."""
+
+    def __init__(self, blocks: int, block_tokens: int, q_heads: int, kv_heads: int, head_dim: int, dtype: str, max_blocks: int):
+        import torch
+        if dtype not in tsq._DTYPES:
+            _refuse("dtype is 'f16' or 'bf16'")
+        self.kind = torch.float16 if dtype == "f16" else torch.bfloat16
+        self.int32, self.int64, self.float32 = torch.int32, torch.int64, torch.float32
+        self.blocks, self.block_tokens, self.q_heads, self.kv_heads = blocks, block_tokens, q_heads, kv_heads
+        self.head_dim, self.dtype, self.max_blocks = head_dim, dtype, max_blocks
+        self.cfg = tsq_cache_config(blocks, block_tokens, q_heads, kv_heads, head_dim, tsq._DTYPES[dtype], max_blocks, 0)
+        self.handle = tsq_cache_create(self.cfg)
+        self._torch, self._lib = torch, lib()
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h and tsq_cache_destroy is not None:
+            tsq_cache_destroy(h)
+            self.handle = None
+
+    _stream = staticmethod(tsq.Plan._stream)
+
+    # -------------------------------------------------------------- buffers
+
+    def _empty(self, shape, kind):
+        return self._torch.empty(shape, dtype=kind, device="cuda")
+
+    def new_memory(self) -> Memory:
+        t = self._torch
+        n, h, b, d = self.blocks, self.kv_heads, self.block_tokens, self.head_dim
+        return Memory(self._empty((n, h, b, d), t.int8), self._empty((n, h, d, b), t.int8),
+                      self._empty((n, h), t.float32), self._empty((n, h), t.float32))
+
+    def wrap(self, k, v, k_scale, v_scale) -> Memory:
+        """A cache in tensors that are there: k [blocks, kv_heads, block_tokens, head_dim] int8,
+        v [blocks, kv_heads, head_dim, block_tokens] int8, scales [blocks, kv_heads] float32."""
+        t = self._torch
+        n, h, b, d = self.blocks, self.kv_heads, self.block_tokens, self.head_dim
+        for x, shape, kind in ((k, (n, h, b, d), t.int8), (v, (n, h, d, b), t.int8), (k_scale, (n, h), t.float32), (v_scale, (n, h), t.float32)):
+            if not (x.is_cuda and x.is_contiguous() and tuple(x.shape) == shape and x.dtype == kind):
+                _refuse("a cache's tensor is %s on the GPU, contiguous, %s" % (shape, kind))
+        return Memory(k, v, k_scale, v_scale)
+
+    def new_table(self, requests: int):
+        return self._torch.full((requests, self.max_blocks), -1, dtype=self.int32, device="cuda")
+
+    def new_ring(self):
+        return self._torch.arange(self.blocks, dtype=self.int32, device="cuda")
+
+    def new_counters(self):
+        return self._torch.tensor([0, self.blocks], dtype=self.int64, device="cuda")
+
+    def new_lengths(self, requests: int):
+        return self._torch.zeros(requests, dtype=self.int32, device="cuda")
+
+    def new_schedule(self, requests: int, tokens: int) -> Schedule:
+        e, i32 = self._empty, self.int32
+        return Schedule(e(requests, i32), e(2, self.int64), e(requests + 1, i32), e(tokens, i32), e(tokens, i32), e(1, i32))
+
+    # -------------------------------------------------------------- checks
+
+    def _ints(self, x, shape, what):
+        if not (x.is_cuda and x.is_contiguous() and x.dtype == self.int32 and x.shape == shape):
+            _refuse("%s is int32 %s on the GPU, contiguous" % (what, tuple(shape)))
+        return x.data_ptr()
+
+    def _rows(self, x, tokens, heads, what):
+        """x: [tokens, heads, head_dim], or [tokens, heads * head_dim]; rows anywhere, the heads of a row together.
+        -> pointer, elements from row to row."""
+        shape, stride = x.shape, x.stride()
+        d = self.head_dim
+        if not (x.is_cuda and x.dtype == self.kind and shape[0] == tokens and
+                ((len(shape) == 3 and shape[1] == heads and shape[2] == d and stride[2] == 1 and (heads == 1 or stride[1] == d)) or
+                 (len(shape) == 2 and shape[1] == heads * d and stride[1] == 1))):
+            _refuse("%s is [%d, %d, %d] of %s on the GPU, the heads of a row together" % (what, tokens, heads, d, self.kind))
+        return x.data_ptr(), (stride[0] if tokens > 1 else heads * d)
+
+    def _into(self, x, tokens, heads, what):
+        x = self._empty((tokens, heads, self.head_dim), self.kind) if x is None else x
+        return (x,) + self._rows(x, tokens, heads, what)
+
+    # -------------------------------------------------------------- the operators
+
+    def schedule(self, new, lengths, table, ring, counters, out: Schedule) -> Schedule:
+        """Block tables, slots and positions of a step: new [requests] int32 new tokens of each request (-1: done),
+        lengths [requests] int32 what it has.  table and ring are updated; the rest is written to `out`
+        (from new_schedule(requests, most new tokens of a step))."""
+        n = new.shape
+        if not (counters.is_cuda and counters.is_contiguous() and counters.dtype == self.int64 and counters.shape == (2,) and
+                out.counters.is_cuda and out.counters.is_contiguous() and out.counters.dtype == self.int64 and out.counters.shape == (2,)):
+            _refuse("counters is int64 (2,) on the GPU, contiguous")
+        if len(n) != 1:
+            _refuse("new is int32 [requests]")
+        i, capacity = self._ints, out.slots.shape
+        status = self._lib.tsq_cache_schedule(
+            self.handle, n[0], i(new, n, "new"), i(lengths, n, "lengths"), i(table, (n[0], self.max_blocks), "table"),
+            i(ring, (self.blocks,), "ring"), counters.data_ptr(), capacity[0], i(out.lengths, n, "out.lengths"),
+            out.counters.data_ptr(), i(out.starts, (n[0] + 1,), "out.starts"), i(out.positions, capacity, "out.positions"),
+            i(out.slots, capacity, "out.slots"), i(out.status, (1,), "out.status"), self._stream())
+        if status:
+            raise TsqError(status, "tsq_cache_schedule")
+        return out
+
+    def norm_rotate(self, q, k, positions, angles, q_weight=None, k_weight=None, eps: float = 1e-6, pairs: str = "halves",
+                    q_out=None, k_out=None):
+        """RMS norm of each head of q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim] (weights [head_dim],
+        or None: no norm), then the rotation by position: angles [rows, rotary] float32 holds the cosines of a
+        position's rotary / 2 angles, then their sines.  q_out, k_out may be q, k themselves."""
+        tokens = q.shape[0]
+        qp, qs = self._rows(q, tokens, self.q_heads, "q")
+        kp, ks = self._rows(k, tokens, self.kv_heads, "k")
+        q_out, qo, qos = self._into(q_out, tokens, self.q_heads, "q_out")
+        k_out, ko, kos = self._into(k_out, tokens, self.kv_heads, "k_out")
+        if not (angles.is_cuda and angles.is_contiguous() and angles.dtype == self.float32 and angles.dim() == 2):
+            _refuse("angles is float32 [rows, rotary] on the GPU, contiguous")
+        if pairs not in ("halves", "neighbours"):
+            _refuse("pairs is 'halves' or 'neighbours'")
+        weights = []
+        for w in (q_weight, k_weight):
+            if w is not None and not (w.is_cuda and w.is_contiguous() and w.dtype == self.kind and w.shape == (self.head_dim,)):
+                _refuse("a norm's weight is [head_dim] of the cache's dtype on the GPU, contiguous")
+            weights.append(None if w is None else w.data_ptr())
+        status = self._lib.tsq_cache_norm_rotate(
+            self.handle, tokens, qp, qs, kp, ks, self._ints(positions, (tokens,), "positions"), angles.data_ptr(), angles.shape[0],
+            angles.shape[1], TSQ_PAIRS_HALVES if pairs == "halves" else TSQ_PAIRS_NEIGHBOURS, weights[0], weights[1], eps,
+            qo, qos, ko, kos, self._stream())
+        if status:
+            raise TsqError(status, "tsq_cache_norm_rotate")
+        return q_out, k_out
+
+    def append(self, memory: Memory, k, v, slots) -> None:
+        """Stores k and v [tokens, kv_heads, head_dim] at slots [tokens] int32 (from a schedule; -1: not stored)."""
+        tokens = k.shape[0]
+        kp, ks = self._rows(k, tokens, self.kv_heads, "k")
+        vp, vs = self._rows(v, tokens, self.kv_heads, "v")
+        status = self._lib.tsq_cache_append(self.handle, memory.ref, tokens, kp, ks, vp, vs, self._ints(slots, (tokens,), "slots"),
+                                            self._stream())
+        if status:
+            raise TsqError(status, "tsq_cache_append")
+
+    def gather(self, memory: Memory, table, starts, lengths, k_out, v_out):
+        """The last starts[r + 1] - starts[r] tokens of each request r, up to lengths[r], into rows starts[r] ... of k_out
+        and v_out [tokens, kv_heads, head_dim] (or [tokens, kv_heads * head_dim], as Plan.compress_batch takes them)."""
+        tokens, n = k_out.shape[0], lengths.shape
+        kp, ks = self._rows(k_out, tokens, self.kv_heads, "k_out")
+        vp, vs = self._rows(v_out, tokens, self.kv_heads, "v_out")
+        i = self._ints
+        status = self._lib.tsq_cache_gather(
+            self.handle, memory.ref, n[0], i(table, (n[0], self.max_blocks), "table"), i(starts, (n[0] + 1,), "starts"),
+            i(lengths, n, "lengths"), tokens, kp, ks, vp, vs, self._stream())
+        if status:
+            raise TsqError(status, "tsq_cache_gather")
+        return k_out, v_out
+
+    def new_workspace(self, requests: int, tokens: int, max_new: int, max_length: int, window: int = 0):
+        """A workspace for attend calls of these numbers on one stream; None where they need none."""
+        n = tsq_cache_attend_workspace_bytes(self.handle, requests, tokens, max_new, max_length, window)
+        return self._empty(n, self._torch.uint8) if n else None
+
+    def attend(self, memory: Memory, q, table, starts, lengths, max_new: int, max_length: int, scale=None, causal: bool = True,
+               window: int = 0, out=None, lse=None, ws=None):
+        """Attention of q [tokens, q_heads, head_dim] over the cache: rows starts[r] .. starts[r + 1] - 1 are the last tokens of
+        request r, which has lengths[r] in the cache.  max_new, max_length: the largest of both over the requests (how the
+        work is split goes by them).  scale: 1 / sqrt(head_dim) if left out.  lse: float32 [tokens, q_heads] to be written."""
+        tokens, n = q.shape[0], lengths.shape
+        qp, qs = self._rows(q, tokens, self.q_heads, "q")
+        out, op, os_ = self._into(out, tokens, self.q_heads, "out")
+        lp = None
+        if lse is not None:
+            if not (lse.is_cuda and lse.is_contiguous() and lse.dtype == self.float32 and lse.shape == (tokens, self.q_heads)):
+                _refuse("lse is float32 [tokens, q_heads] on the GPU, contiguous")
+            lp = lse.data_ptr()
+        i, L = self._ints, self._lib
+        need = L.tsq_cache_attend_workspace_bytes(self.handle, n[0], tokens, max_new, max_length, window)
+        if need and ws is None:
+            ws = self._empty(need, self._torch.uint8)
+        if need and not (ws.is_cuda and ws.is_contiguous() and ws.numel() * ws.element_size() >= need):
+            _refuse("ws has %d bytes on the GPU, contiguous" % need)
+        status = L.tsq_cache_attend(
+            self.handle, memory.ref, n[0], i(table, (n[0], self.max_blocks), "table"), i(starts, (n[0] + 1,), "starts"),
+            i(lengths, n, "lengths"), tokens, max_new, max_length, qp, qs, self.head_dim ** -0.5 if scale is None else scale,
+            causal, window, op, os_, lp, ws.data_ptr() if need else None, self._stream())
+        if status:
+            raise TsqError(status, "tsq_cache_attend")
+        return out

@@ -1,0 +1,405 @@
+// Attention over a cache held in 8 bits (tsq_cache_attend).
+//
+// With a key c_k * s_k and a value c_v * s_v (codes of the cache, and one scale for a block of tokens and a head),
+//   out = sum_t w_t s_v c_v / sum_t w_t,   w_t = exp(scale * s_k * (q . c_k))
+// The codes go into the matrix instructions as they are: whole numbers up to 127 are exact as halves, so q . c_k is
+// exact up to its binary32 sum.  Both scales belong to 16 or more tokens in a row and stay outside: s_k multiplies
+// the scores, and s_v goes into the exponent, P_t = 2^(score_t + log2 s_v - m), so that one exponential makes the
+// weight that the values' codes want; the softmax's denominator takes P_t / s_v back, once for 16 tokens.  The
+// reference m follows the largest exponent of a row in steps: it moves only when an exponent is more than 8 above
+// what it was set for, and is then set 7 below the largest.  P is then at most 2^15, in a half's range, and
+// 11-bit weights down to 2^-21 of the row's largest.
+//
+// Scores are computed transposed, S^T = K Q^T: a lane then has all its scores in one row of the softmax (a query),
+// and the registers that hold P^T are, in the order they are in, an operand of O^T = V^T P^T.  A matrix
+// instruction does not care which tokens its k index stands for as long as both operands agree, so the tokens of
+// a tile are dealt to the lanes such that nothing has to be moved.
+#include <hip/hip_runtime.h>
+
+#include "tsq_cache_internal.hpp"
+
+namespace tsq {
+namespace {
+
+constexpr float kNone = -1e30f;      // reference of a row that has seen nothing
+constexpr float kRoom = 7.0f;        // the reference is set this far below the largest exponent ...
+constexpr float kSlack = 8.0f;       // ... and kept until one exceeds that by as much
+
+__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
+
+// What a workgroup works on: a row tile of a request (rows: query token and head of the group, the group fastest),
+// a kv head, and a piece of the tile's reach along the cache.
+struct Place {
+    uint32_t h, split, r, tile;
+    uint32_t begin, n;               // the request's rows of the call
+    int32_t length;                  // as the caller gave it
+    uint32_t seen;                   // tokens that the table can hold of them
+    bool beyond, last;
+};
+
+template <int ROWS>
+__device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
+    uint32_t x = blockIdx.x;
+    p.h = x % a.kv_heads;
+    x /= a.kv_heads;
+    p.split = x % a.splits;
+    x = a.tiles - 1 - x / a.splits;  // the tiles with the most tokens before them first
+    uint32_t next;                   // tiles that the request has before the next one's begin
+    if (a.tiles_each) {
+        p.r = x / a.tiles_each;
+        p.tile = x % a.tiles_each;
+        next = a.tiles_each;
+    } else {
+        // request r begins at tile first(r) = rows before it / ROWS + r, which leaves it at least as many as it needs
+        uint32_t lo = 0, hi = a.requests;
+        const uint32_t lane = threadIdx.x & 63;
+        auto first = [&](uint32_t r) {
+            return (uint32_t)((uint64_t)min((uint32_t)max(a.starts[r], 0), a.tokens) * a.group / ROWS) + r;
+        };
+        while (hi - lo > 1) {        // a wave halves 64 times at once
+            const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+            const uint64_t below = __ballot(at < hi && first(at) <= x);
+            const uint32_t last = 63 - (uint32_t)__builtin_clzll(below | 1);
+            hi = min(hi, lo + (last + 1) * step);
+            lo += last * step;
+        }
+        p.r = lo;
+        const uint32_t f = first(lo);
+        p.tile = x - f;
+        next = first(lo + 1) - f;
+        if (x < f) return false;
+    }
+    const uint32_t b = min((uint32_t)max(a.starts[p.r], 0), a.tokens), e = min((uint32_t)max(a.starts[p.r + 1], 0), a.tokens);
+    p.begin = b;
+    p.n = e > b ? e - b : 0;
+    p.length = max(a.lengths[p.r], 0);
+    const uint64_t most = (uint64_t)a.max_blocks << a.block_log2;
+    p.beyond = (uint64_t)p.length > most;
+    p.seen = p.beyond ? (uint32_t)most : (uint32_t)p.length;
+    p.last = p.tile + 1 == next;
+    return (uint64_t)p.tile * ROWS < (uint64_t)p.n * a.group;
+}
+
+// Tokens that any row of a tile sees, the part of them that a split has, and what a row sees.
+struct Reach { uint32_t begin, end; };
+template <int ROWS>
+__device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Place &p, uint32_t tile) {
+    const int64_t rows = (int64_t)p.n * a.group, first = (int64_t)tile * ROWS, last = min(first + ROWS, rows) - 1;
+    const int64_t p0 = (int64_t)p.length - p.n + first / a.group, p1 = (int64_t)p.length - p.n + last / a.group;
+    int64_t lo = a.window ? max(p0 - (int64_t)a.window + 1, (int64_t)0) : 0;
+    int64_t hi = a.causal ? min(p1 + 1, (int64_t)p.seen) : (int64_t)p.seen;
+    lo &= ~(int64_t)63;
+    const int64_t begin = lo + (int64_t)p.split * a.chunk;
+    if (p.split + 1 < a.splits) hi = min(hi, begin + a.chunk);
+    Reach w;
+    w.begin = (uint32_t)min(begin, (int64_t)0x7FFFFFC0);
+    w.end = hi > begin ? (uint32_t)hi : w.begin;
+    return w;
+}
+__device__ __forceinline__ void row_sees(const AttendArgs &a, const Place &p, uint32_t row, uint32_t &from, uint32_t &to) {
+    // (rows past the request's are computed along and not written: they ask for no mask)
+    if (row >= p.n * a.group) { from = 0; to = ~0u; return; }
+    const int64_t at = (int64_t)p.length - p.n + row / a.group;
+    const int64_t lo = a.window ? max(at - (int64_t)a.window + 1, (int64_t)0) : 0;
+    const int64_t hi = a.causal ? min(at + 1, (int64_t)p.seen) : (int64_t)p.seen;
+    from = (uint32_t)lo;
+    to = hi > lo ? (uint32_t)hi : 0u;
+}
+
+// What the 16 tokens of a block that a lane works on have in common: the block (0 where there is none, whose codes
+// are then not used), the factor of its scores, and its values' scale as log2 and as reciprocal.  Values that are
+// all 0 weigh nothing whatever their scale: 2^-60 keeps their tokens in the denominator without touching the
+// reference of the others.
+struct Block { uint32_t id; float c, log_v, back_v; };
+__device__ __forceinline__ uint32_t block_id(const AttendArgs &a, const Place &p, uint32_t token, bool &bad) {
+    const uint32_t nth = token >> a.block_log2;
+    bad = p.beyond;
+    if (token >= p.seen) return 0;
+    const uint32_t id = (uint32_t)a.table[(uint64_t)p.r * a.max_blocks + nth];
+    if (id >= a.blocks) { bad = true; return 0; }
+    return id;
+}
+__device__ __forceinline__ Block block_at(const AttendArgs &a, const Place &p, uint32_t token, float row_factor) {
+    Block b;
+    bool bad;
+    b.id = block_id(a, p, token, bad);
+    const uint64_t at = (uint64_t)b.id * a.kv_heads + p.h;
+    const float ks = bad ? __builtin_nanf("") : a.k_scale[at], vs = a.v_scale[at];
+    b.c = ks * row_factor;
+    const float v = vs == 0.0f ? 0x1p-60f : vs;
+    b.log_v = log2_of(v);
+    b.back_v = 1.0f / v;
+    return b;
+}
+
+// A query's 16-bit elements as halves, and what the scores are to be multiplied by for it: binary16 as it is,
+// bfloat16 at a power of two that brings the row's largest element to 2^13 .. 2^14, which leaves every bit of
+// elements down to 2^-27 of it.
+template <bool BF16>
+__device__ __forceinline__ half8_t query_piece(uint4_t w, float f) {
+    if constexpr (!BF16) return __builtin_bit_cast(half8_t, w);
+    else {
+        half8_t o;
+        for (int i = 0; i < 4; ++i) {
+            o[2 * i] = (_Float16)(widen<true>(w[i] & 0xFFFFu) * f);
+            o[2 * i + 1] = (_Float16)(widen<true>(w[i] >> 16) * f);
+        }
+        return o;
+    }
+}
+__device__ __forceinline__ uint32_t piece_most(uint4_t w) {
+    uint32_t m = 0;
+    for (int i = 0; i < 4; ++i) m = max(m, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+    return m;
+}
+// largest magnitude's bits (bfloat16) -> the factor that its row is multiplied by; `back` undoes it
+__device__ __forceinline__ float query_factor(uint32_t most, float &back) {
+    int e = (int)(most >> 7) - 127;
+    if (e > 127) e = 13;             // a NaN or infinity shows in any case
+    if (e < -100) e = -100;
+    back = __builtin_bit_cast(float, (uint32_t)(e - 13 + 127) << 23);
+    return __builtin_bit_cast(float, (uint32_t)(13 - e + 127) << 23);
+}
+
+// Where a row's result goes.
+__device__ __forceinline__ uint64_t row_id(const AttendArgs &a, const Place &p, uint32_t row) {
+    return (uint64_t)(p.begin + row / a.group) * a.q_heads + p.h * a.group + row % a.group;
+}
+
+// Few rows: 16 of a kv head's.  Each of four waves takes every fourth tile of 64 tokens straight from memory to
+// registers and keeps a softmax of its own; they meet in LDS at the end.
+// Lane (m = lane % 16, g = lane / 16).  The tokens of a tile: group g has 16g .. 16g + 15, all of one block.
+//   S^T tile t (16 tokens x 16 rows): row 4g + i is token 16g + 4t + i, so that a lane's 16 scores (t, i) are the
+//   16 tokens of its group, in the order of its 16 bytes of a value's row; its row of the softmax is m.
+//   Keys: operand row m is token 16 (m / 4) + 4t + m % 4; the lane's k indices are the elements 64f + 16g .. + 15.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
+    constexpr int F = D / 64;                            // 64-element pieces of a head
+    __shared__ float sums[4][16][132];
+    __shared__ float stats[4][16][2];
+    Place p;
+    if (!find_place<16>(a, p)) return;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+    const uint32_t B = 1u << a.block_log2;
+    for (uint32_t tile = p.tile;; ++tile) {
+        const uint32_t row = tile * 16 + m, rows = p.n * a.group;
+        // queries
+        half8_t q[F][2];
+        float back = 1.0f;
+        {
+            uint4_t w[F][2];
+            uint32_t most = 0;
+            for (int f = 0; f < F; ++f)
+                for (int e = 0; e < 2; ++e) {
+                    w[f][e] = uint4_t{0, 0, 0, 0};
+                    if (row < rows) {
+                        const uint16_t *src = static_cast<const uint16_t *>(a.q) + (uint64_t)(p.begin + row / a.group) * a.q_stride +
+                                              (uint64_t)(p.h * a.group + row % a.group) * D + 64 * f + 16 * g + 8 * e;
+                        w[f][e] = *reinterpret_cast<const uint4_t *>(src);
+                    }
+                    most = max(most, piece_most(w[f][e]));
+                }
+            float factor = 1.0f;
+            if constexpr (BF16) {
+                most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+                most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+                factor = query_factor(most, back);
+            }
+            for (int f = 0; f < F; ++f)
+                for (int e = 0; e < 2; ++e) q[f][e] = query_piece<BF16>(w[f][e], factor);
+        }
+        const float row_factor = back * a.scale_log2;
+        uint32_t from, to;
+        row_sees(a, p, row, from, to);
+        const Reach reach = reach_of<16>(a, p, tile);
+
+        float4_t acc[D / 16];
+        for (int d = 0; d < D / 16; ++d) acc[d] = float4_t{0, 0, 0, 0};
+        float ref = kNone, weight = 0.0f;
+        for (uint32_t t0 = reach.begin + 64 * wave; t0 < reach.end; t0 += 256) {
+            const Block b = block_at(a, p, t0 + 16 * g, row_factor);
+            const uint32_t key_token = t0 + 16 * (m >> 2);
+            bool bad_key;
+            const uint32_t key_id = block_id(a, p, key_token, bad_key);
+            const int8_t *keys = a.k + (((uint64_t)key_id * a.kv_heads + p.h) * B + (key_token & (B - 1)) + (m & 3)) * D + 16 * g;
+            const int8_t *values = a.v + (((uint64_t)b.id * a.kv_heads + p.h) * D + m) * B + ((t0 + 16 * g) & (B - 1));
+            uint4_t kw[4][F], vw[D / 16];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                for (int f = 0; f < F; ++f) kw[t][f] = *reinterpret_cast<const uint4_t *>(keys + 4 * t * D + 64 * f);
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) vw[d] = *reinterpret_cast<const uint4_t *>(values + (uint64_t)(16 * d) * B);
+            float4_t s[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                s[t] = float4_t{0, 0, 0, 0};
+                for (int f = 0; f < F; ++f)
+                    for (int e = 0; e < 2; ++e) {
+                        const half4_t x = codes_to_half(kw[t][f][2 * e]), y = codes_to_half(kw[t][f][2 * e + 1]);
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), q[f][e], s[t], 0, 0, 0);
+                    }
+            }
+            // exponents, and the reference
+            const uint32_t mine = t0 + 16 * g;
+            const bool whole = __ballot(mine < from || mine + 16 > to) == 0;
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t token = mine + 4 * t + i;
+                    s[t][i] = __builtin_fmaf(s[t][i], b.c, b.log_v);
+                    if (!whole && (token < from || token >= to)) s[t][i] = -INFINITY;
+                    top = fmaxf(top, s[t][i]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (__ballot(top > ref + (kRoom + kSlack))) {
+                const float now = fmaxf(ref, top - kRoom), down = pow2(ref - now);
+                ref = now;
+                weight *= down;
+                for (int d = 0; d < D / 16; ++d) acc[d] *= down;
+            }
+            float sum = 0.0f;
+            half8_t pw[2];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                for (int i = 0; i < 4; ++i) {
+                    const float e = pow2(s[t][i] - ref);
+                    sum += e;
+                    pw[t / 2][4 * (t & 1) + i] = (_Float16)e;
+                }
+            // (a group that a row sees nothing of stays out, whatever its scale is)
+            weight += sum == 0.0f ? 0.0f : sum * b.back_v;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d)
+                for (int u = 0; u < 2; ++u) {
+                    const half4_t x = codes_to_half(vw[d][2 * u]), y = codes_to_half(vw[d][2 * u + 1]);
+                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), pw[u], acc[d], 0, 0, 0);
+                }
+        }
+        weight += __shfl_xor(weight, 16);
+        weight += __shfl_xor(weight, 32);
+
+        // the four waves' sums, at one reference
+        if (g == 0) { stats[wave][m][0] = ref; stats[wave][m][1] = weight; }
+        __syncthreads();
+        float all = fmaxf(fmaxf(stats[0][m][0], stats[1][m][0]), fmaxf(stats[2][m][0], stats[3][m][0]));
+        const float mine = pow2(ref - all);
+        const uint32_t out_row = threadIdx.x >> 4, piece = threadIdx.x & 15, o = tile * 16 + out_row;
+        float total = 0.0f, top = fmaxf(fmaxf(stats[0][out_row][0], stats[1][out_row][0]), fmaxf(stats[2][out_row][0], stats[3][out_row][0]));
+        for (int w = 0; w < 4; ++w) total += stats[w][out_row][1] * pow2(stats[w][out_row][0] - top);
+        const uint64_t id = row_id(a, p, o);
+        for (int part = 0; part < (D + 127) / 128; ++part) {
+            constexpr int N = D < 128 ? D : 128;         // elements at a time
+            if (part) __syncthreads();
+            for (int d = 0; d < N / 16; ++d) *reinterpret_cast<float4_t *>(&sums[wave][m][16 * d + 4 * g]) = acc[part * 8 + d] * mine;
+            __syncthreads();
+            if (piece * 8 < N && o < rows) {
+                float y[8];
+                for (int i = 0; i < 8; ++i)
+                    y[i] = sums[0][out_row][8 * piece + i] + sums[1][out_row][8 * piece + i] + sums[2][out_row][8 * piece + i] + sums[3][out_row][8 * piece + i];
+                if (a.splits == 1) {
+                    const float f = total == 0.0f ? 0.0f : 1.0f / total;
+                    uint4_t w;
+                    for (int i = 0; i < 4; ++i) w[i] = narrow2<BF16>(y[2 * i] * f, y[2 * i + 1] * f);
+                    uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)(p.begin + o / a.group) * a.out_stride +
+                                    (uint64_t)(p.h * a.group + o % a.group) * D + part * 128 + piece * 8;
+                    *reinterpret_cast<uint4_t *>(dst) = w;
+                } else {
+                    float *dst = a.parts + (id * a.splits + p.split) * D + part * 128 + piece * 8;
+                    *reinterpret_cast<float4_t *>(dst) = float4_t{y[0], y[1], y[2], y[3]};
+                    *reinterpret_cast<float4_t *>(dst + 4) = float4_t{y[4], y[5], y[6], y[7]};
+                }
+            }
+        }
+        if (piece == 0 && o < rows) {
+            if (a.splits > 1) {
+                float *dst = a.parts + a.part_rows * a.splits * D + (id * a.splits + p.split) * 2;
+                dst[0] = top;
+                dst[1] = total;
+            } else if (a.lse) {
+                a.lse[id] = total == 0.0f ? -INFINITY : (top + log2_of(total)) * 0.69314718055994530942f;
+            }
+        }
+        if (!p.last || (uint64_t)(tile + 1) * 16 >= rows) return;
+        __syncthreads();
+    }
+}
+
+// The pieces of a row along the cache, joined in their order: a workgroup for four rows.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
+    constexpr int E = D / 64;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t id = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (id >= a.part_rows) return;
+    const uint32_t token = (uint32_t)(id / a.q_heads), head = (uint32_t)(id % a.q_heads);
+    // rows that no request has were not computed and are not written
+    uint32_t lo = 0, hi = a.requests;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (a.starts[mid] <= (int32_t)token) lo = mid; else hi = mid;
+    }
+    if ((int32_t)token < a.starts[lo] || (int32_t)token >= a.starts[lo + 1]) return;
+    const float *sums = a.parts + id * a.splits * D + lane * E, *stats = a.parts + a.part_rows * a.splits * D + id * a.splits * 2;
+    float top = kNone;
+    for (uint32_t i = lane; i < a.splits; i += 64) top = fmaxf(top, stats[2 * i]);
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    float total = 0.0f, y[E];
+    for (int e = 0; e < E; ++e) y[e] = 0.0f;
+    for (uint32_t i = 0; i < a.splits; ++i) {
+        const float w = stats[2 * i + 1];
+        if (w == 0.0f) continue;                         // a piece that the row sees nothing of
+        const float f = pow2(stats[2 * i] - top);
+        total += w * f;
+        for (int e = 0; e < E; ++e) y[e] += sums[(uint64_t)i * D + e] * f;
+    }
+    const float f = total == 0.0f ? 0.0f : 1.0f / total;
+    uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)token * a.out_stride + (uint64_t)head * D + lane * E;
+    for (int e = 0; e < E; ++e) dst[e] = (uint16_t)narrow<BF16>(y[e] * f);
+    if (a.lse && lane == 0) a.lse[id] = total == 0.0f ? -INFINITY : (top + log2_of(total)) * 0.69314718055994530942f;
+}
+
+}  // namespace
+
+AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length, uint32_t window) {
+    AttendLaunch l;
+    const uint64_t group = s.q_heads / s.kv_heads;
+    l.rows = 16;
+    const uint64_t each = (max_new * group + l.rows - 1) / l.rows, packed = tokens * group / l.rows + requests;
+    // the same number for every request saves the search for a tile's request; where requests differ much it would
+    // launch more workgroups than there are tiles
+    l.tiles_each = each == 0 ? 1u : (uint32_t)(each * requests <= packed ? each : 0);
+    l.tiles = (uint32_t)(l.tiles_each ? (uint64_t)l.tiles_each * requests : packed);
+    uint64_t reach = max_length;
+    if (window && reach > (uint64_t)window + max_new) reach = (uint64_t)window + max_new;
+    const uint64_t units = (uint64_t)l.tiles * s.kv_heads, want = 1024;
+    uint64_t splits = units >= want ? 1 : want / units, most = (reach + 255) / 256;
+    if (splits > most) splits = most;
+    if (splits == 0) splits = 1;
+    l.chunk = (uint32_t)(((reach + splits - 1) / splits + 63) / 64 * 64);
+    if (l.chunk == 0) l.chunk = 64;
+    l.splits = (uint32_t)splits;
+    return l;
+}
+
+#define TSQ_BY_SHAPE(kernel, grid, ...)                                                                                     \
+    do {                                                                                                                    \
+        if (s.head_dim == 64) { if (s.bf16) kernel<64, true><<<grid, 256, 0, st>>>(__VA_ARGS__); else kernel<64, false><<<grid, 256, 0, st>>>(__VA_ARGS__); }          \
+        else if (s.head_dim == 128) { if (s.bf16) kernel<128, true><<<grid, 256, 0, st>>>(__VA_ARGS__); else kernel<128, false><<<grid, 256, 0, st>>>(__VA_ARGS__); }  \
+        else { if (s.bf16) kernel<256, true><<<grid, 256, 0, st>>>(__VA_ARGS__); else kernel<256, false><<<grid, 256, 0, st>>>(__VA_ARGS__); }                         \
+    } while (0)
+
+int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &a, void *stream) {
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    TSQ_BY_SHAPE(k_attend_few, l.tiles * l.splits * s.kv_heads, a);
+    if (hipError_t e = hipGetLastError()) return (int)e;
+    if (l.splits > 1) {
+        TSQ_BY_SHAPE(k_attend_join, (uint32_t)((a.part_rows + 3) / 4), a);
+        return (int)hipGetLastError();
+    }
+    return 0;
+}
+
+}  // namespace tsq

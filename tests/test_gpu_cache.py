@@ -1,0 +1,635 @@
+"""The serving operators on the GPU, through the C ABI, against the plain oracle (oracle/cache_oracle.py)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as O
+from paper_2511_04002_amd import cache as cachelib
+from paper_2511_04002_amd import tsq
+
+pytestmark = pytest.mark.gpu
+
+KIND = {"f16": torch.float16, "bf16": torch.bfloat16}
+HALF_ULP = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}       # relative, of one rounding
+TINY = {"f16": 2.0 ** -25, "bf16": 2.0 ** -134}         # absolute, below the normal range
+
+
+def dev(x, kind=None):
+    t = torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    return t if kind is None else t.to(kind)
+
+
+def host(t):
+    return (t.float() if t.dtype in (torch.float16, torch.bfloat16) else t).cpu().numpy()
+
+
+# ------------------------------------------------------------------ schedule
+
+def schedule_both(new, lengths, table, ring, counters, block, max_blocks, capacity):
+    c = cachelib.Cache(len(ring), block, 1, 1, 64, "f16", max_blocks)
+    t, r = dev(table), dev(ring)
+    out = c.new_schedule(len(new), capacity)
+    for x in (out.lengths, out.counters, out.starts, out.positions, out.slots, out.status):
+        x.fill_(77)
+    c.schedule(dev(new), dev(lengths), t, r, dev(counters), out)
+    want = O.schedule(new, lengths, table, ring, counters, block, max_blocks, capacity)
+    got = dict(status=int(out.status.item()), lengths=host(out.lengths), counters=host(out.counters), starts=host(out.starts),
+               positions=host(out.positions), slots=host(out.slots), table=host(t), ring=host(r))
+    for n in want:
+        assert np.array_equal(got[n], want[n]), n
+    return want, out
+
+
+def pool(seed, lengths, block, max_blocks, extra=5, turned=0):
+    """Tables of requests of these lengths, and the ring of what is left, which has gone round `turned` times its size."""
+    g = np.random.default_rng(seed)
+    held = [-(-n // block) for n in lengths]
+    blocks = sum(held) + extra
+    ids = g.permutation(blocks).astype(np.int32)
+    table = np.full((len(lengths), max_blocks), -1, np.int32)
+    at = 0
+    for r, n in enumerate(held):
+        table[r, :n] = ids[at:at + n]
+        at += n
+    ring = np.full(blocks, -9, np.int32)
+    taken = turned * blocks + int(g.integers(blocks))
+    for i, b in enumerate(ids[at:]):
+        ring[(taken + i) % blocks] = b
+    return table, ring, np.array([taken, taken + extra], np.int64)
+
+
+@pytest.mark.parametrize("requests", [1, 2, 63, 64, 65, 1000, 4096])
+@pytest.mark.parametrize("block", [16, 128])
+def test_schedule_of_mixed_requests(requests, block):
+    g = np.random.default_rng(requests + block)
+    lengths = g.integers(0, 5 * block, requests).astype(np.int32)
+    new = g.choice([-1, 0, 1, 2, block - 1, block, block + 1, 3 * block], requests).astype(np.int32)
+    table, ring, counters = pool(1, lengths.tolist(), block, 9, extra=4 * requests + 3, turned=3)
+    want, _ = schedule_both(new, lengths, table, ring, counters, block, 9, int(np.maximum(new, 0).sum()) + 11)
+    assert want["status"] == O.OK
+
+
+@pytest.mark.parametrize("tokens", [1, 4095, 4096, 4097, 70000])
+def test_schedule_of_one_long_request(tokens):
+    table, ring, counters = pool(2, [17], 16, 5000, extra=4500, turned=10 ** 9)
+    schedule_both(np.array([tokens], np.int32), np.array([17], np.int32), table, ring, counters, 16, 5000, tokens)
+
+
+def test_schedule_goes_on_from_its_own_outputs_and_blocks_come_back():
+    c = cachelib.Cache(12, 16, 1, 1, 64, "f16", 4)
+    table, ring, counters, lengths = c.new_table(3), c.new_ring(), c.new_counters(), c.new_lengths(3)
+    t, r, n, ct = host(table), host(ring), host(lengths), host(counters)
+    for step, new in enumerate([[20, 64, 1], [1, 0, 15], [-1, 0, 1], [60, -1, 0], [4, 64, 16], [-1, -1, -1], [64, 64, 64]]):
+        new = np.array(new, np.int32)
+        out = c.schedule(dev(new), lengths, table, ring, counters, c.new_schedule(3, 200))
+        want = O.schedule(new, n, t, r, ct, 16, 4, 200)
+        for a, b in ((out.lengths, "lengths"), (out.counters, "counters"), (out.slots, "slots"), (table, "table"), (ring, "ring")):
+            assert np.array_equal(host(a), want[b]), (step, b)
+        out.check()
+        lengths, counters = out.lengths, out.counters
+        t, r, n, ct = want["table"], want["ring"], want["lengths"], want["counters"]
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(new=[100, 1]), O.CAPACITY),                    # more blocks than are free
+    (dict(new=[0, 200]), O.CAPACITY),                    # longer than a row of the table
+    (dict(new=[30, 31], capacity=60), O.CAPACITY),       # more tokens than the outputs hold
+    (dict(new=[2 ** 31 - 1, 1]), O.CAPACITY),
+    (dict(new=[-2, 1]), O.INVALID),
+    (dict(lengths=[-1, 0]), O.INVALID),
+    (dict(lengths=[2 ** 31 - 1, 0], new=[0, 0]), O.INVALID),
+    (dict(counters=[5, 4]), O.INVALID),
+    (dict(counters=[-1, 4]), O.INVALID),
+    (dict(counters=[0, 100]), O.INVALID),
+    (dict(counters=[0, 9], new=[-1, -1]), O.INVALID),    # more blocks come back than there are
+])
+def test_schedule_that_cannot_be_taken_changes_nothing(change, status):
+    lengths = np.array(change.get("lengths", [30, 5]), np.int32)
+    table, ring, counters = pool(3, [30, 5], 16, 8, extra=7)
+    if "counters" in change:
+        counters = np.array(change["counters"], np.int64)
+    want, out = schedule_both(np.array(change.get("new", [1, 1]), np.int32), lengths, table, ring, counters, 16, 8, change.get("capacity", 400))
+    assert want["status"] == status
+    with pytest.raises(tsq.TsqError):
+        out.check()
+
+
+def test_schedule_of_tables_that_hold_no_block_gives_no_slot():
+    table = np.array([[3, 99, -1], [-5, 0, 0]], np.int32)
+    schedule_both(np.array([20, 2], np.int32), np.array([8, 3], np.int32), table, np.array([4, 50, 6, 7, 5], np.int32),
+                  np.array([0, 5], np.int64), 16, 3, 30)
+
+
+# ------------------------------------------------------------------ norm and rotation
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads", [(1, 1), (12, 12), (40, 8), (7, 1)])
+@pytest.mark.parametrize("dim,rotary", [(64, 64), (64, 16), (128, 128), (128, 48), (256, 256), (256, 64)])
+@pytest.mark.parametrize("pairs", ["halves", "neighbours"])
+def test_norm_rotate(dtype, heads, dim, rotary, pairs):
+    g = np.random.default_rng(dim + rotary)
+    hq, hk = heads
+    for tokens, normed, packed in ((1, True, False), (5, False, True), (67, True, True)):
+        c = cachelib.Cache(1, 16, hq, hk, dim, dtype, 1)
+        width = (hq + 2 * hk) * dim
+        x = dev(g.standard_normal((tokens, width)) * g.choice([0.01, 1.0, 30.0], (1, width)), KIND[dtype])
+        q, k = x[:, :hq * dim], x[:, hq * dim:(hq + hk) * dim]
+        if not packed:
+            q, k = q.contiguous().view(tokens, hq, dim), k.contiguous().view(tokens, hk, dim)
+        angles = g.uniform(-1, 1, (300, rotary)).astype(np.float32)
+        positions = g.integers(0, 300, tokens).astype(np.int32)
+        weights = [dev(g.standard_normal(dim), KIND[dtype]) if normed else None for _ in range(2)]
+        got = c.norm_rotate(q, k, dev(positions), dev(angles), weights[0], weights[1], 1e-5, pairs)
+        for y, z, h, w in ((q, got[0], hq, weights[0]), (k, got[1], hk, weights[1])):
+            src = host(y).reshape(tokens, h, dim)
+            want = O.norm_rotate(src, None if w is None else host(w), 1e-5, angles, positions, rotary, pairs == "neighbours")
+            # one rounding to 16 bits, and a few in binary32 of the two products
+            size = np.abs(O.norm_rotate(np.abs(src), None if w is None else np.abs(host(w)), 1e-5, np.abs(angles), positions, rotary, pairs == "neighbours"))
+            size = np.maximum(size, np.abs(want)).max(-1, keepdims=True)
+            assert (np.abs(host(z) - want) <= HALF_ULP[dtype] * np.abs(want) + 2.0 ** -18 * size + TINY[dtype]).all()
+
+
+def test_norm_rotate_in_place_and_rows_without_a_position():
+    g = np.random.default_rng(5)
+    c = cachelib.Cache(1, 16, 4, 2, 128, "bf16", 1)
+    x = dev(g.standard_normal((9, 8 * 128)), torch.bfloat16)
+    before = x.clone()
+    q, k = x[:, :512], x[:, 512:768]
+    angles = dev(g.uniform(-1, 1, (50, 128)).astype(np.float32))
+    positions = dev(np.array([0, -1, 49, 50, 3, -7, 2 ** 31 - 1, 7, 8], np.int32))
+    w = dev(g.standard_normal(128), torch.bfloat16)
+    want = c.norm_rotate(q, k, positions, angles, w, w)
+    rows = [0, 2, 4, 7, 8]
+    c.norm_rotate(q, k, positions, angles, w, w, q_out=q, k_out=k)
+    for a, b in ((q, want[0]), (k, want[1])):
+        assert torch.equal(a[rows], b.flatten(1)[rows])
+        assert a[[3, 6]].isnan().all()                       # past the angles
+    assert torch.equal(x[[1, 5]], before[[1, 5]]) and torch.equal(x[:, 768:], before[:, 768:])
+
+
+def test_norm_rotate_leaves_what_does_not_turn():
+    c = cachelib.Cache(1, 16, 1, 1, 64, "f16", 1)
+    x = torch.full((1, 64), float("inf"), dtype=torch.float16, device="cuda")
+    angles = torch.zeros((1, 32), device="cuda")
+    q, _ = c.norm_rotate(x, x.clone(), torch.zeros(1, dtype=torch.int32, device="cuda"), angles)
+    assert q[0, 0, 32:].isinf().all() and q[0, 0, :32].isnan().all()      # inf * cos 0
+
+
+def test_norm_rotate_of_no_tokens():
+    c = cachelib.Cache(1, 16, 1, 1, 64, "f16", 1)
+    x = torch.empty((0, 64), dtype=torch.float16, device="cuda")
+    q, k = c.norm_rotate(x, x, torch.empty(0, dtype=torch.int32, device="cuda"), torch.zeros((1, 64), device="cuda"))
+    assert q.shape == (0, 1, 64) and k.shape == (0, 1, 64)
+
+
+# ------------------------------------------------------------------ append and gather
+
+class Both:
+    """A cache on the GPU and the same one in the oracle."""
+
+    def __init__(self, blocks, block, heads, dim, dtype, max_blocks, seed, q_heads=None):
+        self.c = cachelib.Cache(blocks, block, q_heads or heads, heads, dim, dtype, max_blocks)
+        g = self.g = np.random.default_rng(seed)
+        self.block, self.heads, self.dim, self.dtype, self.max_blocks = block, heads, dim, dtype, max_blocks
+        self.k = g.integers(-127, 128, (blocks, heads, block, dim)).astype(np.int8)
+        self.v = g.integers(-127, 128, (blocks, heads, dim, block)).astype(np.int8)
+        self.ks, self.vs = (np.exp(g.standard_normal((blocks, heads))).astype(np.float32) / 40 for _ in range(2))
+        self.m = self.c.wrap(dev(self.k), dev(self.v), dev(self.ks), dev(self.vs))
+
+    def append(self, k, v, slots):
+        """k, v: CUDA tensors [tokens, heads, dim]."""
+        slots = np.asarray(slots, np.int32)
+        self.c.append(self.m, k, v, dev(slots))
+        O.append(self.k, self.v, self.ks, self.vs, host(k), host(v), slots, self.block)
+
+    def same(self, filled):
+        """Codes of the places that hold tokens ({block: how many}) and the scales of those blocks are the oracle's."""
+        k, v, ks, vs = (host(x) for x in (self.m.k, self.m.v, self.m.k_scale, self.m.v_scale))
+        for b, n in filled.items():
+            for got, want in ((ks[b], self.ks[b]), (vs[b], self.vs[b])):
+                assert np.array_equal(got, want, equal_nan=True), b
+            fine = ~np.isnan(self.ks[b])
+            assert np.array_equal(k[b][fine, :n], self.k[b][fine, :n]), b
+            fine = ~np.isnan(self.vs[b])
+            assert np.array_equal(v[b][fine, :, :n], self.v[b][fine, :, :n]), b
+
+
+def rows(g, tokens, heads, dim, dtype, scale=1.0):
+    return dev(g.standard_normal((tokens, heads, dim)) * scale, KIND[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+def test_append_of_runs_of_all_lengths(dtype, dim, block):
+    b = Both(9, block, 3, dim, dtype, 9, dim + block)
+    filled, at = {}, 0
+    g = b.g
+    order = g.permutation(9)
+    # a request that grows by runs of many lengths over all its blocks, larger and smaller values in turn
+    for i, n in enumerate([1, 1, 3, block - 5, 1, block, 2 * block + 7, 5, 17, 1, block - 1]):
+        n = min(n, 9 * block - at)
+        slots = [int(order[t // block]) * block + t % block for t in range(at, at + n)]
+        b.append(rows(g, n, 3, dim, dtype, [1.0, 3.0, 0.2, 10.0][i % 4]), rows(g, n, 3, dim, dtype, [2.0, 0.1, 5.0][i % 3]), slots)
+        at += n
+        filled = {int(order[j]): min(block, at - j * block) for j in range(-(-at // block))}
+        b.same(filled)
+
+
+def test_append_of_one_token_each_of_many_requests_from_strided_rows():
+    b = Both(70, 16, 2, 128, "bf16", 1, 3)
+    g = b.g
+    filled = {}
+    for step in range(18):
+        ids = g.permutation(70)[:65]
+        slots = [int(i) * 16 + filled.get(int(i), 0) if filled.get(int(i), 0) < 16 else -1 for i in ids]
+        qkv = rows(g, 65, 9, 128, "bf16", float(g.choice([0.5, 1, 2])))
+        b.append(qkv[:, 5:7], qkv[:, 7:9], slots)
+        for s in slots:
+            if s >= 0:
+                filled[s // 16] = s % 16 + 1
+        b.same(filled)
+
+
+def test_append_skips_slots_outside_the_cache():
+    b = Both(4, 16, 1, 64, "f16", 4, 4)
+    slots = [-1, 64, 65, 2 ** 31 - 1, 16, 17, 18, -1, 48]
+    b.append(rows(b.g, 9, 1, 64, "f16"), rows(b.g, 9, 1, 64, "f16"), slots)
+    k = host(b.m.k)
+    assert np.array_equal(k[0], b.k[0]) and np.array_equal(k[2], b.k[2])
+    b.same({1: 3, 3: 1})
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_append_of_zeros_tiny_and_huge_values(dtype):
+    b = Both(8, 16, 1, 64, dtype, 8, 6)
+    big = 65504.0 if dtype == "f16" else 3.3895313e38
+    tiny = 2.0 ** -24 if dtype == "f16" else 2.0 ** -133
+    for block, first, second in ((0, 0.0, 0.0), (1, 0.0, 1.0), (2, big, -big), (3, tiny, tiny), (4, tiny, big), (5, 2.0 ** -14, 0.0)):
+        for place, value in ((0, first), (1, second), (2, first)):
+            x = torch.full((1, 1, 64), value, dtype=KIND[dtype], device="cuda")
+            b.append(x, x, [block * 16 + place])
+        b.same({block: 3})
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_append_of_values_that_are_not_finite_marks_the_block_and_a_new_use_clears_it(bad):
+    b = Both(3, 16, 2, 128, "f16", 3, 7)
+    x = rows(b.g, 5, 2, 128, "f16")
+    x[3, 1, 77] = bad
+    b.append(x, rows(b.g, 5, 2, 128, "f16"), range(16, 21))
+    b.same({1: 5})
+    assert np.isnan(b.ks[1, 1]) and not np.isnan(b.ks[1, 0]) and not np.isnan(b.vs[1]).any()
+    b.append(rows(b.g, 2, 2, 128, "f16"), rows(b.g, 2, 2, 128, "f16"), [21, 22])
+    b.same({1: 7})
+    assert np.isnan(b.ks[1, 1])
+    b.append(rows(b.g, 2, 2, 128, "f16"), rows(b.g, 2, 2, 128, "f16"), [16, 17])
+    b.same({1: 2})
+    assert not np.isnan(b.ks[1]).any()
+
+
+def test_append_keeps_elements_within_half_a_step():
+    b = Both(64, 16, 4, 128, "bf16", 64, 8)
+    x, y = rows(b.g, 1000, 4, 128, "bf16", 2.0), rows(b.g, 1000, 4, 128, "bf16", 0.3)
+    b.append(x, y, range(1000))
+    k = O.tokens_of(host(b.m.k), host(b.m.k_scale), np.arange(64), 1000, 16, 64)
+    step = host(b.m.k_scale)[np.arange(1000) // 16][:, :, None]
+    assert (np.abs(k - host(x)) <= 0.5 * step * (1 + 2.0 ** -15)).all()     # x * (1 / s): three roundings
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("block", [16, 32, 128])
+def test_gather(dtype, dim, block):
+    b = Both(60, block, 3, dim, dtype, 8, dim + block)
+    g = b.g
+    lengths = np.array([1, 0, block, 5 * block + 3, block - 1, 2, 8 * block], np.int32)
+    # all of a request, a part of it, more than it has, and none
+    counts = [1, 2, block, 2 * block + 5, 0, 2, 8 * block - 3]
+    table = g.permutation(60)[:56].reshape(7, 8).astype(np.int32)
+    table[3, 4] = 60
+    starts = np.concatenate(([0], np.cumsum(counts))).astype(np.int32)
+    total = int(starts[-1])
+    out = [torch.full((total + 3, 3, dim), 7.0, dtype=KIND[dtype], device="cuda") for _ in range(2)]
+    b.c.gather(b.m, dev(table), dev(starts), dev(lengths), *out)
+    for got, codes, scale in ((out[0], b.k, b.ks), (out[1], b.v.swapaxes(2, 3), b.vs)):
+        got = host(got)
+        assert (got[total:] == 7).all()
+        for r, n in enumerate(counts):
+            want = O.tokens_of(codes, scale, table[r], int(lengths[r]), block, 8)
+            want = np.concatenate((np.full((max(0, n - len(want)), 3, dim), np.nan), want))[len(want) - n if n < len(want) else 0:]
+            part = got[starts[r]:starts[r + 1]]
+            assert np.array_equal(np.isnan(part), np.isnan(want)), r
+            # code * scale in binary32, then one rounding
+            fine = ~np.isnan(want)
+            assert (np.abs(part - want)[fine] <= (HALF_ULP[dtype] + 2.0 ** -22) * np.abs(want)[fine] + TINY[dtype]).all(), r
+
+
+def test_gather_into_rows_that_the_compressor_takes():
+    b = Both(40, 16, 4, 128, "f16", 20, 9)
+    table = dev(b.g.permutation(40).reshape(2, 20).astype(np.int32))
+    starts, lengths = dev(np.array([0, 100, 320], np.int32)), dev(np.array([100, 220], np.int32))
+    k, v = (torch.empty((320, 512), dtype=torch.float16, device="cuda") for _ in range(2))
+    b.c.gather(b.m, table, starts, lengths, k, v)
+    plan = tsq.Plan(640, 512, "f16", 1e4, (8,), 0.05)
+    blob, _ = plan.compress_batch([k, v])
+    back = [torch.empty_like(k), torch.empty_like(v)]
+    plan.decompress_batch(blob, back)
+    for x, y in ((k, back[0]), (v, back[1])):
+        assert (x - y).abs().max() <= x.abs().max() / 127
+
+
+# ------------------------------------------------------------------ attention
+
+def attend_both(b, q_heads, counts, lengths, causal=True, window=0, table=None, q=None, max_new=None, max_length=None, scale=None,
+                extra=0, unused=0.0):
+    g, dim, dtype = b.g, b.dim, b.dtype
+    counts, lengths = np.asarray(counts), np.asarray(lengths, np.int32)
+    starts = np.concatenate(([0], np.cumsum(counts))).astype(np.int32)
+    total = int(starts[-1])
+    if table is None:
+        ids = g.permutation(b.k.shape[0])
+        table, at = np.full((len(counts), b.max_blocks), -1, np.int32), 0
+        for r, n in enumerate(lengths):
+            held = -(-int(n) // b.block)
+            table[r, :held] = ids[at:at + held]
+            at += held
+    if q is None:
+        q = rows(g, total + extra, q_heads, dim, dtype, 1.5)
+    scale = dim ** -0.5 if scale is None else scale
+    out = torch.full((total + extra, q_heads, dim), 7.0, dtype=KIND[dtype], device="cuda")
+    lse = torch.full((total + extra, q_heads), 7.0, device="cuda")
+    b.c.attend(b.m, q, dev(table), dev(starts), dev(lengths), max(counts) if max_new is None else max_new,
+               max(lengths) if max_length is None else max_length, scale, causal, window, out, lse)
+    got, got_lse = host(out), host(lse)
+    assert (got[total:] == 7).all() and (got_lse[total:] == 7).all()
+    with np.errstate(all="ignore"):
+        want, want_lse, spread = O.attend(b.k, b.v, b.ks, b.vs, b.block, b.max_blocks, table, starts, lengths, host(q)[:total], scale, causal, window)
+    got, got_lse = got[:total], got_lse[:total]
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isnan(got_lse), np.isnan(want_lse))
+    fine = ~np.isnan(want)
+    # an output's own rounding; a relative error of the weights acts on the sum of weight * |value|: half a unit of 11
+    # bits each (2^-11), and what binary32 makes of exponents of up to a few hundred (2^-24 of them)
+    # the smallest weights are rounded to a half's least step, 2^-24 where the largest weight is at least 2^7
+    least = 2.0 ** -32 * lengths.max() * 127 * float(b.vs[np.isfinite(b.vs)].max())
+    bound = HALF_ULP[dtype] * np.abs(want) + (2.0 ** -11 + 2.0 ** -14) * spread + TINY[dtype] + least
+    assert (np.abs(got - want)[fine] <= bound[fine]).all(), float((np.abs(got - want) / bound)[fine].max())
+    empty = np.isneginf(want_lse)
+    assert np.array_equal(np.isneginf(got_lse), empty)
+    fine = np.isfinite(want_lse)
+    assert (np.abs(got_lse - want_lse)[fine] <= 2.0 ** -19 * np.maximum(1, np.abs(want_lse))[fine] + 2.0 ** -17).all()
+    assert (got[empty] == 0).all()
+    return out, lse, want
+
+
+SHAPES = [(1, 1, 64), (12, 12, 64), (5, 1, 128), (8, 1, 128), (16, 2, 128), (28, 4, 128), (40, 2, 128), (4, 2, 256), (16, 1, 256)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads", SHAPES)
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+def test_attend_single_tokens(dtype, heads, block):
+    hq, hk, dim = heads
+    b = Both(90, block, hk, dim, dtype, 40, hq + block, q_heads=hq)
+    lengths = [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 200, 300]
+    attend_both(b, hq, [1] * len(lengths), lengths)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads", [(2, 2, 64), (8, 1, 128), (6, 2, 128), (4, 1, 256)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 40), (False, 17), (True, 100000)])
+def test_attend_several_tokens_and_chunks(dtype, heads, causal, window):
+    hq, hk, dim = heads
+    b = Both(90, 16, hk, dim, dtype, 40, hq + window, q_heads=hq)
+    attend_both(b, hq, [1, 2, 0, 8, 33, 70, 150, 3], [1, 90, 5, 8, 100, 70, 171, 300], causal, window)
+
+
+@pytest.mark.parametrize("block", [16, 64, 128])
+def test_attend_prompt(block):
+    b = Both(3000 // block + 2, block, 2, 128, "bf16", 3000 // block + 1, block, q_heads=8)
+    attend_both(b, 8, [517, 131], [517, 131])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads", [(1, 1, 64), (8, 1, 128), (4, 2, 256)])
+@pytest.mark.parametrize("counts,lengths", [([1], [7001]), ([3], [5000]), ([1, 1], [4097, 31]), ([40], [6000])])
+def test_attend_along_a_long_cache(dtype, heads, counts, lengths):
+    hq, hk, dim = heads
+    b = Both(620, 16, hk, dim, dtype, 500, 11, q_heads=hq)
+    need = cachelib.tsq_cache_attend_workspace_bytes(b.c.handle, len(counts), sum(counts), max(counts), max(lengths))
+    assert need > 0                                          # the cache's length is split and joined
+    attend_both(b, hq, counts, lengths)
+
+
+def test_attend_of_requests_larger_than_they_were_announced():
+    b = Both(300, 16, 2, 128, "f16", 120, 12, q_heads=8)
+    attend_both(b, 8, [9, 1, 40], [1800, 700, 40], max_new=1, max_length=1)
+    attend_both(b, 8, [9, 1, 40], [1800, 700, 40], max_new=1, max_length=600)
+    attend_both(b, 8, [9, 1, 40], [1800, 700, 40], max_new=0, max_length=0)
+
+
+def test_attend_rows_that_see_nothing():
+    b = Both(20, 16, 1, 64, "f16", 8, 13, q_heads=3)
+    # more queries than tokens, and a request without any
+    attend_both(b, 3, [5, 1, 40], [3, 0, 20])
+    attend_both(b, 3, [5, 1, 40], [3, 0, 20], causal=False)
+    attend_both(b, 3, [5, 1, 40], [3, 0, 20], window=2)
+    attend_both(b, 3, [1, 2], [0, 0], extra=3)
+
+
+def test_attend_rows_that_no_request_has():
+    b = Both(20, 16, 2, 128, "bf16", 8, 14, q_heads=2)
+    attend_both(b, 2, [1, 2], [30, 40], extra=5)
+    attend_both(b, 2, [30, 2], [30, 40], extra=50)
+
+
+def test_attend_many_requests():
+    b = Both(1400, 16, 1, 64, "f16", 12, 15, q_heads=2)
+    g = b.g
+    lengths = g.integers(0, 60, 300)
+    attend_both(b, 2, [1] * 300, lengths)
+    counts = np.minimum(g.integers(0, 9, 300), lengths)
+    counts[7] = lengths[7] = 150
+    attend_both(b, 2, counts, lengths)
+
+
+def test_attend_table_entries_outside_the_cache_and_lengths_past_the_table():
+    b = Both(20, 16, 1, 128, "f16", 6, 16, q_heads=4)
+    table = b.g.permutation(20)[:18].reshape(3, 6).astype(np.int32)
+    table[1, 2] = 20
+    table[2, 0] = -3
+    attend_both(b, 4, [50, 45, 2], [90, 48, 30], table=table)
+    attend_both(b, 4, [1, 1, 1], [97, 96, 10], table=table)
+
+
+def test_attend_marked_blocks_reach_only_the_rows_that_see_them():
+    b = Both(20, 16, 2, 128, "f16", 10, 17, q_heads=4)
+    table = np.arange(20, dtype=np.int32).reshape(2, 10)
+    b.ks[3, 0] = b.vs[5, 1] = b.vs[14, 0] = np.nan
+    b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
+    attend_both(b, 4, [130, 1], [150, 100], table=table)
+    attend_both(b, 4, [130, 1], [150, 100], table=table, window=20)
+
+
+def test_attend_ignores_what_lies_behind_a_request_and_in_blocks_of_nobody():
+    b = Both(6, 16, 1, 64, "bf16", 4, 18, q_heads=2)
+    table = np.array([[1, 2, 5, 5], [3, 5, 5, 0]], np.int32)
+    b.ks[[0, 4, 5]] = np.nan
+    b.vs[[0, 4, 5]] = np.inf
+    b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
+    attend_both(b, 2, [1, 3], [20, 9], table=table)
+    attend_both(b, 2, [20, 9], [20, 9], table=table)
+
+
+def test_attend_blocks_of_zeros_and_scales_far_apart():
+    b = Both(40, 16, 1, 128, "bf16", 20, 19, q_heads=2)
+    table = b.g.permutation(40).reshape(2, 20).astype(np.int32)
+    b.vs[table[0, ::3]] = 0.0
+    b.v[table[0, ::3]] = 0
+    b.ks[table[0, 5]] = 0.0
+    b.k[table[0, 5]] = 0
+    b.vs[table[1]] *= np.float32(2.0) ** b.g.integers(-8, 8, (20, 1)).astype(np.float32)
+    b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
+    attend_both(b, 2, [1, 1], [301, 317], table=table)
+    attend_both(b, 2, [60, 60], [301, 317], table=table)
+    attend_both(b, 2, [301, 317], [301, 317], table=table)
+
+
+def test_attend_one_token_that_takes_all_the_weight_and_queries_far_from_one():
+    for dtype in ("f16", "bf16"):
+        b = Both(40, 16, 1, 128, dtype, 20, 20, q_heads=3)
+        q = rows(b.g, 40, 3, 128, dtype, 30.0)
+        attend_both(b, 3, [40], [300], q=q)
+        q = rows(b.g, 40, 3, 128, dtype, 2.0 ** -10)
+        attend_both(b, 3, [40], [300], q=q)
+        q[:] = 0
+        attend_both(b, 3, [40], [300], q=q)
+        if dtype == "bf16":
+            q = rows(b.g, 40, 3, 128, dtype, 2.0 ** 60)
+            attend_both(b, 3, [40], [300], q=q, scale=2.0 ** -64)
+
+
+def test_attend_queries_that_are_not_finite_spoil_their_own_rows_only():
+    b = Both(40, 16, 1, 128, "bf16", 20, 21, q_heads=4)
+    q = rows(b.g, 41, 4, 128, "bf16")
+    table = b.g.permutation(40).reshape(2, 20).astype(np.int32)
+    good = b.c.attend(b.m, q, dev(table), dev(np.array([0, 1, 41], np.int32)), dev(np.array([200, 90], np.int32)), 40, 200)
+    q2 = q.clone()
+    q2[0, 1, 5], q2[20, 2, 100], q2[33, 0, 64] = float("nan"), float("inf"), -float("inf")
+    got = b.c.attend(b.m, q2, dev(table), dev(np.array([0, 1, 41], np.int32)), dev(np.array([200, 90], np.int32)), 40, 200)
+    bad = torch.zeros((41, 4), dtype=torch.bool, device="cuda")
+    bad[0, 1] = bad[20, 2] = bad[33, 0] = True
+    assert got[bad].isnan().all() and torch.equal(got[~bad], good[~bad])
+
+
+def test_attend_gives_the_same_bits_again_on_another_stream_with_a_workspace_of_its_own():
+    b = Both(620, 16, 2, 128, "f16", 300, 22, q_heads=16)
+    table = dev(b.g.permutation(620)[:600].reshape(2, 300).astype(np.int32))
+    starts, lengths = dev(np.array([0, 1, 2], np.int32)), dev(np.array([4800, 3333], np.int32))
+    q = rows(b.g, 2, 16, 128, "f16")
+    first = b.c.attend(b.m, q, table, starts, lengths, 1, 4800)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        ws = b.c.new_workspace(2, 2, 1, 4800)
+        assert ws is not None
+        outs = [b.c.attend(b.m, q, table, starts, lengths, 1, 4800, ws=ws) for _ in range(20)]
+    torch.cuda.current_stream().wait_stream(stream)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o, first)
+
+
+def test_attend_reads_strided_queries_and_writes_strided_outputs():
+    b = Both(30, 16, 2, 64, "f16", 10, 23, q_heads=4)
+    qkv = rows(b.g, 5, 8, 64, "f16")
+    wide = torch.zeros((5, 11 * 64), dtype=torch.float16, device="cuda")
+    table = dev(b.g.permutation(30).reshape(3, 10).astype(np.int32))
+    starts, lengths = dev(np.array([0, 1, 3, 5], np.int32)), dev(np.array([100, 150, 7], np.int32))
+    want = b.c.attend(b.m, qkv[:, :4].contiguous(), table, starts, lengths, 2, 150)
+    b.c.attend(b.m, qkv[:, :4], table, starts, lengths, 2, 150, out=wide[:, 128:384])
+    assert torch.equal(wide[:, 128:384], want.flatten(1)) and (wide[:, :128] == 0).all() and (wide[:, 384:] == 0).all()
+
+
+# ------------------------------------------------------------------ the step as a whole
+
+def test_a_step_in_a_graph_replayed_with_other_data_between():
+    c = cachelib.Cache(64, 16, 8, 2, 128, "bf16", 32)
+    requests, tokens = 3, 3
+    memory, table, ring = c.new_memory(), c.new_table(requests), c.new_ring()
+    lengths, counters = c.new_lengths(requests), c.new_counters()
+    new = torch.ones(requests, dtype=torch.int32, device="cuda")
+    out = c.new_schedule(requests, tokens)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    angles = torch.rand((512, 128), device="cuda", generator=g)
+    x = torch.zeros((tokens, 12 * 128), dtype=torch.bfloat16, device="cuda")
+    y = torch.zeros((tokens, 8, 128), dtype=torch.bfloat16, device="cuda")
+
+    def step(c, memory, table, ring, lengths, counters, out, y):
+        c.schedule(new, lengths, table, ring, counters, out)
+        q, k = c.norm_rotate(x[:, :1024], x[:, 1024:1280], out.positions, angles)
+        c.append(memory, k, x[:, 1280:].unflatten(1, (2, 128)), out.slots)
+        c.attend(memory, q, table, out.starts, out.lengths, 1, 512, out=y)
+        lengths.copy_(out.lengths)
+        counters.copy_(out.counters)
+
+    eager = dict(memory=c.new_memory(), table=c.new_table(requests), ring=c.new_ring(), lengths=c.new_lengths(requests),
+                 counters=c.new_counters(), out=c.new_schedule(requests, tokens), y=torch.zeros_like(y))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):                            # once outside, as a capture wants it; then back to the beginning
+        step(c, memory, table, ring, lengths, counters, out, y)
+    torch.cuda.current_stream().wait_stream(side)
+    lengths.zero_()
+    counters.copy_(c.new_counters())
+    ring.copy_(c.new_ring())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(c, memory, table, ring, lengths, counters, out, y)
+    for i in range(40):
+        x.copy_(torch.randn(x.shape, device="cuda", generator=g))
+        graph.replay()
+        step(c, **eager)
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager["y"]) and torch.equal(lengths, eager["lengths"]) and torch.equal(table, eager["table"]), i
+    assert int(lengths[0]) == 40
+
+
+@pytest.mark.parametrize("call", ["norm_rotate", "append", "gather", "attend", "schedule", "wrap"])
+def test_tensors_that_do_not_fit_are_refused(call):
+    c = cachelib.Cache(4, 16, 4, 2, 128, "f16", 2)
+    m = c.new_memory()
+    h = lambda *s: torch.zeros(s, dtype=torch.float16, device="cuda")        # noqa: E731
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")          # noqa: E731
+    angles = torch.zeros((9, 128), device="cuda")
+    if call == "norm_rotate":
+        good = [h(3, 4, 128), h(3, 2, 128), i(3), angles]
+        wrong = [(0, h(3, 3, 128)), (0, h(3, 4, 128).bfloat16()), (0, h(3, 4, 128).cpu()), (0, h(3, 4, 256)[..., ::2]), (1, h(2, 2, 128)),
+                 (2, i(2)), (2, i(3).long()), (3, angles.double()), (3, angles[:, ::2])]
+        f = c.norm_rotate
+    elif call == "append":
+        good = [m, h(3, 2, 128), h(3, 2, 128), i(3)]
+        wrong = [(1, h(3, 4, 128)), (2, h(4, 2, 128)), (3, i(4)), (3, i(6)[::2])]
+        f = c.append
+    elif call == "gather":
+        good = [m, i(2, 2), i(3), i(2), h(3, 2, 128), h(3, 2, 128)]
+        wrong = [(1, i(2, 3)), (2, i(2)), (4, h(3, 2, 64)), (5, h(2, 2, 128))]
+        f = c.gather
+    elif call == "attend":
+        good = [m, h(3, 4, 128), i(2, 2), i(3), i(2), 2, 9]
+        wrong = [(1, h(3, 2, 128)), (2, i(3, 2)), (3, i(4)), (4, i(2).long())]
+        f = c.attend
+    elif call == "schedule":
+        good = [i(2), i(2), i(2, 2), i(4), c.new_counters(), c.new_schedule(2, 5)]
+        wrong = [(0, i(2, 1)), (1, i(3)), (2, i(2, 3)), (3, i(5)), (4, i(2)), (5, c.new_schedule(3, 5))]
+        f = c.schedule
+    else:
+        good = [m.k, m.v, m.k_scale, m.v_scale]
+        wrong = [(0, m.k.float()), (1, m.v.transpose(2, 3)), (2, m.k_scale.cpu()), (3, m.v_scale[:3])]
+        f = c.wrap
+    for at, x in wrong:
+        args = list(good)
+        args[at] = x
+        with pytest.raises(ValueError):
+            f(*args)
