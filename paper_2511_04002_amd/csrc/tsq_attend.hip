@@ -327,6 +327,220 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
     }
 }
 
+// Many rows: 128 of a kv head's in a workgroup of four waves, 32 each.  A tile of 64 tokens goes through registers
+// into LDS, as halves, once for all rows: the waves' threads convert a share of it each while the other buffer is
+// worked on.
+// Lane (n = lane % 32, hi = lane / 32).  S^T in two 32 x 32 pieces: register i of a piece is token
+// 8 (i / 4) + 4 hi + i % 4, row n.  P^T as an operand of 16 tokens wants eight of them from each half of the wave:
+// registers 8u .. 8u + 7 are tokens 4 hi + (0..3) and 8 + 4 hi + (0..3) of the 16, so the values' rows in LDS hold
+// each 16 tokens in the order 0-3, 8-11, 4-7, 12-15.
+template <int D>
+struct ManyTile {                                        // rows padded by 16 bytes: neighbours begin four banks apart
+    _Float16 k[64][D + 8];
+    _Float16 v[D][64 + 8];
+    float k_scale[4], log_v[4], back_v[4];               // of each 16 tokens
+};
+
+template <int D, bool BF16>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a) {
+    constexpr int N = D / 64;                            // 16-byte pieces of keys, and of values, that a thread stages
+    __shared__ ManyTile<D> buffer[2];
+    Place p;
+    if (!find_place<128>(a, p)) return;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, hi = lane >> 5;
+    const uint32_t B = 1u << a.block_log2;
+    for (uint32_t tile = p.tile;; ++tile) {
+        const uint32_t row = tile * 128 + wave * 32 + n, rows = p.n * a.group;
+        half8_t q[D / 16];
+        float back = 1.0f;
+        {
+            uint4_t w[D / 16];
+            uint32_t most = 0;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                w[s] = uint4_t{0, 0, 0, 0};
+                if (row < rows) {
+                    const uint16_t *src = static_cast<const uint16_t *>(a.q) + (uint64_t)(p.begin + row / a.group) * a.q_stride +
+                                          (uint64_t)(p.h * a.group + row % a.group) * D + 16 * s + 8 * hi;
+                    w[s] = *reinterpret_cast<const uint4_t *>(src);
+                }
+                most = max(most, piece_most(w[s]));
+            }
+            float factor = 1.0f;
+            if constexpr (BF16) {
+                most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+                factor = query_factor(most, back);
+            }
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) q[s] = query_piece<BF16>(w[s], factor);
+        }
+        const float row_factor = back * a.scale_log2;
+        uint32_t from, to;
+        row_sees(a, p, row, from, to);
+        const Reach reach = reach_of<128>(a, p, tile);
+
+        float16_t acc[D / 32];
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+            for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
+        float ref = kNone, weight = 0.0f;
+
+        // staging: what this thread brings of a tile
+        uint32_t key_id[N], value_id = 0;
+        uint4_t kw[N], vw[N];
+        float k_scale = 0.0f, v_scale = 0.0f;
+        auto ask_ids = [&](uint32_t t0) {
+            bool bad;
+#pragma unroll
+            for (int i = 0; i < N; ++i) key_id[i] = block_id(a, p, t0 + (i * 256 + tid) / (D / 16), bad);
+            value_id = block_id(a, p, t0 + 16 * (tid & 3), bad);
+            if (bad) value_id |= 1u << 31;               // (a block number has 27 bits)
+        };
+        auto ask = [&](uint32_t t0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t e = i * 256 + tid, token = t0 + e / (D / 16), piece = e % (D / 16);
+                kw[i] = *reinterpret_cast<const uint4_t *>(a.k + (((uint64_t)key_id[i] * a.kv_heads + p.h) * B + (token & (B - 1))) * D + 16 * piece);
+            }
+            const uint64_t head = (uint64_t)(value_id & 0x7FFFFFFFu) * a.kv_heads + p.h;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                vw[i] = *reinterpret_cast<const uint4_t *>(a.v + (head * D + (i * 256 + tid) / 4) * B + ((t0 + 16 * (tid & 3)) & (B - 1)));
+            if (tid < 4) {
+                k_scale = value_id >> 31 ? __builtin_nanf("") : a.k_scale[head];
+                v_scale = a.v_scale[head];
+            }
+        };
+        auto put = [&](ManyTile<D> &t) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t e = i * 256 + tid;
+                half4_t h[4];
+                for (int j = 0; j < 4; ++j) h[j] = codes_to_half(kw[i][j]);
+                _Float16 *to_k = &t.k[e / (D / 16)][16 * (e % (D / 16))];
+                *reinterpret_cast<half8_t *>(to_k) = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                *reinterpret_cast<half8_t *>(to_k + 8) = __builtin_shufflevector(h[2], h[3], 0, 1, 2, 3, 4, 5, 6, 7);
+                for (int j = 0; j < 4; ++j) h[j] = codes_to_half(vw[i][j]);
+                _Float16 *to_v = &t.v[e / 4][16 * (e & 3)];
+                *reinterpret_cast<half8_t *>(to_v) = __builtin_shufflevector(h[0], h[2], 0, 1, 2, 3, 4, 5, 6, 7);
+                *reinterpret_cast<half8_t *>(to_v + 8) = __builtin_shufflevector(h[1], h[3], 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+            if (tid < 4) {
+                const float v = v_scale == 0.0f ? 0x1p-60f : v_scale;
+                t.k_scale[tid] = k_scale;
+                t.log_v[tid] = log2_of(v);
+                t.back_v[tid] = 1.0f / v;
+            }
+        };
+
+        if (reach.begin < reach.end) {
+            ask_ids(reach.begin);
+            ask(reach.begin);
+            ask_ids(reach.begin + 64);
+            put(buffer[0]);
+        }
+        __syncthreads();
+        uint32_t at = 0;
+        for (uint32_t t0 = reach.begin; t0 < reach.end; t0 += 64, at ^= 1) {
+            const ManyTile<D> &t = buffer[at];
+            const bool more = t0 + 64 < reach.end;
+            if (more) {
+                ask(t0 + 64);
+                ask_ids(t0 + 128);
+            }
+            // (a wave whose rows all end before the tile, or begin behind it, only helps to stage)
+            if (__ballot(from < t0 + 64 && to > t0)) {
+                float16_t s[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    for (int i = 0; i < 16; ++i) s[c][i] = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < D / 16; ++e)
+                        s[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(&t.k[32 * c + n][16 * e + 8 * hi]), q[e], s[c], 0, 0, 0);
+                }
+                const bool whole = __ballot(t0 < from || t0 + 64 > to) == 0;
+                const float4_t ks = *reinterpret_cast<const float4_t *>(t.k_scale), lv = *reinterpret_cast<const float4_t *>(t.log_v);
+                const float4_t bv = *reinterpret_cast<const float4_t *>(t.back_v);
+                if (!whole) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        for (int i = 0; i < 16; ++i) {
+                            const uint32_t token = t0 + 32 * c + 8 * (i / 4) + 4 * hi + i % 4;
+                            if (token < from || token >= to) s[c][i] = -INFINITY;
+                        }
+                }
+                float factor[4], top = -INFINITY;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    float m = s[b / 2][8 * (b & 1)];
+                    for (int i = 1; i < 8; ++i) m = fmaxf(m, s[b / 2][8 * (b & 1) + i]);
+                    factor[b] = ks[b] * row_factor;
+                    // (-inf times a scale of 0 is a NaN, which the maximum passes over)
+                    top = fmaxf(top, __builtin_fmaf(m, factor[b], lv[b]));
+                }
+                top = fmaxf(top, __shfl_xor(top, 32));
+                if (__ballot(top > ref + (kRoom + kSlack))) {
+                    const float now = fmaxf(ref, top - kRoom), down = pow2(ref - now);
+                    ref = now;
+                    weight *= down;
+#pragma unroll
+                    for (int d = 0; d < D / 32; ++d) acc[d] *= down;
+                }
+                half8_t pw[4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const float off = lv[b] - ref;
+                    float e[8], sum = 0.0f;
+                    for (int i = 0; i < 8; ++i) {
+                        const float x = s[b / 2][8 * (b & 1) + i];
+                        e[i] = pow2(__builtin_fmaf(x, factor[b], off));
+                        if (!whole && x == -INFINITY) e[i] = 0.0f;
+                        sum += e[i];
+                    }
+                    if (whole) weight = __builtin_fmaf(sum, bv[b], weight);
+                    else weight += sum == 0.0f ? 0.0f : sum * bv[b];
+                    for (int i = 0; i < 8; ++i) pw[b][i] = (_Float16)e[i];
+                }
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(&t.v[32 * d + n][16 * u + 8 * hi]), pw[u], acc[d], 0, 0, 0);
+            }
+            if (more) put(buffer[at ^ 1]);
+            __syncthreads();
+        }
+        weight += __shfl_xor(weight, 32);
+
+        if (row < rows) {
+            const uint64_t id = row_id(a, p, row);
+            if (a.splits == 1) {
+                const float f = weight == 0.0f ? 0.0f : 1.0f / weight;
+                uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)(p.begin + row / a.group) * a.out_stride +
+                                (uint64_t)(p.h * a.group + row % a.group) * D + 4 * hi;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+                    for (int b = 0; b < 4; ++b)
+                        *reinterpret_cast<uint2_t *>(dst + 32 * d + 8 * b) =
+                            uint2_t{narrow2<BF16>(acc[d][4 * b] * f, acc[d][4 * b + 1] * f), narrow2<BF16>(acc[d][4 * b + 2] * f, acc[d][4 * b + 3] * f)};
+                if (a.lse && hi == 0) a.lse[id] = weight == 0.0f ? -INFINITY : (ref + log2_of(weight)) * 0.69314718055994530942f;
+            } else {
+                float *dst = a.parts + (id * a.splits + p.split) * D + 4 * hi;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+                    for (int b = 0; b < 4; ++b)
+                        *reinterpret_cast<float4_t *>(dst + 32 * d + 8 * b) = float4_t{acc[d][4 * b], acc[d][4 * b + 1], acc[d][4 * b + 2], acc[d][4 * b + 3]};
+                if (hi == 0) {
+                    float *st = a.parts + a.part_rows * a.splits * D + (id * a.splits + p.split) * 2;
+                    st[0] = ref;
+                    st[1] = weight;
+                }
+            }
+        }
+        if (!p.last || (uint64_t)(tile + 1) * 128 >= rows) return;
+    }
+}
+
 // The pieces of a row along the cache, joined in their order: a workgroup for four rows.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
@@ -366,15 +580,15 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
 AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length, uint32_t window) {
     AttendLaunch l;
     const uint64_t group = s.q_heads / s.kv_heads;
-    l.rows = 16;
-    const uint64_t each = (max_new * group + l.rows - 1) / l.rows, packed = tokens * group / l.rows + requests;
+    l.rows = (uint64_t)max_new * group > 32 ? 128 : 16;
+    const uint64_t each = ((uint64_t)max_new * group + l.rows - 1) / l.rows, packed = tokens * group / l.rows + requests;
     // the same number for every request saves the search for a tile's request; where requests differ much it would
     // launch more workgroups than there are tiles
     l.tiles_each = each == 0 ? 1u : (uint32_t)(each * requests <= packed ? each : 0);
     l.tiles = (uint32_t)(l.tiles_each ? (uint64_t)l.tiles_each * requests : packed);
     uint64_t reach = max_length;
     if (window && reach > (uint64_t)window + max_new) reach = (uint64_t)window + max_new;
-    const uint64_t units = (uint64_t)l.tiles * s.kv_heads, want = 1024;
+    const uint64_t units = (uint64_t)l.tiles * s.kv_heads, want = l.rows == 16 ? 1024 : 512;
     uint64_t splits = units >= want ? 1 : want / units, most = (reach + 255) / 256;
     if (splits > most) splits = most;
     if (splits == 0) splits = 1;
@@ -393,7 +607,9 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
 
 int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &a, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    TSQ_BY_SHAPE(k_attend_few, l.tiles * l.splits * s.kv_heads, a);
+    const uint32_t grid = l.tiles * l.splits * s.kv_heads;
+    if (l.rows == 16) TSQ_BY_SHAPE(k_attend_few, grid, a);
+    else TSQ_BY_SHAPE(k_attend_many, grid, a);
     if (hipError_t e = hipGetLastError()) return (int)e;
     if (l.splits > 1) {
         TSQ_BY_SHAPE(k_attend_join, (uint32_t)((a.part_rows + 3) / 4), a);
