@@ -541,12 +541,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
     }
 }
 
-// The pieces of a row along the cache, joined in their order: a workgroup for four rows.
-template <int D, bool BF16>
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
-    constexpr int E = D / 64;
-    const uint32_t lane = threadIdx.x & 63;
-    const uint64_t id = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+// The pieces of a row along the cache, joined: WAVES waves for a row, D / 4 lanes of them for a piece, so that
+// PIECES = 256 WAVES / D pieces are read at once.  Which lanes add which pieces, and in which order the lanes'
+// sums are added, is fixed.
+template <int D, bool BF16, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(AttendArgs a) {
+    constexpr uint32_t LANES = D / 4, PIECES = 64 * WAVES / LANES, ROWS = WAVES == 1 ? 4 : 1;
+    __shared__ float4_t sums[WAVES > 1 ? WAVES : 1][LANES];
+    __shared__ float totals[WAVES > 1 ? WAVES : 1], tops[WAVES > 1 ? WAVES : 1];
+    const uint32_t tid = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint64_t id = (uint64_t)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
     if (id >= a.part_rows) return;
     const uint32_t token = (uint32_t)(id / a.q_heads), head = (uint32_t)(id % a.q_heads);
     // rows that no request has were not computed and are not written
@@ -556,23 +560,44 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
         if (a.starts[mid] <= (int32_t)token) lo = mid; else hi = mid;
     }
     if ((int32_t)token < a.starts[lo] || (int32_t)token >= a.starts[lo + 1]) return;
-    const float *sums = a.parts + id * a.splits * D + lane * E, *stats = a.parts + a.part_rows * a.splits * D + id * a.splits * 2;
+    const uint32_t part = tid / LANES, piece = tid % LANES;
+    const float *parts = a.parts + id * a.splits * D + 4 * piece, *stats = a.parts + a.part_rows * a.splits * D + id * a.splits * 2;
     float top = kNone;
-    for (uint32_t i = lane; i < a.splits; i += 64) top = fmaxf(top, stats[2 * i]);
+    for (uint32_t i = tid; i < a.splits; i += 64 * WAVES) top = fmaxf(top, stats[2 * i]);
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    float total = 0.0f, y[E];
-    for (int e = 0; e < E; ++e) y[e] = 0.0f;
-    for (uint32_t i = 0; i < a.splits; ++i) {
-        const float w = stats[2 * i + 1];
-        if (w == 0.0f) continue;                         // a piece that the row sees nothing of
-        const float f = pow2(stats[2 * i] - top);
-        total += w * f;
-        for (int e = 0; e < E; ++e) y[e] += sums[(uint64_t)i * D + e] * f;
+    if constexpr (WAVES > 1) {
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, tops[w]);
     }
+    float total = 0.0f;
+    float4_t y = {0, 0, 0, 0};
+#pragma unroll 4
+    for (uint32_t i = part; i < a.splits; i += PIECES) {
+        const float w = stats[2 * i + 1], f = pow2(stats[2 * i] - top);
+        const float4_t v = *reinterpret_cast<const float4_t *>(parts + (uint64_t)i * D);
+        // (of a piece that the row sees nothing of, the sums are 0)
+        total = __builtin_fmaf(w, f, total);
+        for (int e = 0; e < 4; ++e) y[e] = __builtin_fmaf(v[e], f, y[e]);
+    }
+    for (uint32_t d = LANES; d < 64; d <<= 1) {
+        total += __shfl_xor(total, (int)d);
+        for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], (int)d);
+    }
+    if constexpr (WAVES > 1) {
+        if (lane < LANES) sums[wave][lane] = y;
+        if (lane == 0) totals[wave] = total;
+        __syncthreads();
+        if (tid >= LANES) return;
+        y = sums[0][tid];
+        total = totals[0];
+        for (int w = 1; w < WAVES; ++w) { y += sums[w][tid]; total += totals[w]; }
+    }
+    if (tid >= LANES) return;
     const float f = total == 0.0f ? 0.0f : 1.0f / total;
-    uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)token * a.out_stride + (uint64_t)head * D + lane * E;
-    for (int e = 0; e < E; ++e) dst[e] = (uint16_t)narrow<BF16>(y[e] * f);
-    if (a.lse && lane == 0) a.lse[id] = total == 0.0f ? -INFINITY : (top + log2_of(total)) * 0.69314718055994530942f;
+    uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)token * a.out_stride + (uint64_t)head * D + 4 * piece;
+    *reinterpret_cast<uint2_t *>(dst) = uint2_t{narrow2<BF16>(y[0] * f, y[1] * f), narrow2<BF16>(y[2] * f, y[3] * f)};
+    if (a.lse && tid == 0) a.lse[id] = total == 0.0f ? -INFINITY : (top + log2_of(total)) * 0.69314718055994530942f;
 }
 
 }  // namespace
@@ -598,24 +623,21 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
     return l;
 }
 
-#define TSQ_BY_SHAPE(kernel, grid, ...)                                                                                     \
-    do {                                                                                                                    \
-        if (s.head_dim == 64) { if (s.bf16) kernel<64, true><<<grid, 256, 0, st>>>(__VA_ARGS__); else kernel<64, false><<<grid, 256, 0, st>>>(__VA_ARGS__); }          \
-        else if (s.head_dim == 128) { if (s.bf16) kernel<128, true><<<grid, 256, 0, st>>>(__VA_ARGS__); else kernel<128, false><<<grid, 256, 0, st>>>(__VA_ARGS__); }  \
-        else { if (s.bf16) kernel<256, true><<<grid, 256, 0, st>>>(__VA_ARGS__); else kernel<256, false><<<grid, 256, 0, st>>>(__VA_ARGS__); }                         \
-    } while (0)
-
 int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &a, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const uint32_t grid = l.tiles * l.splits * s.kv_heads;
-    if (l.rows == 16) TSQ_BY_SHAPE(k_attend_few, grid, a);
-    else TSQ_BY_SHAPE(k_attend_many, grid, a);
+    by_shape(s, [&](auto d, auto bf16) {
+        if (l.rows == 16) k_attend_few<d(), bf16()><<<grid, 256, 0, st>>>(a);
+        else k_attend_many<d(), bf16()><<<grid, 256, 0, st>>>(a);
+    });
     if (hipError_t e = hipGetLastError()) return (int)e;
-    if (l.splits > 1) {
-        TSQ_BY_SHAPE(k_attend_join, (uint32_t)((a.part_rows + 3) / 4), a);
-        return (int)hipGetLastError();
-    }
-    return 0;
+    if (l.splits == 1) return 0;
+    // a wave reads a few pieces of a row one after the other; more of them want more waves
+    by_shape(s, [&](auto d, auto bf16) {
+        if (l.splits <= 16) k_attend_join<d(), bf16(), 1><<<(uint32_t)((a.part_rows + 3) / 4), 256, 0, st>>>(a);
+        else k_attend_join<d(), bf16(), 8><<<(uint32_t)a.part_rows, 512, 0, st>>>(a);
+    });
+    return (int)hipGetLastError();
 }
 
 }  // namespace tsq

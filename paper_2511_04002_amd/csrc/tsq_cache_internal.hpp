@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace tsq {
 
 constexpr uint32_t kMaxScheduleRequests = 4096;   // three words of LDS each in k_schedule: 48 KB
@@ -80,6 +82,14 @@ struct AttendLaunch { uint32_t rows, tiles, tiles_each, splits, chunk; };
 AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length,
                            uint32_t window);
 int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &a, void *stream);
+
+// f(head_dim, bfloat16 or not), both as types whose value is known when compiling.
+template <class F> void by_shape(const CacheShape &s, F f) {
+    auto kind = [&](auto d) { if (s.bf16) f(d, std::true_type{}); else f(d, std::false_type{}); };
+    if (s.head_dim == 64) kind(std::integral_constant<int, 64>{});
+    else if (s.head_dim == 128) kind(std::integral_constant<int, 128>{});
+    else kind(std::integral_constant<int, 256>{});
+}
 
 #ifdef __HIPCC__
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));

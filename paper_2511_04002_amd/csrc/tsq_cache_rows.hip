@@ -448,14 +448,6 @@ int workgroups(uint64_t waves, uint32_t *out) {
 
 }  // namespace
 
-#define TSQ_BY_SHAPE(kernel, grid, ...)                                                                                     \
-    do {                                                                                                                    \
-        const hipStream_t st = static_cast<hipStream_t>(stream);                                                            \
-        if (s.head_dim == 64) { if (s.bf16) kernel<64, true><<<grid, 256, 0, st>>>(__VA_ARGS__); else kernel<64, false><<<grid, 256, 0, st>>>(__VA_ARGS__); }          \
-        else if (s.head_dim == 128) { if (s.bf16) kernel<128, true><<<grid, 256, 0, st>>>(__VA_ARGS__); else kernel<128, false><<<grid, 256, 0, st>>>(__VA_ARGS__); }  \
-        else { if (s.bf16) kernel<256, true><<<grid, 256, 0, st>>>(__VA_ARGS__); else kernel<256, false><<<grid, 256, 0, st>>>(__VA_ARGS__); }                         \
-    } while (0)
-
 int launch_schedule(const ScheduleArgs &a, void *stream) {
     const uint32_t groups = a.capacity <= 4 * kScheduleThreads ? 1 : (a.capacity + 4 * kScheduleThreads - 1) / (4 * kScheduleThreads);
     k_schedule<<<groups < 256 ? groups : 256, kScheduleThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
@@ -467,21 +459,21 @@ int launch_norm_rotate(const CacheShape &s, const NormRotateArgs &a, void *strea
     uint32_t grid;
     const uint32_t each = passes;
     if (int e = workgroups((uint64_t)a.tokens * each, &grid)) return e;
-    TSQ_BY_SHAPE(k_norm_rotate, grid, a, passes, each);
+    by_shape(s, [&](auto d, auto bf16) { k_norm_rotate<d(), bf16()><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, passes, each); });
     return (int)hipGetLastError();
 }
 
 int launch_append(const CacheShape &s, const AppendArgs &a, void *stream) {
     uint32_t grid;
     if (int e = workgroups((((uint64_t)a.tokens + a.segment - 1) / a.segment) * a.kv_heads * 2, &grid)) return e;
-    TSQ_BY_SHAPE(k_append, grid, a);
+    by_shape(s, [&](auto d, auto bf16) { k_append<d(), bf16()><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a); });
     return (int)hipGetLastError();
 }
 
 int launch_gather(const CacheShape &s, const GatherArgs &a, void *stream) {
     uint32_t grid;
     if (int e = workgroups((((uint64_t)a.tokens + 15) / 16) * a.kv_heads * 2, &grid)) return e;
-    TSQ_BY_SHAPE(k_gather, grid, a);
+    by_shape(s, [&](auto d, auto bf16) { k_gather<d(), bf16()><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a); });
     return (int)hipGetLastError();
 }
 
