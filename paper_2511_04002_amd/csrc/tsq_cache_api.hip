@@ -133,7 +133,7 @@ tsq_status tsq_cache_append(const tsq_cache *c, const tsq_cache_memory *m, uint3
     a.slots = static_cast<const int32_t *>(d_slots);
     a.tokens = tokens; a.kv_heads = c->s.kv_heads; a.blocks = c->s.blocks;
     a.block_tokens = c->s.block_tokens; a.block_log2 = c->s.block_log2;
-    a.segment = 1;
+    a.window = a.waves_each = 0;
     return hip_rc(launch_append(c->s, a, stream));
 }
 
@@ -156,6 +156,7 @@ tsq_status tsq_cache_gather(const tsq_cache *c, const tsq_cache_memory *m, uint3
     a.lengths = static_cast<const int32_t *>(d_lengths);
     a.requests = requests; a.tokens = tokens; a.kv_heads = c->s.kv_heads; a.blocks = c->s.blocks;
     a.block_tokens = c->s.block_tokens; a.block_log2 = c->s.block_log2; a.max_blocks = c->s.max_blocks;
+    a.waves_each = 0;
     return hip_rc(launch_gather(c->s, a, stream));
 }
 

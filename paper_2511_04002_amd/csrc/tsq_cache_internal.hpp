@@ -43,7 +43,7 @@ struct AppendArgs {
     float *scale[2];
     const int32_t *slots;
     uint32_t tokens, kv_heads, blocks, block_tokens, block_log2;
-    uint32_t segment;            // rows that a wave looks for runs in
+    uint32_t window, waves_each; // rows that are looked through for runs together, and the waves that share them
 };
 
 struct GatherArgs {
@@ -53,6 +53,7 @@ struct GatherArgs {
     const float *scale[2];
     const int32_t *table, *starts, *lengths;
     uint32_t requests, tokens, kv_heads, blocks, block_tokens, block_log2, max_blocks;
+    uint32_t waves_each;         // waves that share the heads of 16 rows
 };
 
 struct AttendArgs {
