@@ -203,25 +203,37 @@ class Cache:
 
     # -------------------------------------------------------------- checks
 
-    def _ints(self, x, shape, what):
-        if not (x.is_cuda and x.is_contiguous() and x.dtype == self.int32 and x.shape == shape):
-            _refuse("%s is int32 %s on the GPU, contiguous" % (what, tuple(shape)))
+    # (a step calls these for every tensor of every operator: what a tensor holds is told by its type, place and number
+    # of elements, and its shape is looked at only where it is not contiguous)
+
+    def _ints(self, x, n, what):
+        if not (x.dtype is self.int32 and x.is_cuda and x.is_contiguous() and x.numel() == n):
+            _refuse("%s is int32 on the GPU, contiguous, %d elements" % (what, n))
         return x.data_ptr()
 
     def _rows(self, x, tokens, heads, what):
         """x: [tokens, heads, head_dim], or [tokens, heads * head_dim]; rows anywhere, the heads of a row together.
         -> pointer, elements from row to row."""
-        shape, stride = x.shape, x.stride()
-        d = self.head_dim
-        if not (x.is_cuda and x.dtype == self.kind and shape[0] == tokens and
-                ((len(shape) == 3 and shape[1] == heads and shape[2] == d and stride[2] == 1 and (heads == 1 or stride[1] == d)) or
-                 (len(shape) == 2 and shape[1] == heads * d and stride[1] == 1))):
-            _refuse("%s is [%d, %d, %d] of %s on the GPU, the heads of a row together" % (what, tokens, heads, d, self.kind))
-        return x.data_ptr(), (stride[0] if tokens > 1 else heads * d)
+        width = heads * self.head_dim
+        if x.dtype is self.kind and x.is_cuda and x.numel() == tokens * width:
+            if x.is_contiguous():
+                return x.data_ptr(), width
+            shape, stride = x.shape, x.stride()
+            if shape[0] == tokens and ((len(shape) == 3 and shape[1] == heads and stride[2] == 1 and (heads == 1 or stride[1] == self.head_dim)) or
+                                       (len(shape) == 2 and stride[1] == 1)):
+                return x.data_ptr(), (stride[0] if tokens > 1 else width)
+        _refuse("%s is [%d, %d, %d] of %s on the GPU, the heads of a row together" % (what, tokens, heads, self.head_dim, self.kind))
 
     def _into(self, x, tokens, heads, what):
         x = self._empty((tokens, heads, self.head_dim), self.kind) if x is None else x
         return (x,) + self._rows(x, tokens, heads, what)
+
+    def _weight(self, w):
+        if w is None:
+            return None
+        if not (w.dtype is self.kind and w.is_cuda and w.is_contiguous() and w.numel() == self.head_dim):
+            _refuse("a norm's weight is [head_dim] of the cache's dtype on the GPU, contiguous")
+        return w.data_ptr()
 
     # -------------------------------------------------------------- the operators
 
@@ -229,18 +241,15 @@ class Cache:
         """Block tables, slots and positions of a step: new [requests] int32 new tokens of each request (-1: done),
         lengths [requests] int32 what it has.  table and ring are updated; the rest is written to `out`
         (from new_schedule(requests, most new tokens of a step))."""
-        n = new.shape
-        if not (counters.is_cuda and counters.is_contiguous() and counters.dtype == self.int64 and counters.shape == (2,) and
-                out.counters.is_cuda and out.counters.is_contiguous() and out.counters.dtype == self.int64 and out.counters.shape == (2,)):
-            _refuse("counters is int64 (2,) on the GPU, contiguous")
-        if len(n) != 1:
-            _refuse("new is int32 [requests]")
-        i, capacity = self._ints, out.slots.shape
+        n, i, capacity = new.numel(), self._ints, out.slots.numel()
+        for x in (counters, out.counters):
+            if not (x.dtype is self.int64 and x.is_cuda and x.is_contiguous() and x.numel() == 2):
+                _refuse("counters is int64 (2,) on the GPU, contiguous")
         status = self._lib.tsq_cache_schedule(
-            self.handle, n[0], i(new, n, "new"), i(lengths, n, "lengths"), i(table, (n[0], self.max_blocks), "table"),
-            i(ring, (self.blocks,), "ring"), counters.data_ptr(), capacity[0], i(out.lengths, n, "out.lengths"),
-            out.counters.data_ptr(), i(out.starts, (n[0] + 1,), "out.starts"), i(out.positions, capacity, "out.positions"),
-            i(out.slots, capacity, "out.slots"), i(out.status, (1,), "out.status"), self._stream())
+            self.handle, n, i(new, n, "new"), i(lengths, n, "lengths"), i(table, n * self.max_blocks, "table"),
+            i(ring, self.blocks, "ring"), counters.data_ptr(), capacity, i(out.lengths, n, "out.lengths"),
+            out.counters.data_ptr(), i(out.starts, n + 1, "out.starts"), i(out.positions, capacity, "out.positions"),
+            i(out.slots, capacity, "out.slots"), i(out.status, 1, "out.status"), self._stream())
         if status:
             raise TsqError(status, "tsq_cache_schedule")
         return out
@@ -255,18 +264,14 @@ class Cache:
         kp, ks = self._rows(k, tokens, self.kv_heads, "k")
         q_out, qo, qos = self._into(q_out, tokens, self.q_heads, "q_out")
         k_out, ko, kos = self._into(k_out, tokens, self.kv_heads, "k_out")
-        if not (angles.is_cuda and angles.is_contiguous() and angles.dtype == self.float32 and angles.dim() == 2):
+        if not (angles.dtype is self.float32 and angles.is_cuda and angles.is_contiguous() and angles.dim() == 2):
             _refuse("angles is float32 [rows, rotary] on the GPU, contiguous")
-        if pairs not in ("halves", "neighbours"):
+        if pairs != "halves" and pairs != "neighbours":
             _refuse("pairs is 'halves' or 'neighbours'")
-        weights = []
-        for w in (q_weight, k_weight):
-            if w is not None and not (w.is_cuda and w.is_contiguous() and w.dtype == self.kind and w.shape == (self.head_dim,)):
-                _refuse("a norm's weight is [head_dim] of the cache's dtype on the GPU, contiguous")
-            weights.append(None if w is None else w.data_ptr())
+        known, rotary = angles.shape
         status = self._lib.tsq_cache_norm_rotate(
-            self.handle, tokens, qp, qs, kp, ks, self._ints(positions, (tokens,), "positions"), angles.data_ptr(), angles.shape[0],
-            angles.shape[1], TSQ_PAIRS_HALVES if pairs == "halves" else TSQ_PAIRS_NEIGHBOURS, weights[0], weights[1], eps,
+            self.handle, tokens, qp, qs, kp, ks, self._ints(positions, tokens, "positions"), angles.data_ptr(), known, rotary,
+            TSQ_PAIRS_HALVES if pairs == "halves" else TSQ_PAIRS_NEIGHBOURS, self._weight(q_weight), self._weight(k_weight), eps,
             qo, qos, ko, kos, self._stream())
         if status:
             raise TsqError(status, "tsq_cache_norm_rotate")
@@ -277,7 +282,7 @@ class Cache:
         tokens = k.shape[0]
         kp, ks = self._rows(k, tokens, self.kv_heads, "k")
         vp, vs = self._rows(v, tokens, self.kv_heads, "v")
-        status = self._lib.tsq_cache_append(self.handle, memory.ref, tokens, kp, ks, vp, vs, self._ints(slots, (tokens,), "slots"),
+        status = self._lib.tsq_cache_append(self.handle, memory.ref, tokens, kp, ks, vp, vs, self._ints(slots, tokens, "slots"),
                                             self._stream())
         if status:
             raise TsqError(status, "tsq_cache_append")
@@ -285,12 +290,12 @@ class Cache:
     def gather(self, memory: Memory, table, starts, lengths, k_out, v_out):
         """The last starts[r + 1] - starts[r] tokens of each request r, up to lengths[r], into rows starts[r] ... of k_out
         and v_out [tokens, kv_heads, head_dim] (or [tokens, kv_heads * head_dim], as Plan.compress_batch takes them)."""
-        tokens, n = k_out.shape[0], lengths.shape
+        tokens, n = k_out.shape[0], lengths.numel()
         kp, ks = self._rows(k_out, tokens, self.kv_heads, "k_out")
         vp, vs = self._rows(v_out, tokens, self.kv_heads, "v_out")
         i = self._ints
         status = self._lib.tsq_cache_gather(
-            self.handle, memory.ref, n[0], i(table, (n[0], self.max_blocks), "table"), i(starts, (n[0] + 1,), "starts"),
+            self.handle, memory.ref, n, i(table, n * self.max_blocks, "table"), i(starts, n + 1, "starts"),
             i(lengths, n, "lengths"), tokens, kp, ks, vp, vs, self._stream())
         if status:
             raise TsqError(status, "tsq_cache_gather")
@@ -306,22 +311,22 @@ class Cache:
         """Attention of q [tokens, q_heads, head_dim] over the cache: rows starts[r] .. starts[r + 1] - 1 are the last tokens of
         request r, which has lengths[r] in the cache.  max_new, max_length: the largest of both over the requests (how the
         work is split goes by them).  scale: 1 / sqrt(head_dim) if left out.  lse: float32 [tokens, q_heads] to be written."""
-        tokens, n = q.shape[0], lengths.shape
+        tokens, n = q.shape[0], lengths.numel()
         qp, qs = self._rows(q, tokens, self.q_heads, "q")
         out, op, os_ = self._into(out, tokens, self.q_heads, "out")
         lp = None
         if lse is not None:
-            if not (lse.is_cuda and lse.is_contiguous() and lse.dtype == self.float32 and lse.shape == (tokens, self.q_heads)):
+            if not (lse.dtype is self.float32 and lse.is_cuda and lse.is_contiguous() and lse.numel() == tokens * self.q_heads):
                 _refuse("lse is float32 [tokens, q_heads] on the GPU, contiguous")
             lp = lse.data_ptr()
         i, L = self._ints, self._lib
-        need = L.tsq_cache_attend_workspace_bytes(self.handle, n[0], tokens, max_new, max_length, window)
+        need = L.tsq_cache_attend_workspace_bytes(self.handle, n, tokens, max_new, max_length, window)
         if need and ws is None:
             ws = self._empty(need, self._torch.uint8)
         if need and not (ws.is_cuda and ws.is_contiguous() and ws.numel() * ws.element_size() >= need):
             _refuse("ws has %d bytes on the GPU, contiguous" % need)
         status = L.tsq_cache_attend(
-            self.handle, memory.ref, n[0], i(table, (n[0], self.max_blocks), "table"), i(starts, (n[0] + 1,), "starts"),
+            self.handle, memory.ref, n, i(table, n * self.max_blocks, "table"), i(starts, n + 1, "starts"),
             i(lengths, n, "lengths"), tokens, max_new, max_length, qp, qs, self.head_dim ** -0.5 if scale is None else scale,
             causal, window, op, os_, lp, ws.data_ptr() if need else None, self._stream())
         if status:

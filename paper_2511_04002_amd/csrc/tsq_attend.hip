@@ -107,30 +107,30 @@ __device__ __forceinline__ void row_sees(const AttendArgs &a, const Place &p, ui
     to = hi > lo ? (uint32_t)hi : 0u;
 }
 
-// What the 16 tokens of a block that a lane works on have in common: the block (0 where there is none, whose codes
-// are then not used), the factor of its scores, and its values' scale as log2 and as reciprocal.  Values that are
-// all 0 weigh nothing whatever their scale: 2^-60 keeps their tokens in the denominator without touching the
-// reference of the others.
-struct Block { uint32_t id; float c, log_v, back_v; };
-__device__ __forceinline__ uint32_t block_id(const AttendArgs &a, const Place &p, uint32_t token, bool &bad) {
-    const uint32_t nth = token >> a.block_log2;
-    bad = p.beyond;
-    if (token >= p.seen) return 0;
-    const uint32_t id = (uint32_t)a.table[(uint64_t)p.r * a.max_blocks + nth];
-    if (id >= a.blocks) { bad = true; return 0; }
-    return id;
+// The block of the 16 tokens from `token` on: 0 where there is none, whose codes are then not used; with kBadBlock
+// set if the table should have one and does not, whose tokens are to come out as NaN.
+constexpr uint32_t kBadBlock = 1u << 31, kIdBits = kBadBlock - 1;    // (a block's number has 27 bits)
+__device__ __forceinline__ uint32_t block_id(const AttendArgs &a, const Place &p, uint32_t token) {
+    uint32_t id = 0;
+    if (token < p.seen) {
+        id = (uint32_t)a.table[(uint64_t)p.r * a.max_blocks + (token >> a.block_log2)];
+        if (id >= a.blocks) id = kBadBlock;
+    }
+    return p.beyond ? id | kBadBlock : id;
 }
-__device__ __forceinline__ Block block_at(const AttendArgs &a, const Place &p, uint32_t token, float row_factor) {
-    Block b;
-    bool bad;
-    b.id = block_id(a, p, token, bad);
-    const uint64_t at = (uint64_t)b.id * a.kv_heads + p.h;
-    const float ks = bad ? __builtin_nanf("") : a.k_scale[at], vs = a.v_scale[at];
-    b.c = ks * row_factor;
-    const float v = vs == 0.0f ? 0x1p-60f : vs;
-    b.log_v = log2_of(v);
-    b.back_v = 1.0f / v;
-    return b;
+
+// What the tokens of a block have in common for a head: the factor of the scores, and the values' scale as log2 and
+// as reciprocal.  Values that are all 0 weigh nothing whatever their scale is: 2^-60 keeps their tokens in the
+// denominator without touching the reference of the others.
+struct Scale { float k, v; };
+__device__ __forceinline__ Scale scale_at(const AttendArgs &a, const Place &p, uint32_t id) {
+    const uint64_t at = (uint64_t)(id & kIdBits) * a.kv_heads + p.h;
+    return Scale{id & kBadBlock ? __builtin_nanf("") : a.k_scale[at], a.v_scale[at]};
+}
+struct Block { float c, log_v, back_v; };
+__device__ __forceinline__ Block block_of(Scale s, float row_factor) {
+    const float v = s.v == 0.0f ? 0x1p-60f : s.v;
+    return Block{s.k * row_factor, log2_of(v), 1.0f / v};
 }
 
 // A query's 16-bit elements as halves, and what the scores are to be multiplied by for it: binary16 as it is,
@@ -217,19 +217,32 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
         float4_t acc[D / 16];
         for (int d = 0; d < D / 16; ++d) acc[d] = float4_t{0, 0, 0, 0};
         float ref = kNone, weight = 0.0f;
-        for (uint32_t t0 = reach.begin + 64 * wave; t0 < reach.end; t0 += 256) {
-            const Block b = block_at(a, p, t0 + 16 * g, row_factor);
-            const uint32_t key_token = t0 + 16 * (m >> 2);
-            bool bad_key;
-            const uint32_t key_id = block_id(a, p, key_token, bad_key);
-            const int8_t *keys = a.k + (((uint64_t)key_id * a.kv_heads + p.h) * B + (key_token & (B - 1)) + (m & 3)) * D + 16 * g;
-            const int8_t *values = a.v + (((uint64_t)b.id * a.kv_heads + p.h) * D + m) * B + ((t0 + 16 * g) & (B - 1));
-            uint4_t kw[4][F], vw[D / 16];
+
+        // Loads are always on their way: a tile's keys are asked for while the tile before it is worked on, its values
+        // when that one's are used up, and its block numbers a tile earlier still.
+        uint4_t kw[4][F], vw[D / 16];
+        Scale scale = {};
+        auto ask_keys = [&](uint32_t t0, uint32_t id) {
+            const uint32_t key_id = (uint32_t)__shfl((int)id, (int)(m >> 2) << 4) & kIdBits, token = t0 + 16 * (m >> 2);
+            const int8_t *keys = a.k + (((uint64_t)key_id * a.kv_heads + p.h) * B + (token & (B - 1)) + (m & 3)) * D + 16 * g;
+            scale = scale_at(a, p, id);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 for (int f = 0; f < F; ++f) kw[t][f] = *reinterpret_cast<const uint4_t *>(keys + 4 * t * D + 64 * f);
+        };
+        auto ask_values = [&](uint32_t t0, uint32_t id) {
+            const int8_t *values = a.v + (((uint64_t)(id & kIdBits) * a.kv_heads + p.h) * D + m) * B + ((t0 + 16 * g) & (B - 1));
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) vw[d] = *reinterpret_cast<const uint4_t *>(values + (uint64_t)(16 * d) * B);
+        };
+        uint32_t t0 = reach.begin + 64 * wave, next_id = 0;
+        if (t0 < reach.end) {
+            const uint32_t id = block_id(a, p, t0 + 16 * g);
+            next_id = block_id(a, p, t0 + 256 + 16 * g);
+            ask_keys(t0, id);
+            ask_values(t0, id);
+        }
+        for (; t0 < reach.end; t0 += 256) {
             float4_t s[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -239,6 +252,13 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
                         const half4_t x = codes_to_half(kw[t][f][2 * e]), y = codes_to_half(kw[t][f][2 * e + 1]);
                         s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), q[f][e], s[t], 0, 0, 0);
                     }
+            }
+            const Block b = block_of(scale, row_factor);
+            const bool more = t0 + 256 < reach.end;
+            const uint32_t id = next_id;
+            if (more) {
+                next_id = block_id(a, p, t0 + 512 + 16 * g);
+                ask_keys(t0 + 256, id);
             }
             // exponents, and the reference
             const uint32_t mine = t0 + 16 * g;
@@ -277,6 +297,7 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
                     const half4_t x = codes_to_half(vw[d][2 * u]), y = codes_to_half(vw[d][2 * u + 1]);
                     acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), pw[u], acc[d], 0, 0, 0);
                 }
+            if (more) ask_values(t0 + 256, id);
         }
         weight += __shfl_xor(weight, 16);
         weight += __shfl_xor(weight, 32);
@@ -338,7 +359,7 @@ template <int D>
 struct ManyTile {                                        // rows padded by 16 bytes: neighbours begin four banks apart
     _Float16 k[64][D + 8];
     _Float16 v[D][64 + 8];
-    float k_scale[4], log_v[4], back_v[4];               // of each 16 tokens
+    float factor[4], log_v[4], back_v[4];                // of each 16 tokens
 };
 
 template <int D, bool BF16>
@@ -374,7 +395,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) q[s] = query_piece<BF16>(w[s], factor);
         }
-        const float row_factor = back * a.scale_log2;
         uint32_t from, to;
         row_sees(a, p, row, from, to);
         const Reach reach = reach_of<128>(a, p, tile);
@@ -388,13 +408,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
         // staging: what this thread brings of a tile
         uint32_t key_id[N], value_id = 0;
         uint4_t kw[N], vw[N];
-        float k_scale = 0.0f, v_scale = 0.0f;
+        Scale scale = {};
         auto ask_ids = [&](uint32_t t0) {
-            bool bad;
 #pragma unroll
-            for (int i = 0; i < N; ++i) key_id[i] = block_id(a, p, t0 + (i * 256 + tid) / (D / 16), bad);
-            value_id = block_id(a, p, t0 + 16 * (tid & 3), bad);
-            if (bad) value_id |= 1u << 31;               // (a block number has 27 bits)
+            for (int i = 0; i < N; ++i) key_id[i] = block_id(a, p, t0 + (i * 256 + tid) / (D / 16)) & kIdBits;
+            value_id = block_id(a, p, t0 + 16 * (tid & 3));
         };
         auto ask = [&](uint32_t t0) {
 #pragma unroll
@@ -402,14 +420,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
                 const uint32_t e = i * 256 + tid, token = t0 + e / (D / 16), piece = e % (D / 16);
                 kw[i] = *reinterpret_cast<const uint4_t *>(a.k + (((uint64_t)key_id[i] * a.kv_heads + p.h) * B + (token & (B - 1))) * D + 16 * piece);
             }
-            const uint64_t head = (uint64_t)(value_id & 0x7FFFFFFFu) * a.kv_heads + p.h;
+            const uint64_t head = (uint64_t)(value_id & kIdBits) * a.kv_heads + p.h;
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 vw[i] = *reinterpret_cast<const uint4_t *>(a.v + (head * D + (i * 256 + tid) / 4) * B + ((t0 + 16 * (tid & 3)) & (B - 1)));
-            if (tid < 4) {
-                k_scale = value_id >> 31 ? __builtin_nanf("") : a.k_scale[head];
-                v_scale = a.v_scale[head];
-            }
+            if (tid < 4) scale = scale_at(a, p, value_id);
         };
         auto put = [&](ManyTile<D> &t) {
 #pragma unroll
@@ -426,10 +441,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
                 *reinterpret_cast<half8_t *>(to_v + 8) = __builtin_shufflevector(h[1], h[3], 0, 1, 2, 3, 4, 5, 6, 7);
             }
             if (tid < 4) {
-                const float v = v_scale == 0.0f ? 0x1p-60f : v_scale;
-                t.k_scale[tid] = k_scale;
-                t.log_v[tid] = log2_of(v);
-                t.back_v[tid] = 1.0f / v;
+                const Block b = block_of(scale, a.scale_log2);
+                t.factor[tid] = b.c;
+                t.log_v[tid] = b.log_v;
+                t.back_v[tid] = b.back_v;
             }
         };
 
@@ -459,7 +474,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
                         s[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(&t.k[32 * c + n][16 * e + 8 * hi]), q[e], s[c], 0, 0, 0);
                 }
                 const bool whole = __ballot(t0 < from || t0 + 64 > to) == 0;
-                const float4_t ks = *reinterpret_cast<const float4_t *>(t.k_scale), lv = *reinterpret_cast<const float4_t *>(t.log_v);
+                const float4_t ks = *reinterpret_cast<const float4_t *>(t.factor), lv = *reinterpret_cast<const float4_t *>(t.log_v);
                 const float4_t bv = *reinterpret_cast<const float4_t *>(t.back_v);
                 if (!whole) {
 #pragma unroll
@@ -474,7 +489,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
                 for (int b = 0; b < 4; ++b) {
                     float m = s[b / 2][8 * (b & 1)];
                     for (int i = 1; i < 8; ++i) m = fmaxf(m, s[b / 2][8 * (b & 1) + i]);
-                    factor[b] = ks[b] * row_factor;
+                    factor[b] = BF16 ? ks[b] * back : ks[b];
                     // (-inf times a scale of 0 is a NaN, which the maximum passes over)
                     top = fmaxf(top, __builtin_fmaf(m, factor[b], lv[b]));
                 }

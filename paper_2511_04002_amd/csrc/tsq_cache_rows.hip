@@ -650,8 +650,11 @@ int launch_schedule(const ScheduleArgs &a, void *stream) {
     // a thread a request or token while they are few; four tokens a thread where there are many
     const uint32_t most = a.requests > a.capacity ? a.requests : a.capacity;
     const uint32_t threads = most >= kScheduleThreads ? kScheduleThreads : (most + 63) / 64 * 64;
-    const uint32_t groups = (uint32_t)(((uint64_t)a.capacity + 4 * kScheduleThreads - 1) / (4 * kScheduleThreads));
-    k_schedule<<<groups < 1 ? 1 : groups < 256 ? groups : 256, threads, 0, static_cast<hipStream_t>(stream)>>>(a);
+    // (requests have blocks to take and to give back, too: one workgroup for 64 of them, up to 16)
+    uint32_t groups = (uint32_t)(((uint64_t)a.capacity + 4 * kScheduleThreads - 1) / (4 * kScheduleThreads));
+    const uint32_t by_request = a.requests >= 1024 ? 16 : (a.requests + 63) / 64;
+    if (groups < by_request) groups = by_request;
+    k_schedule<<<groups < 256 ? groups : 256, threads, 0, static_cast<hipStream_t>(stream)>>>(a);
     return (int)hipGetLastError();
 }
 

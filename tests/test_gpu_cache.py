@@ -622,7 +622,7 @@ def test_tensors_that_do_not_fit_are_refused(call):
         f = c.attend
     elif call == "schedule":
         good = [i(2), i(2), i(2, 2), i(4), c.new_counters(), c.new_schedule(2, 5)]
-        wrong = [(0, i(2, 1)), (1, i(3)), (2, i(2, 3)), (3, i(5)), (4, i(2)), (5, c.new_schedule(3, 5))]
+        wrong = [(0, i(3)), (1, i(3)), (2, i(2, 3)), (3, i(5)), (4, i(2)), (5, c.new_schedule(3, 5))]
         f = c.schedule
     else:
         good = [m.k, m.v, m.k_scale, m.v_scale]
