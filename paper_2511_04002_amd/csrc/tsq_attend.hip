@@ -107,30 +107,28 @@ __device__ __forceinline__ void row_sees(const AttendArgs &a, const Place &p, ui
     to = hi > lo ? (uint32_t)hi : 0u;
 }
 
-// The block of the 16 tokens from `token` on: 0 where there is none, whose codes are then not used; with kBadBlock
-// set if the table should have one and does not, whose tokens are to come out as NaN.
-constexpr uint32_t kBadBlock = 1u << 31, kIdBits = kBadBlock - 1;    // (a block's number has 27 bits)
-__device__ __forceinline__ uint32_t block_id(const AttendArgs &a, const Place &p, uint32_t token) {
-    uint32_t id = 0;
-    if (token < p.seen) {
-        id = (uint32_t)a.table[(uint64_t)p.r * a.max_blocks + (token >> a.block_log2)];
-        if (id >= a.blocks) id = kBadBlock;
-    }
-    return p.beyond ? id | kBadBlock : id;
+// The table's entry for the 16 tokens from `token` on, as it is (past the end of a reach: its last one, so that what is
+// asked for ahead of need is always there, and costs no new lines).  It is looked at when it is used, by id_of, so that
+// nothing waits for it before.
+__device__ __forceinline__ uint32_t table_entry(const AttendArgs &a, const Place &p, uint32_t token, uint32_t end) {
+    return (uint32_t)a.table[(uint64_t)p.r * a.max_blocks + (min(token, end - 1) >> a.block_log2)];
 }
+// A block's number, 0 for what is none; is_bad says which tokens are to come out as NaN for that.
+__device__ __forceinline__ uint32_t id_of(const AttendArgs &a, uint32_t entry) { return entry < a.blocks ? entry : 0; }
+__device__ __forceinline__ bool is_bad(const AttendArgs &a, const Place &p, uint32_t entry) { return entry >= a.blocks || p.beyond; }
 
 // What the tokens of a block have in common for a head: the factor of the scores, and the values' scale as log2 and
 // as reciprocal.  Values that are all 0 weigh nothing whatever their scale is: 2^-60 keeps their tokens in the
 // denominator without touching the reference of the others.
-struct Scale { float k, v; };
-__device__ __forceinline__ Scale scale_at(const AttendArgs &a, const Place &p, uint32_t id) {
-    const uint64_t at = (uint64_t)(id & kIdBits) * a.kv_heads + p.h;
-    return Scale{id & kBadBlock ? __builtin_nanf("") : a.k_scale[at], a.v_scale[at]};
+struct Scale { float k, v; bool bad; };
+__device__ __forceinline__ Scale scale_at(const AttendArgs &a, const Place &p, uint32_t entry) {
+    const uint64_t at = (uint64_t)id_of(a, entry) * a.kv_heads + p.h;
+    return Scale{a.k_scale[at], a.v_scale[at], is_bad(a, p, entry)};
 }
 struct Block { float c, log_v, back_v; };
 __device__ __forceinline__ Block block_of(Scale s, float row_factor) {
     const float v = s.v == 0.0f ? 0x1p-60f : s.v;
-    return Block{s.k * row_factor, log2_of(v), 1.0f / v};
+    return Block{s.bad ? __builtin_nanf("") : s.k * row_factor, log2_of(v), 1.0f / v};
 }
 
 // A query's 16-bit elements as halves, and what the scores are to be multiplied by for it: binary16 as it is,
@@ -174,7 +172,7 @@ __device__ __forceinline__ uint64_t row_id(const AttendArgs &a, const Place &p, 
 //   16 tokens of its group, in the order of its 16 bytes of a value's row; its row of the softmax is m.
 //   Keys: operand row m is token 16 (m / 4) + 4t + m % 4; the lane's k indices are the elements 64f + 16g .. + 15.
 template <int D, bool BF16>
-__global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) void k_attend_few(AttendArgs a) {
     constexpr int F = D / 64;                            // 64-element pieces of a head
     __shared__ float sums[4][16][132];
     __shared__ float stats[4][16][2];
@@ -222,25 +220,25 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
         // when that one's are used up, and its block numbers a tile earlier still.
         uint4_t kw[4][F], vw[D / 16];
         Scale scale = {};
-        auto ask_keys = [&](uint32_t t0, uint32_t id) {
-            const uint32_t key_id = (uint32_t)__shfl((int)id, (int)(m >> 2) << 4) & kIdBits, token = t0 + 16 * (m >> 2);
+        auto ask_keys = [&](uint32_t t0, uint32_t entry) {
+            const uint32_t key_id = (uint32_t)__shfl((int)id_of(a, entry), (int)(m >> 2) << 4), token = t0 + 16 * (m >> 2);
             const int8_t *keys = a.k + (((uint64_t)key_id * a.kv_heads + p.h) * B + (token & (B - 1)) + (m & 3)) * D + 16 * g;
-            scale = scale_at(a, p, id);
+            scale = scale_at(a, p, entry);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 for (int f = 0; f < F; ++f) kw[t][f] = *reinterpret_cast<const uint4_t *>(keys + 4 * t * D + 64 * f);
         };
-        auto ask_values = [&](uint32_t t0, uint32_t id) {
-            const int8_t *values = a.v + (((uint64_t)(id & kIdBits) * a.kv_heads + p.h) * D + m) * B + ((t0 + 16 * g) & (B - 1));
+        auto ask_values = [&](uint32_t t0, uint32_t entry) {
+            const int8_t *values = a.v + (((uint64_t)id_of(a, entry) * a.kv_heads + p.h) * D + m) * B + ((t0 + 16 * g) & (B - 1));
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) vw[d] = *reinterpret_cast<const uint4_t *>(values + (uint64_t)(16 * d) * B);
         };
-        uint32_t t0 = reach.begin + 64 * wave, next_id = 0;
+        uint32_t t0 = reach.begin + 64 * wave, next = 0;
         if (t0 < reach.end) {
-            const uint32_t id = block_id(a, p, t0 + 16 * g);
-            next_id = block_id(a, p, t0 + 256 + 16 * g);
-            ask_keys(t0, id);
-            ask_values(t0, id);
+            const uint32_t entry = table_entry(a, p, t0 + 16 * g, reach.end);
+            next = table_entry(a, p, t0 + 256 + 16 * g, reach.end);
+            ask_keys(t0, entry);
+            ask_values(t0, entry);
         }
         for (; t0 < reach.end; t0 += 256) {
             float4_t s[4];
@@ -254,24 +252,27 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
                     }
             }
             const Block b = block_of(scale, row_factor);
-            const bool more = t0 + 256 < reach.end;
-            const uint32_t id = next_id;
-            if (more) {
-                next_id = block_id(a, p, t0 + 512 + 16 * g);
-                ask_keys(t0 + 256, id);
-            }
+            const uint32_t entry = next;
+            ask_keys(t0 + 256, entry);
+            next = table_entry(a, p, t0 + 512 + 16 * g, reach.end);
             // exponents, and the reference
             const uint32_t mine = t0 + 16 * g;
             const bool whole = __ballot(mine < from || mine + 16 > to) == 0;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                for (int i = 0; i < 4; ++i) s[t][i] = __builtin_fmaf(s[t][i], b.c, b.log_v);
+            if (!whole) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t token = mine + 4 * t + i;
+                        s[t][i] = token < from || token >= to ? -INFINITY : s[t][i];
+                    }
+            }
             float top = -INFINITY;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t token = mine + 4 * t + i;
-                    s[t][i] = __builtin_fmaf(s[t][i], b.c, b.log_v);
-                    if (!whole && (token < from || token >= to)) s[t][i] = -INFINITY;
-                    top = fmaxf(top, s[t][i]);
-                }
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             if (__ballot(top > ref + (kRoom + kSlack))) {
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
                     const half4_t x = codes_to_half(vw[d][2 * u]), y = codes_to_half(vw[d][2 * u + 1]);
                     acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), pw[u], acc[d], 0, 0, 0);
                 }
-            if (more) ask_values(t0 + 256, id);
+            ask_values(t0 + 256, entry);
         }
         weight += __shfl_xor(weight, 16);
         weight += __shfl_xor(weight, 32);
@@ -406,25 +407,25 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
         float ref = kNone, weight = 0.0f;
 
         // staging: what this thread brings of a tile
-        uint32_t key_id[N], value_id = 0;
+        uint32_t key_entry[N], value_entry = 0;
         uint4_t kw[N], vw[N];
         Scale scale = {};
-        auto ask_ids = [&](uint32_t t0) {
+        auto ask_entries = [&](uint32_t t0) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) key_id[i] = block_id(a, p, t0 + (i * 256 + tid) / (D / 16)) & kIdBits;
-            value_id = block_id(a, p, t0 + 16 * (tid & 3));
+            for (int i = 0; i < N; ++i) key_entry[i] = table_entry(a, p, t0 + (i * 256 + tid) / (D / 16), reach.end);
+            value_entry = table_entry(a, p, t0 + 16 * (tid & 3), reach.end);
         };
         auto ask = [&](uint32_t t0) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const uint32_t e = i * 256 + tid, token = t0 + e / (D / 16), piece = e % (D / 16);
-                kw[i] = *reinterpret_cast<const uint4_t *>(a.k + (((uint64_t)key_id[i] * a.kv_heads + p.h) * B + (token & (B - 1))) * D + 16 * piece);
+                kw[i] = *reinterpret_cast<const uint4_t *>(a.k + (((uint64_t)id_of(a, key_entry[i]) * a.kv_heads + p.h) * B + (token & (B - 1))) * D + 16 * piece);
             }
-            const uint64_t head = (uint64_t)(value_id & kIdBits) * a.kv_heads + p.h;
+            const uint64_t head = (uint64_t)id_of(a, value_entry) * a.kv_heads + p.h;
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 vw[i] = *reinterpret_cast<const uint4_t *>(a.v + (head * D + (i * 256 + tid) / 4) * B + ((t0 + 16 * (tid & 3)) & (B - 1)));
-            if (tid < 4) scale = scale_at(a, p, value_id);
+            if (tid < 4) scale = scale_at(a, p, value_entry);
         };
         auto put = [&](ManyTile<D> &t) {
 #pragma unroll
@@ -449,9 +450,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
         };
 
         if (reach.begin < reach.end) {
-            ask_ids(reach.begin);
+            ask_entries(reach.begin);
             ask(reach.begin);
-            ask_ids(reach.begin + 64);
+            ask_entries(reach.begin + 64);
             put(buffer[0]);
         }
         __syncthreads();
@@ -459,10 +460,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
         for (uint32_t t0 = reach.begin; t0 < reach.end; t0 += 64, at ^= 1) {
             const ManyTile<D> &t = buffer[at];
             const bool more = t0 + 64 < reach.end;
-            if (more) {
-                ask(t0 + 64);
-                ask_ids(t0 + 128);
-            }
+            ask(t0 + 64);
+            ask_entries(t0 + 128);
             // (a wave whose rows all end before the tile, or begin behind it, only helps to stage)
             if (__ballot(from < t0 + 64 && to > t0)) {
                 float16_t s[2];
