@@ -407,8 +407,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
         float ref = kNone, weight = 0.0f;
 
         // staging: what this thread brings of a tile
+        // (a thread's places in a block are the same for all tiles, but for the half of a block of 128 tokens)
         uint32_t key_entry[N], value_entry = 0;
         uint4_t kw[N], vw[N];
+        const uint32_t block_bytes = a.kv_heads * B * D;
+        const int8_t *keys[N], *values[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t e = i * 256 + tid;
+            keys[i] = a.k + (uint64_t)p.h * B * D + (e / (D / 16) & (B - 1)) * D + 16 * (e % (D / 16));
+            values[i] = a.v + (uint64_t)p.h * B * D + (uint64_t)(e / 4) * B + (16 * (tid & 3) & (B - 1));
+        }
         Scale scale = {};
         auto ask_entries = [&](uint32_t t0) {
 #pragma unroll
@@ -416,15 +425,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
             value_entry = table_entry(a, p, t0 + 16 * (tid & 3), reach.end);
         };
         auto ask = [&](uint32_t t0) {
+            const uint32_t half = t0 & (B - 1);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const uint32_t e = i * 256 + tid, token = t0 + e / (D / 16), piece = e % (D / 16);
-                kw[i] = *reinterpret_cast<const uint4_t *>(a.k + (((uint64_t)id_of(a, key_entry[i]) * a.kv_heads + p.h) * B + (token & (B - 1))) * D + 16 * piece);
-            }
-            const uint64_t head = (uint64_t)id_of(a, value_entry) * a.kv_heads + p.h;
+            for (int i = 0; i < N; ++i) kw[i] = *reinterpret_cast<const uint4_t *>(keys[i] + ((uint64_t)id_of(a, key_entry[i]) * block_bytes + half * D));
+            const uint64_t at = (uint64_t)id_of(a, value_entry) * block_bytes + half;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                vw[i] = *reinterpret_cast<const uint4_t *>(a.v + (head * D + (i * 256 + tid) / 4) * B + ((t0 + 16 * (tid & 3)) & (B - 1)));
+            for (int i = 0; i < N; ++i) vw[i] = *reinterpret_cast<const uint4_t *>(values[i] + at);
             if (tid < 4) scale = scale_at(a, p, value_entry);
         };
         auto put = [&](ManyTile<D> &t) {
@@ -504,16 +510,29 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     const float off = lv[b] - ref;
-                    float e[8], sum = 0.0f;
-                    for (int i = 0; i < 8; ++i) {
-                        const float x = s[b / 2][8 * (b & 1) + i];
-                        e[i] = pow2(__builtin_fmaf(x, factor[b], off));
-                        if (!whole && x == -INFINITY) e[i] = 0.0f;
-                        sum += e[i];
-                    }
-                    if (whole) weight = __builtin_fmaf(sum, bv[b], weight);
-                    else weight += sum == 0.0f ? 0.0f : sum * bv[b];
-                    for (int i = 0; i < 8; ++i) pw[b][i] = (_Float16)e[i];
+                    for (int i = 0; i < 8; ++i) s[b / 2][8 * (b & 1) + i] = pow2(__builtin_fmaf(s[b / 2][8 * (b & 1) + i], factor[b], off));
+                }
+                if (!whole) {                            // (a factor of 0 or NaN has made NaN of -inf)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        for (int i = 0; i < 16; ++i) {
+                            const uint32_t token = t0 + 32 * c + 8 * (i / 4) + 4 * hi + i % 4;
+                            if (token < from || token >= to) s[c][i] = 0.0f;
+                        }
+                }
+                float sum[4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const float16_t &e = s[b / 2];
+                    const int o = 8 * (b & 1);
+                    sum[b] = ((e[o] + e[o + 1]) + (e[o + 2] + e[o + 3])) + ((e[o + 4] + e[o + 5]) + (e[o + 6] + e[o + 7]));
+                    for (int i = 0; i < 8; ++i) pw[b][i] = (_Float16)e[o + i];
+                }
+                // (a block that a row sees nothing of stays out, whatever its scale is)
+                if (whole) {
+                    for (int b = 0; b < 4; ++b) weight = __builtin_fmaf(sum[b], bv[b], weight);
+                } else {
+                    for (int b = 0; b < 4; ++b) weight += sum[b] == 0.0f ? 0.0f : sum[b] * bv[b];
                 }
 #pragma unroll
                 for (int d = 0; d < D / 32; ++d)
