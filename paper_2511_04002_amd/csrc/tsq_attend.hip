@@ -28,6 +28,14 @@ constexpr float kSlack = 8.0f;       // ... and kept until one exceeds that by a
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
 
+// The larger of a lane's value and that of the lane 32 away.
+__device__ __forceinline__ float max_across_halves(float x) {
+    const uint32_t bits = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+    const uint32_t a = r[0], b = r[1];                   // (a cast of an element itself would take the first)
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
 // What a workgroup works on: a row tile of a request (rows: query token and head of the group, the group fastest),
 // a kv head, and a piece of the tile's reach along the cache.
 struct Place {
@@ -89,7 +97,7 @@ __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Place &p, u
     const int64_t p0 = (int64_t)p.length - p.n + first / a.group, p1 = (int64_t)p.length - p.n + last / a.group;
     int64_t lo = a.window ? max(p0 - (int64_t)a.window + 1, (int64_t)0) : 0;
     int64_t hi = a.causal ? min(p1 + 1, (int64_t)p.seen) : (int64_t)p.seen;
-    lo &= ~(int64_t)63;
+    lo &= ~(int64_t)127;             // (a whole tile's, and a block's)
     const int64_t begin = lo + (int64_t)p.split * a.chunk;
     if (p.split + 1 < a.splits) hi = min(hi, begin + a.chunk);
     Reach w;
@@ -274,7 +282,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) void k_attend
             for (int t = 0; t < 4; ++t)
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
             top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
+            top = max_across_halves(top);
             if (__ballot(top > ref + (kRoom + kSlack))) {
                 const float now = fmaxf(ref, top - kRoom), down = pow2(ref - now);
                 ref = now;
@@ -356,23 +364,25 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) void k_attend
 // 8 (i / 4) + 4 hi + i % 4, row n.  P^T as an operand of 16 tokens wants eight of them from each half of the wave:
 // registers 8u .. 8u + 7 are tokens 4 hi + (0..3) and 8 + 4 hi + (0..3) of the 16, so the values' rows in LDS hold
 // each 16 tokens in the order 0-3, 8-11, 4-7, 12-15.
-template <int D>
+template <int D, int TOKENS>
 struct ManyTile {                                        // rows padded by 16 bytes: neighbours begin four banks apart
-    _Float16 k[64][D + 8];
-    _Float16 v[D][64 + 8];
-    float factor[4], log_v[4], back_v[4];                // of each 16 tokens
+    _Float16 k[TOKENS][D + 8];
+    _Float16 v[D][TOKENS + 8];
+    float factor[TOKENS / 16], log_v[TOKENS / 16], back_v[TOKENS / 16];      // of each 16 tokens
 };
 
-template <int D, bool BF16>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a) {
-    constexpr int N = D / 64;                            // 16-byte pieces of keys, and of values, that a thread stages
-    __shared__ ManyTile<D> buffer[2];
+template <int D, bool BF16, int WAVES, int TOKENS>
+__global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a) {
+    constexpr int ROWS = 32 * WAVES, THREADS = 64 * WAVES, SUBS = TOKENS / 16;
+    constexpr int N = TOKENS * D / 16 / THREADS;         // 16-byte pieces of keys, and of values, that a thread stages
+    typedef ManyTile<D, TOKENS> Tile;
+    __shared__ Tile buffer[2];
     Place p;
-    if (!find_place<128>(a, p)) return;
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, hi = lane >> 5;
+    if (!find_place<ROWS>(a, p)) return;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6)), n = lane & 31, hi = lane >> 5;
     const uint32_t B = 1u << a.block_log2;
     for (uint32_t tile = p.tile;; ++tile) {
-        const uint32_t row = tile * 128 + wave * 32 + n, rows = p.n * a.group;
+        const uint32_t row = tile * ROWS + wave * 32 + n, rows = p.n * a.group;
         half8_t q[D / 16];
         float back = 1.0f;
         {
@@ -398,7 +408,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
         }
         uint32_t from, to;
         row_sees(a, p, row, from, to);
-        const Reach reach = reach_of<128>(a, p, tile);
+        const Reach reach = reach_of<ROWS>(a, p, tile);
 
         float16_t acc[D / 32];
 #pragma unroll
@@ -414,15 +424,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
         const int8_t *keys[N], *values[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const uint32_t e = i * 256 + tid;
+            const uint32_t e = i * THREADS + tid;
             keys[i] = a.k + (uint64_t)p.h * B * D + (e / (D / 16) & (B - 1)) * D + 16 * (e % (D / 16));
-            values[i] = a.v + (uint64_t)p.h * B * D + (uint64_t)(e / 4) * B + (16 * (tid & 3) & (B - 1));
+            values[i] = a.v + (uint64_t)p.h * B * D + (uint64_t)(e / SUBS) * B + (16 * (tid % SUBS) & (B - 1));
         }
         Scale scale = {};
         auto ask_entries = [&](uint32_t t0) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) key_entry[i] = table_entry(a, p, t0 + (i * 256 + tid) / (D / 16), reach.end);
-            value_entry = table_entry(a, p, t0 + 16 * (tid & 3), reach.end);
+            for (int i = 0; i < N; ++i) key_entry[i] = table_entry(a, p, t0 + (i * THREADS + tid) / (D / 16), reach.end);
+            value_entry = table_entry(a, p, t0 + 16 * (tid % SUBS), reach.end);
         };
         auto ask = [&](uint32_t t0) {
             const uint32_t half = t0 & (B - 1);
@@ -431,23 +441,23 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
             const uint64_t at = (uint64_t)id_of(a, value_entry) * block_bytes + half;
 #pragma unroll
             for (int i = 0; i < N; ++i) vw[i] = *reinterpret_cast<const uint4_t *>(values[i] + at);
-            if (tid < 4) scale = scale_at(a, p, value_entry);
+            if (tid < SUBS) scale = scale_at(a, p, value_entry);
         };
-        auto put = [&](ManyTile<D> &t) {
+        auto put = [&](Tile &t) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const uint32_t e = i * 256 + tid;
+                const uint32_t e = i * THREADS + tid;
                 half4_t h[4];
                 for (int j = 0; j < 4; ++j) h[j] = codes_to_half(kw[i][j]);
                 _Float16 *to_k = &t.k[e / (D / 16)][16 * (e % (D / 16))];
                 *reinterpret_cast<half8_t *>(to_k) = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
                 *reinterpret_cast<half8_t *>(to_k + 8) = __builtin_shufflevector(h[2], h[3], 0, 1, 2, 3, 4, 5, 6, 7);
                 for (int j = 0; j < 4; ++j) h[j] = codes_to_half(vw[i][j]);
-                _Float16 *to_v = &t.v[e / 4][16 * (e & 3)];
+                _Float16 *to_v = &t.v[e / SUBS][16 * (e % SUBS)];
                 *reinterpret_cast<half8_t *>(to_v) = __builtin_shufflevector(h[0], h[2], 0, 1, 2, 3, 4, 5, 6, 7);
                 *reinterpret_cast<half8_t *>(to_v + 8) = __builtin_shufflevector(h[1], h[3], 0, 1, 2, 3, 4, 5, 6, 7);
             }
-            if (tid < 4) {
+            if (tid < SUBS) {
                 const Block b = block_of(scale, a.scale_log2);
                 t.factor[tid] = b.c;
                 t.log_v[tid] = b.log_v;
@@ -455,37 +465,68 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
             }
         };
 
+        // What a tile brings is asked for a tile ahead and put into the other buffer when the present one is worked on.
         if (reach.begin < reach.end) {
             ask_entries(reach.begin);
             ask(reach.begin);
-            ask_entries(reach.begin + 64);
+            ask_entries(reach.begin + TOKENS);
             put(buffer[0]);
+            ask(reach.begin + TOKENS);
+            ask_entries(reach.begin + 2 * TOKENS);
         }
         __syncthreads();
         uint32_t at = 0;
-        for (uint32_t t0 = reach.begin; t0 < reach.end; t0 += 64, at ^= 1) {
-            const ManyTile<D> &t = buffer[at];
-            const bool more = t0 + 64 < reach.end;
-            ask(t0 + 64);
-            ask_entries(t0 + 128);
-            // (a wave whose rows all end before the tile, or begin behind it, only helps to stage)
-            if (__ballot(from < t0 + 64 && to > t0)) {
+        for (uint32_t t0 = reach.begin; t0 < reach.end; t0 += TOKENS, at ^= 1) {
+            const Tile &t = buffer[at];
+#pragma unroll
+            for (uint32_t part = 0; part < TOKENS; part += 64) {
+                const uint32_t u0 = t0 + part;
+                // (a wave whose rows all end before these tokens, or begin behind them, only helps to stage)
+                if (!__ballot(from < u0 + 64 && to > u0)) continue;
                 float16_t s[2];
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     for (int i = 0; i < 16; ++i) s[c][i] = 0.0f;
 #pragma unroll
                     for (int e = 0; e < D / 16; ++e)
-                        s[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(&t.k[32 * c + n][16 * e + 8 * hi]), q[e], s[c], 0, 0, 0);
+                        s[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(&t.k[part + 32 * c + n][16 * e + 8 * hi]), q[e], s[c], 0, 0, 0);
                 }
-                const bool whole = __ballot(t0 < from || t0 + 64 > to) == 0;
-                const float4_t ks = *reinterpret_cast<const float4_t *>(t.factor), lv = *reinterpret_cast<const float4_t *>(t.log_v);
-                const float4_t bv = *reinterpret_cast<const float4_t *>(t.back_v);
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
+                __builtin_amdgcn_s_setprio(0);
+                const bool whole = __ballot(u0 < from || u0 + 64 > to) == 0;
+                const float4_t ks = *reinterpret_cast<const float4_t *>(t.factor + part / 16), lv = *reinterpret_cast<const float4_t *>(t.log_v + part / 16);
+                const float4_t bv = *reinterpret_cast<const float4_t *>(t.back_v + part / 16);
                 if (!whole) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
                         for (int i = 0; i < 16; ++i) {
-                            const uint32_t token = t0 + 32 * c + 8 * (i / 4) + 4 * hi + i % 4;
+                            const uint32_t token = u0 + 32 * c + 8 * (i / 4) + 4 * hi + i % 4;
                             if (token < from || token >= to) s[c][i] = -INFINITY;
                         }
                 }
@@ -498,7 +539,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
                     // (-inf times a scale of 0 is a NaN, which the maximum passes over)
                     top = fmaxf(top, __builtin_fmaf(m, factor[b], lv[b]));
                 }
-                top = fmaxf(top, __shfl_xor(top, 32));
+                top = max_across_halves(top);
                 if (__ballot(top > ref + (kRoom + kSlack))) {
                     const float now = fmaxf(ref, top - kRoom), down = pow2(ref - now);
                     ref = now;
@@ -516,7 +557,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
                         for (int i = 0; i < 16; ++i) {
-                            const uint32_t token = t0 + 32 * c + 8 * (i / 4) + 4 * hi + i % 4;
+                            const uint32_t token = u0 + 32 * c + 8 * (i / 4) + 4 * hi + i % 4;
                             if (token < from || token >= to) s[c][i] = 0.0f;
                         }
                 }
@@ -534,13 +575,43 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
                 } else {
                     for (int b = 0; b < 4; ++b) weight += sum[b] == 0.0f ? 0.0f : sum[b] * bv[b];
                 }
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int d = 0; d < D / 32; ++d)
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(&t.v[32 * d + n][16 * u + 8 * hi]), pw[u], acc[d], 0, 0, 0);
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(&t.v[32 * d + n][part + 16 * u + 8 * hi]), pw[u], acc[d], 0, 0, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 4, 1);
+                __builtin_amdgcn_s_setprio(0);
             }
-            if (more) put(buffer[at ^ 1]);
+            if (t0 + TOKENS < reach.end) put(buffer[at ^ 1]);
+            ask(t0 + 2 * TOKENS);
+            ask_entries(t0 + 3 * TOKENS);
             __syncthreads();
         }
         weight += __shfl_xor(weight, 32);
@@ -570,7 +641,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
                 }
             }
         }
-        if (!p.last || (uint64_t)(tile + 1) * 128 >= rows) return;
+        if (!p.last || (uint64_t)(tile + 1) * ROWS >= rows) return;
     }
 }
 
@@ -638,7 +709,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
 AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length, uint32_t window) {
     AttendLaunch l;
     const uint64_t group = s.q_heads / s.kv_heads;
-    l.rows = (uint64_t)max_new * group > 32 ? 128 : 16;
+    l.rows = (uint64_t)max_new * group <= 32 ? 16 : s.head_dim == 256 || (uint64_t)max_new * group <= 128 ? 128 : 256;
     const uint64_t each = ((uint64_t)max_new * group + l.rows - 1) / l.rows, packed = tokens * group / l.rows + requests;
     // the same number for every request saves the search for a tile's request; where requests differ much it would
     // launch more workgroups than there are tiles
@@ -650,8 +721,8 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
     uint64_t splits = units >= want ? 1 : want / units, most = (reach + 255) / 256;
     if (splits > most) splits = most;
     if (splits == 0) splits = 1;
-    l.chunk = (uint32_t)(((reach + splits - 1) / splits + 63) / 64 * 64);
-    if (l.chunk == 0) l.chunk = 64;
+    l.chunk = (uint32_t)(((reach + splits - 1) / splits + 127) / 128 * 128);
+    if (l.chunk == 0) l.chunk = 128;
     l.splits = (uint32_t)splits;
     return l;
 }
@@ -661,7 +732,8 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
     const uint32_t grid = l.tiles * l.splits * s.kv_heads;
     by_shape(s, [&](auto d, auto bf16) {
         if (l.rows == 16) k_attend_few<d(), bf16()><<<grid, 256, 0, st>>>(a);
-        else k_attend_many<d(), bf16()><<<grid, 256, 0, st>>>(a);
+        else if (l.rows == 128) k_attend_many<d(), bf16(), 4, 64><<<grid, 256, 0, st>>>(a);
+        else if constexpr (d() != 256) k_attend_many<d(), bf16(), 8, 128><<<grid, 512, 0, st>>>(a);
     });
     if (hipError_t e = hipGetLastError()) return (int)e;
     if (l.splits == 1) return 0;

@@ -67,7 +67,7 @@ struct AttendArgs {
     uint64_t q_stride, out_stride, part_rows;
     uint32_t requests, tokens, q_heads, kv_heads, group, blocks, block_log2, max_blocks;
     uint32_t tiles, tiles_each;  // row tiles of the call; of each request, or 0: they follow one another (see find_tile)
-    uint32_t splits, chunk;      // pieces of a tile's reach along the cache, and the tokens of a piece (a multiple of 64)
+    uint32_t splits, chunk;      // pieces of a tile's reach along the cache, and the tokens of a piece (a multiple of 128)
     uint32_t window;
     int32_t causal;
     float scale_log2;            // scale * log2(e)
