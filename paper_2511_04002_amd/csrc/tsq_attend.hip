@@ -173,27 +173,31 @@ __device__ __forceinline__ uint64_t row_id(const AttendArgs &a, const Place &p, 
     return (uint64_t)(p.begin + row / a.group) * a.q_heads + p.h * a.group + row % a.group;
 }
 
-// Few rows: 16 of a kv head's.  Each of four waves takes every fourth tile of 64 tokens straight from memory to
-// registers and keeps a softmax of its own; they meet in LDS at the end.
+// Few rows: 16 of a kv head's, or 32 (SETS = 2, which share the codes once they are halves).  Each of four waves takes
+// every fourth tile of 64 tokens straight from memory to registers and keeps a softmax of its own; they meet in LDS at
+// the end.
 // Lane (m = lane % 16, g = lane / 16).  The tokens of a tile: group g has 16g .. 16g + 15, all of one block.
 //   S^T tile t (16 tokens x 16 rows): row 4g + i is token 16g + 4t + i, so that a lane's 16 scores (t, i) are the
 //   16 tokens of its group, in the order of its 16 bytes of a value's row; its row of the softmax is m.
 //   Keys: operand row m is token 16 (m / 4) + 4t + m % 4; the lane's k indices are the elements 64f + 16g .. + 15.
-template <int D, bool BF16>
-__global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) void k_attend_few(AttendArgs a) {
+template <int D, bool BF16, int SETS>
+__global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) void k_attend_few(AttendArgs a) {
     constexpr int F = D / 64;                            // 64-element pieces of a head
+    constexpr int ROWS = 16 * SETS;
     __shared__ float sums[4][16][132];
     __shared__ float stats[4][16][2];
     Place p;
-    if (!find_place<16>(a, p)) return;
+    if (!find_place<ROWS>(a, p)) return;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
     const uint32_t B = 1u << a.block_log2;
     for (uint32_t tile = p.tile;; ++tile) {
-        const uint32_t row = tile * 16 + m, rows = p.n * a.group;
-        // queries
-        half8_t q[F][2];
-        float back = 1.0f;
-        {
+        const uint32_t rows = p.n * a.group;
+        half8_t q[SETS][F][2];
+        float back[SETS];
+        uint32_t from[SETS], to[SETS];
+#pragma unroll
+        for (int c = 0; c < SETS; ++c) {
+            const uint32_t row = tile * ROWS + 16 * c + m;
             uint4_t w[F][2];
             uint32_t most = 0;
             for (int f = 0; f < F; ++f)
@@ -207,22 +211,26 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) void k_attend
                     most = max(most, piece_most(w[f][e]));
                 }
             float factor = 1.0f;
+            back[c] = 1.0f;
             if constexpr (BF16) {
                 most = max(most, (uint32_t)__shfl_xor((int)most, 16));
                 most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-                factor = query_factor(most, back);
+                factor = query_factor(most, back[c]);
             }
             for (int f = 0; f < F; ++f)
-                for (int e = 0; e < 2; ++e) q[f][e] = query_piece<BF16>(w[f][e], factor);
+                for (int e = 0; e < 2; ++e) q[c][f][e] = query_piece<BF16>(w[f][e], factor);
+            row_sees(a, p, row, from[c], to[c]);
         }
-        const float row_factor = back * a.scale_log2;
-        uint32_t from, to;
-        row_sees(a, p, row, from, to);
-        const Reach reach = reach_of<16>(a, p, tile);
+        const Reach reach = reach_of<ROWS>(a, p, tile);
 
-        float4_t acc[D / 16];
-        for (int d = 0; d < D / 16; ++d) acc[d] = float4_t{0, 0, 0, 0};
-        float ref = kNone, weight = 0.0f;
+        float4_t acc[SETS][D / 16];
+        float ref[SETS], weight[SETS];
+#pragma unroll
+        for (int c = 0; c < SETS; ++c) {
+            for (int d = 0; d < D / 16; ++d) acc[c][d] = float4_t{0, 0, 0, 0};
+            ref[c] = kNone;
+            weight[c] = 0.0f;
+        }
 
         // Loads are always on their way: a tile's keys are asked for while the tile before it is worked on, its values
         // when that one's are used up, and its block numbers a tile earlier still.
@@ -249,110 +257,120 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 3) void k_attend
             ask_values(t0, entry);
         }
         for (; t0 < reach.end; t0 += 256) {
-            float4_t s[4];
+            float4_t s[SETS][4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                s[t] = float4_t{0, 0, 0, 0};
+                for (int c = 0; c < SETS; ++c) s[c][t] = float4_t{0, 0, 0, 0};
                 for (int f = 0; f < F; ++f)
                     for (int e = 0; e < 2; ++e) {
                         const half4_t x = codes_to_half(kw[t][f][2 * e]), y = codes_to_half(kw[t][f][2 * e + 1]);
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), q[f][e], s[t], 0, 0, 0);
+                        const half8_t k = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+                        for (int c = 0; c < SETS; ++c) s[c][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[c][f][e], s[c][t], 0, 0, 0);
                     }
             }
-            const Block b = block_of(scale, row_factor);
+            const Block b = block_of(scale, a.scale_log2);
             const uint32_t entry = next;
             ask_keys(t0 + 256, entry);
             next = table_entry(a, p, t0 + 512 + 16 * g, reach.end);
             // exponents, and the reference
             const uint32_t mine = t0 + 16 * g;
-            const bool whole = __ballot(mine < from || mine + 16 > to) == 0;
+            half8_t pw[SETS][2];
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                for (int i = 0; i < 4; ++i) s[t][i] = __builtin_fmaf(s[t][i], b.c, b.log_v);
-            if (!whole) {
+            for (int c = 0; c < SETS; ++c) {
+                const bool whole = __ballot(mine < from[c] || mine + 16 > to[c]) == 0;
+                const float f = BF16 ? b.c * back[c] : b.c;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    for (int i = 0; i < 4; ++i) s[c][t][i] = __builtin_fmaf(s[c][t][i], f, b.log_v);
+                if (!whole) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t token = mine + 4 * t + i;
+                            s[c][t][i] = token < from[c] || token >= to[c] ? -INFINITY : s[c][t][i];
+                        }
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[c][t][i]);
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = max_across_halves(top);
+                if (__ballot(top > ref[c] + (kRoom + kSlack))) {
+                    const float now = fmaxf(ref[c], top - kRoom), down = pow2(ref[c] - now);
+                    ref[c] = now;
+                    weight[c] *= down;
+                    for (int d = 0; d < D / 16; ++d) acc[c][d] *= down;
+                }
+                float sum = 0.0f;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
                     for (int i = 0; i < 4; ++i) {
-                        const uint32_t token = mine + 4 * t + i;
-                        s[t][i] = token < from || token >= to ? -INFINITY : s[t][i];
+                        const float e = pow2(s[c][t][i] - ref[c]);
+                        sum += e;
+                        pw[c][t / 2][4 * (t & 1) + i] = (_Float16)e;
                     }
+                // (a group that a row sees nothing of stays out, whatever its scale is)
+                weight[c] += sum == 0.0f ? 0.0f : sum * b.back_v;
             }
-            float top = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = max_across_halves(top);
-            if (__ballot(top > ref + (kRoom + kSlack))) {
-                const float now = fmaxf(ref, top - kRoom), down = pow2(ref - now);
-                ref = now;
-                weight *= down;
-                for (int d = 0; d < D / 16; ++d) acc[d] *= down;
-            }
-            float sum = 0.0f;
-            half8_t pw[2];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                for (int i = 0; i < 4; ++i) {
-                    const float e = pow2(s[t][i] - ref);
-                    sum += e;
-                    pw[t / 2][4 * (t & 1) + i] = (_Float16)e;
-                }
-            // (a group that a row sees nothing of stays out, whatever its scale is)
-            weight += sum == 0.0f ? 0.0f : sum * b.back_v;
 #pragma unroll
             for (int d = 0; d < D / 16; ++d)
                 for (int u = 0; u < 2; ++u) {
                     const half4_t x = codes_to_half(vw[d][2 * u]), y = codes_to_half(vw[d][2 * u + 1]);
-                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), pw[u], acc[d], 0, 0, 0);
+                    const half8_t v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+                    for (int c = 0; c < SETS; ++c) acc[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pw[c][u], acc[c][d], 0, 0, 0);
                 }
             ask_values(t0 + 256, entry);
         }
-        weight += __shfl_xor(weight, 16);
-        weight += __shfl_xor(weight, 32);
 
         // the four waves' sums, at one reference
-        if (g == 0) { stats[wave][m][0] = ref; stats[wave][m][1] = weight; }
-        __syncthreads();
-        float all = fmaxf(fmaxf(stats[0][m][0], stats[1][m][0]), fmaxf(stats[2][m][0], stats[3][m][0]));
-        const float mine = pow2(ref - all);
-        const uint32_t out_row = threadIdx.x >> 4, piece = threadIdx.x & 15, o = tile * 16 + out_row;
-        float total = 0.0f, top = fmaxf(fmaxf(stats[0][out_row][0], stats[1][out_row][0]), fmaxf(stats[2][out_row][0], stats[3][out_row][0]));
-        for (int w = 0; w < 4; ++w) total += stats[w][out_row][1] * pow2(stats[w][out_row][0] - top);
-        const uint64_t id = row_id(a, p, o);
-        for (int part = 0; part < (D + 127) / 128; ++part) {
-            constexpr int N = D < 128 ? D : 128;         // elements at a time
-            if (part) __syncthreads();
-            for (int d = 0; d < N / 16; ++d) *reinterpret_cast<float4_t *>(&sums[wave][m][16 * d + 4 * g]) = acc[part * 8 + d] * mine;
+#pragma unroll
+        for (int c = 0; c < SETS; ++c) {
+            weight[c] += __shfl_xor(weight[c], 16);
+            weight[c] += __shfl_xor(weight[c], 32);
+            if (c) __syncthreads();
+            if (g == 0) { stats[wave][m][0] = ref[c]; stats[wave][m][1] = weight[c]; }
             __syncthreads();
-            if (piece * 8 < N && o < rows) {
-                float y[8];
-                for (int i = 0; i < 8; ++i)
-                    y[i] = sums[0][out_row][8 * piece + i] + sums[1][out_row][8 * piece + i] + sums[2][out_row][8 * piece + i] + sums[3][out_row][8 * piece + i];
-                if (a.splits == 1) {
-                    const float f = total == 0.0f ? 0.0f : 1.0f / total;
-                    uint4_t w;
-                    for (int i = 0; i < 4; ++i) w[i] = narrow2<BF16>(y[2 * i] * f, y[2 * i + 1] * f);
-                    uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)(p.begin + o / a.group) * a.out_stride +
-                                    (uint64_t)(p.h * a.group + o % a.group) * D + part * 128 + piece * 8;
-                    *reinterpret_cast<uint4_t *>(dst) = w;
-                } else {
-                    float *dst = a.parts + (id * a.splits + p.split) * D + part * 128 + piece * 8;
-                    *reinterpret_cast<float4_t *>(dst) = float4_t{y[0], y[1], y[2], y[3]};
-                    *reinterpret_cast<float4_t *>(dst + 4) = float4_t{y[4], y[5], y[6], y[7]};
+            const float all = fmaxf(fmaxf(stats[0][m][0], stats[1][m][0]), fmaxf(stats[2][m][0], stats[3][m][0]));
+            const float mine = pow2(ref[c] - all);
+            const uint32_t out_row = threadIdx.x >> 4, piece = threadIdx.x & 15, o = tile * ROWS + 16 * c + out_row;
+            float total = 0.0f, top = fmaxf(fmaxf(stats[0][out_row][0], stats[1][out_row][0]), fmaxf(stats[2][out_row][0], stats[3][out_row][0]));
+            for (int w = 0; w < 4; ++w) total += stats[w][out_row][1] * pow2(stats[w][out_row][0] - top);
+            const uint64_t id = row_id(a, p, o);
+            for (int part = 0; part < (D + 127) / 128; ++part) {
+                constexpr int N = D < 128 ? D : 128;     // elements at a time
+                if (part) __syncthreads();
+                for (int d = 0; d < N / 16; ++d) *reinterpret_cast<float4_t *>(&sums[wave][m][16 * d + 4 * g]) = acc[c][part * 8 + d] * mine;
+                __syncthreads();
+                if (piece * 8 < N && o < rows) {
+                    float y[8];
+                    for (int i = 0; i < 8; ++i)
+                        y[i] = sums[0][out_row][8 * piece + i] + sums[1][out_row][8 * piece + i] + sums[2][out_row][8 * piece + i] + sums[3][out_row][8 * piece + i];
+                    if (a.splits == 1) {
+                        const float f = total == 0.0f ? 0.0f : 1.0f / total;
+                        uint4_t w;
+                        for (int i = 0; i < 4; ++i) w[i] = narrow2<BF16>(y[2 * i] * f, y[2 * i + 1] * f);
+                        uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)(p.begin + o / a.group) * a.out_stride +
+                                        (uint64_t)(p.h * a.group + o % a.group) * D + part * 128 + piece * 8;
+                        *reinterpret_cast<uint4_t *>(dst) = w;
+                    } else {
+                        float *dst = a.parts + (id * a.splits + p.split) * D + part * 128 + piece * 8;
+                        *reinterpret_cast<float4_t *>(dst) = float4_t{y[0], y[1], y[2], y[3]};
+                        *reinterpret_cast<float4_t *>(dst + 4) = float4_t{y[4], y[5], y[6], y[7]};
+                    }
+                }
+            }
+            if (piece == 0 && o < rows) {
+                if (a.splits > 1) {
+                    float *dst = a.parts + a.part_rows * a.splits * D + (id * a.splits + p.split) * 2;
+                    dst[0] = top;
+                    dst[1] = total;
+                } else if (a.lse) {
+                    a.lse[id] = total == 0.0f ? -INFINITY : (top + log2_of(total)) * 0.69314718055994530942f;
                 }
             }
         }
-        if (piece == 0 && o < rows) {
-            if (a.splits > 1) {
-                float *dst = a.parts + a.part_rows * a.splits * D + (id * a.splits + p.split) * 2;
-                dst[0] = top;
-                dst[1] = total;
-            } else if (a.lse) {
-                a.lse[id] = total == 0.0f ? -INFINITY : (top + log2_of(total)) * 0.69314718055994530942f;
-            }
-        }
-        if (!p.last || (uint64_t)(tile + 1) * 16 >= rows) return;
+        if (!p.last || (uint64_t)(tile + 1) * ROWS >= rows) return;
         __syncthreads();
     }
 }
@@ -706,24 +724,43 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
 
 }  // namespace
 
+// Which kernel, how many rows a workgroup, and into how many pieces the cache's length is cut.
+//
+// Rows: a request with at most 64 rows of a kv head goes to k_attend_few, whose time is the cache's bytes as long as
+// they are read once or twice (32 requests of 8192 tokens, 64 heads on 8 of 128, 4 queries each: 140 us in two passes
+// of 16 rows, 202 us by k_attend_many).  k_attend_many takes 256 rows a workgroup, 128 where a request has no more.
+// Pieces: `slots` workgroups run at once.  Fewer units than that leave the device partly idle, so each is cut; a piece
+// costs its start and its share of the join.
 AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length, uint32_t window) {
     AttendLaunch l;
-    const uint64_t group = s.q_heads / s.kv_heads;
-    l.rows = (uint64_t)max_new * group <= 32 ? 16 : s.head_dim == 256 || (uint64_t)max_new * group <= 128 ? 128 : 256;
-    const uint64_t each = ((uint64_t)max_new * group + l.rows - 1) / l.rows, packed = tokens * group / l.rows + requests;
-    // the same number for every request saves the search for a tile's request; where requests differ much it would
-    // launch more workgroups than there are tiles
-    l.tiles_each = each == 0 ? 1u : (uint32_t)(each * requests <= packed ? each : 0);
-    l.tiles = (uint32_t)(l.tiles_each ? (uint64_t)l.tiles_each * requests : packed);
+    const uint64_t group = s.q_heads / s.kv_heads, most = max_new * group;
+    auto tile = [&](uint32_t rows) {
+        l.rows = rows;
+        const uint64_t each = (most + rows - 1) / rows, packed = tokens * group / rows + requests;
+        // the same number for every request saves the search for a tile's request; where requests differ much it would
+        // launch more workgroups than there are tiles
+        l.tiles_each = each == 0 ? 1u : (uint32_t)(each * requests <= packed ? each : 0);
+        l.tiles = (uint32_t)(l.tiles_each ? (uint64_t)l.tiles_each * requests : packed);
+    };
+    uint64_t slots;
+    if (most <= (s.head_dim == 256 ? 32 : 64)) {
+        tile(most <= 16 || s.head_dim == 256 ? 16 : 32);
+        slots = s.head_dim == 256 ? 256 : s.head_dim == 128 || l.rows == 32 ? 512 : 768;
+    } else {
+        tile(s.head_dim == 256 || most <= 128 ? 128 : 256);
+        slots = s.head_dim == 256 || l.rows == 256 ? 256 : 512;
+    }
     uint64_t reach = max_length;
     if (window && reach > (uint64_t)window + max_new) reach = (uint64_t)window + max_new;
-    const uint64_t units = (uint64_t)l.tiles * s.kv_heads, want = l.rows == 16 ? 1024 : 512;
-    uint64_t splits = units >= want ? 1 : want / units, most = (reach + 255) / 256;
-    if (splits > most) splits = most;
+    const uint64_t units = (uint64_t)l.tiles * s.kv_heads, longest = (reach + 255) / 256;
+    uint64_t splits = slots / (units ? units : 1);
+    if (splits > longest) splits = longest;
     if (splits == 0) splits = 1;
     l.chunk = (uint32_t)(((reach + splits - 1) / splits + 127) / 128 * 128);
     if (l.chunk == 0) l.chunk = 128;
-    l.splits = (uint32_t)splits;
+    // (pieces of whole tiles may be fewer)
+    l.splits = (uint32_t)((reach + l.chunk - 1) / l.chunk);
+    if (l.splits == 0) l.splits = 1;
     return l;
 }
 
@@ -731,7 +768,8 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const uint32_t grid = l.tiles * l.splits * s.kv_heads;
     by_shape(s, [&](auto d, auto bf16) {
-        if (l.rows == 16) k_attend_few<d(), bf16()><<<grid, 256, 0, st>>>(a);
+        if (l.rows == 16) k_attend_few<d(), bf16(), 1><<<grid, 256, 0, st>>>(a);
+        else if (l.rows == 32) { if constexpr (d() != 256) k_attend_few<d(), bf16(), 2><<<grid, 256, 0, st>>>(a); }
         else if (l.rows == 128) k_attend_many<d(), bf16(), 4, 64><<<grid, 256, 0, st>>>(a);
         else if constexpr (d() != 256) k_attend_many<d(), bf16(), 8, 128><<<grid, 512, 0, st>>>(a);
     });
