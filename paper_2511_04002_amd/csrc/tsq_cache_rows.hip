@@ -261,8 +261,8 @@ __global__ __launch_bounds__(256) void k_norm_rotate(NormRotateArgs a, uint32_t 
             o0[i] = narrow2<BF16>(y[2 * i], y[2 * i + 1]);
             o1[i] = narrow2<BF16>(y[8 + 2 * i], y[9 + 2 * i]);
         }
-        *reinterpret_cast<uint4_t *>(out + e0) = o0;
-        *reinterpret_cast<uint4_t *>(out + e1) = o1;
+        __builtin_nontemporal_store(o0, reinterpret_cast<uint4_t *>(out + e0));
+        __builtin_nontemporal_store(o1, reinterpret_cast<uint4_t *>(out + e1));
     }
 }
 
@@ -602,15 +602,15 @@ __global__ __launch_bounds__(256) void k_gather(GatherArgs a) {
                 uint4_t y;
                 for (int e = 0; e < 4; ++e)
                     y[e] = narrow2<BF16>(code_at(kw[t][e / 2], 2 * (e & 1)) * k_scale, code_at(kw[t][e / 2], 2 * (e & 1) + 1) * k_scale);
-                *reinterpret_cast<uint4_t *>(k_out + (TPI * t + sub) * a.stride[0] + 8 * piece) = y;
+                __builtin_nontemporal_store(y, reinterpret_cast<uint4_t *>(k_out + (TPI * t + sub) * a.stride[0] + 8 * piece));
             }
             auto put = [&](const uint32_t *w, uint32_t byte, uint32_t t) {     // a token's elements: byte of each w[e]
                 uint16_t *to = v_out + (uint64_t)t * a.stride[1] + E * lane;
                 float y[E];
                 for (int e = 0; e < E; ++e) y[e] = code_at(w[e], (int)byte) * v_scale;
-                if constexpr (E == 1) to[0] = (uint16_t)narrow<BF16>(y[0]);
-                else if constexpr (E == 2) *reinterpret_cast<uint32_t *>(to) = narrow2<BF16>(y[0], y[1]);
-                else *reinterpret_cast<uint2_t *>(to) = uint2_t{narrow2<BF16>(y[0], y[1]), narrow2<BF16>(y[2], y[3])};
+                if constexpr (E == 1) __builtin_nontemporal_store((uint16_t)narrow<BF16>(y[0]), to);
+                else if constexpr (E == 2) __builtin_nontemporal_store(narrow2<BF16>(y[0], y[1]), reinterpret_cast<uint32_t *>(to));
+                else __builtin_nontemporal_store(uint2_t{narrow2<BF16>(y[0], y[1]), narrow2<BF16>(y[2], y[3])}, reinterpret_cast<uint2_t *>(to));
             };
             if (n == 16 && o == first) {
 #pragma unroll
