@@ -431,6 +431,18 @@ __device__ __forceinline__ void store_values(const uint16_t *x, uint64_t stride,
                 for (int i = 0; i < 4; ++i) v[i] = recode(v[i], s.factor);
                 *at = v;
             }
+    if (n == 1 && !s.again) {
+        // one token into a block whose scale stays: its bytes alone
+        Row one = {};
+        const uint16_t *row = x + E * lane;
+        if constexpr (E == 1) one.v[0] = row[0];
+        else if constexpr (E == 2) one.v[0] = *reinterpret_cast<const uint32_t *>(row);
+        else { const uint2_t q = *reinterpret_cast<const uint2_t *>(row); one.v[0] = q[0]; one.v[1] = q[1]; }
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            codes[(uint64_t)(E * lane + e) * B + o] = (int8_t)code_bits(widen<BF16>((one.v[e / 2] >> (16 * (e & 1))) & 0xFFFFu), s.inverse);
+        return;
+    }
     auto put = [&](const Row *from, uint32_t c) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -674,7 +686,7 @@ int launch_append(const CacheShape &s, const AppendArgs &args, void *stream) {
     const uint64_t windows = ((uint64_t)a.tokens + a.window - 1) / a.window;
     // as many waves as fill the device, if there is work for them: at most a run a row
     const uint64_t most = (uint64_t)(a.tokens < a.window ? a.tokens : a.window) * s.kv_heads * 2;
-    uint64_t each = (8192 + windows - 1) / windows;
+    uint64_t each = (16384 + windows - 1) / windows;
     if (each > most) each = most;
     a.waves_each = (uint32_t)each;
     uint32_t grid;
