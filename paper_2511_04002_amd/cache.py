@@ -162,7 +162,9 @@ class Cache:
             tsq_cache_destroy(h)
             self.handle = None
 
-    _stream = staticmethod(tsq.Plan._stream)
+    @staticmethod
+    def _stream() -> int:
+        return (tsq._current_stream or tsq.Plan._stream)()
 
     # -------------------------------------------------------------- buffers
 
@@ -210,6 +212,14 @@ class Cache:
         if not (x.dtype is self.int32 and x.is_cuda and x.is_contiguous() and x.numel() == n):
             _refuse("%s is int32 on the GPU, contiguous, %d elements" % (what, n))
         return x.data_ptr()
+
+    def _requests(self, table, starts, lengths, n):
+        i32 = self.int32
+        if not (table.dtype is i32 and starts.dtype is i32 and lengths.dtype is i32 and table.is_cuda and starts.is_cuda and lengths.is_cuda and
+                table.is_contiguous() and starts.is_contiguous() and lengths.is_contiguous() and
+                table.numel() == n * self.max_blocks and starts.numel() == n + 1):
+            _refuse("table, starts and lengths are int32 on the GPU, contiguous, [%d, %d], [%d] and [%d]" % (n, self.max_blocks, n + 1, n))
+        return table.data_ptr(), starts.data_ptr(), lengths.data_ptr()
 
     def _rows(self, x, tokens, heads, what):
         """x: [tokens, heads, head_dim], or [tokens, heads * head_dim]; rows anywhere, the heads of a row together.
@@ -293,10 +303,8 @@ class Cache:
         tokens, n = k_out.shape[0], lengths.numel()
         kp, ks = self._rows(k_out, tokens, self.kv_heads, "k_out")
         vp, vs = self._rows(v_out, tokens, self.kv_heads, "v_out")
-        i = self._ints
-        status = self._lib.tsq_cache_gather(
-            self.handle, memory.ref, n, i(table, n * self.max_blocks, "table"), i(starts, n + 1, "starts"),
-            i(lengths, n, "lengths"), tokens, kp, ks, vp, vs, self._stream())
+        status = self._lib.tsq_cache_gather(self.handle, memory.ref, n, *self._requests(table, starts, lengths, n), tokens, kp, ks, vp, vs,
+                                            self._stream())
         if status:
             raise TsqError(status, "tsq_cache_gather")
         return k_out, v_out
@@ -319,16 +327,18 @@ class Cache:
             if not (lse.dtype is self.float32 and lse.is_cuda and lse.is_contiguous() and lse.numel() == tokens * self.q_heads):
                 _refuse("lse is float32 [tokens, q_heads] on the GPU, contiguous")
             lp = lse.data_ptr()
-        i, L = self._ints, self._lib
-        need = L.tsq_cache_attend_workspace_bytes(self.handle, n, tokens, max_new, max_length, window)
-        if need and ws is None:
-            ws = self._empty(need, self._torch.uint8)
-        if need and not (ws.is_cuda and ws.is_contiguous() and ws.numel() * ws.element_size() >= need):
-            _refuse("ws has %d bytes on the GPU, contiguous" % need)
+        L, wp = self._lib, None
+        # (256 tokens are never cut, and then there is no workspace)
+        need = 0 if max_length <= 256 else L.tsq_cache_attend_workspace_bytes(self.handle, n, tokens, max_new, max_length, window)
+        if need:
+            if ws is None:
+                ws = self._empty(need, self._torch.uint8)
+            if not (ws.is_cuda and ws.is_contiguous() and ws.numel() * ws.element_size() >= need):
+                _refuse("ws has %d bytes on the GPU, contiguous" % need)
+            wp = ws.data_ptr()
         status = L.tsq_cache_attend(
-            self.handle, memory.ref, n, i(table, n * self.max_blocks, "table"), i(starts, n + 1, "starts"),
-            i(lengths, n, "lengths"), tokens, max_new, max_length, qp, qs, self.head_dim ** -0.5 if scale is None else scale,
-            causal, window, op, os_, lp, ws.data_ptr() if need else None, self._stream())
+            self.handle, memory.ref, n, *self._requests(table, starts, lengths, n), tokens, max_new, max_length, qp, qs,
+            self.head_dim ** -0.5 if scale is None else scale, causal, window, op, os_, lp, wp, self._stream())
         if status:
             raise TsqError(status, "tsq_cache_attend")
         return out

@@ -149,3 +149,11 @@ def test_attend_workspace(L, handle):
     one = f(handle, 1, 1, 1, 1 << 20)
     assert one > 0 and one % (8 * 130 * 4) == 0              # pieces of [q_heads] rows: sums and two statistics each
     assert f(handle, 1, 1, 1, 1 << 20, 100) == 0             # a window leaves little to split
+
+
+def test_attend_of_256_tokens_needs_no_workspace(L):
+    for heads, dim in ((1, 64), (8, 128), (1, 256)):
+        h = cache.tsq_cache_create(cfg(q_heads=heads, kv_heads=1, head_dim=dim))
+        for tokens, new in ((1, 1), (7, 7), (256, 256), (5000, 1)):
+            assert cache.tsq_cache_attend_workspace_bytes(h, 1, tokens, new, 256) == 0
+        cache.tsq_cache_destroy(h)
