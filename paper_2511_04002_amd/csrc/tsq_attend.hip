@@ -675,18 +675,33 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
     const uint64_t id = (uint64_t)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
     if (id >= a.part_rows) return;
     const uint32_t token = (uint32_t)(id / a.q_heads), head = (uint32_t)(id % a.q_heads);
-    // rows that no request has were not computed and are not written
-    uint32_t lo = 0, hi = a.requests;
-    while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) >> 1;
-        if (a.starts[mid] <= (int32_t)token) lo = mid; else hi = mid;
-    }
-    if ((int32_t)token < a.starts[lo] || (int32_t)token >= a.starts[lo + 1]) return;
+    // What most rows have is asked for at once: the first pieces of each lane and their statistics.
     const uint32_t part = tid / LANES, piece = tid % LANES;
     const float *parts = a.parts + id * a.splits * D + 4 * piece, *stats = a.parts + a.part_rows * a.splits * D + id * a.splits * 2;
+    constexpr int KEPT = 4;
+    float4_t v[KEPT];
+    float2_t st[KEPT];
+#pragma unroll
+    for (int u = 0; u < KEPT; ++u) {
+        const uint32_t i = min(part + u * PIECES, a.splits - 1);
+        st[u] = *reinterpret_cast<const float2_t *>(stats + 2 * i);
+        v[u] = *reinterpret_cast<const float4_t *>(parts + (uint64_t)i * D);
+    }
+    // rows that no request has were not computed and are not written
+    uint32_t lo = 0, hi = a.requests;
+    while (hi - lo > 1) {                                // a wave halves 64 times at once
+        const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const uint64_t below = __ballot(at < hi && a.starts[at] <= (int32_t)token);
+        const uint32_t last = 63 - (uint32_t)__builtin_clzll(below | 1);
+        hi = min(hi, lo + (last + 1) * step);
+        lo += last * step;
+    }
+    if ((int32_t)token < a.starts[lo] || (int32_t)token >= a.starts[lo + 1]) return;
     float top = kNone;
-    for (uint32_t i = tid; i < a.splits; i += 64 * WAVES) top = fmaxf(top, stats[2 * i]);
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+#pragma unroll
+    for (int u = 0; u < KEPT; ++u) top = fmaxf(top, st[u][0]);
+    for (uint32_t i = part + KEPT * PIECES; i < a.splits; i += PIECES) top = fmaxf(top, stats[2 * i]);
+    for (uint32_t d = LANES; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, (int)d));
     if constexpr (WAVES > 1) {
         if (lane == 0) tops[wave] = top;
         __syncthreads();
@@ -694,14 +709,17 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
     }
     float total = 0.0f;
     float4_t y = {0, 0, 0, 0};
-#pragma unroll 4
-    for (uint32_t i = part; i < a.splits; i += PIECES) {
-        const float w = stats[2 * i + 1], f = pow2(stats[2 * i] - top);
-        const float4_t v = *reinterpret_cast<const float4_t *>(parts + (uint64_t)i * D);
+    auto add = [&](float2_t t, float4_t x) {
         // (of a piece that the row sees nothing of, the sums are 0)
-        total = __builtin_fmaf(w, f, total);
-        for (int e = 0; e < 4; ++e) y[e] = __builtin_fmaf(v[e], f, y[e]);
-    }
+        const float f = pow2(t[0] - top);
+        total = __builtin_fmaf(t[1], f, total);
+        for (int e = 0; e < 4; ++e) y[e] = __builtin_fmaf(x[e], f, y[e]);
+    };
+#pragma unroll
+    for (int u = 0; u < KEPT; ++u)
+        if (part + u * PIECES < a.splits) add(st[u], v[u]);
+    for (uint32_t i = part + KEPT * PIECES; i < a.splits; i += PIECES)
+        add(*reinterpret_cast<const float2_t *>(stats + 2 * i), *reinterpret_cast<const float4_t *>(parts + (uint64_t)i * D));
     for (uint32_t d = LANES; d < 64; d <<= 1) {
         total += __shfl_xor(total, (int)d);
         for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], (int)d);
@@ -750,9 +768,9 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
         tile(s.head_dim == 256 || most <= 128 ? 128 : 256);
         slots = s.head_dim == 256 || l.rows == 256 ? 256 : 512;
     }
-    uint64_t reach = max_length;
+    uint64_t reach = max_length, least = l.rows >= 128 ? 128 : 256;     // a tile of k_attend_many, one of each wave of k_attend_few
     if (window && reach > (uint64_t)window + max_new) reach = (uint64_t)window + max_new;
-    const uint64_t units = (uint64_t)l.tiles * s.kv_heads, longest = (reach + 255) / 256;
+    const uint64_t units = (uint64_t)l.tiles * s.kv_heads, longest = reach <= 256 ? 1 : (reach + least - 1) / least;
     uint64_t splits = slots / (units ? units : 1);
     if (splits > longest) splits = longest;
     if (splits == 0) splits = 1;
