@@ -633,3 +633,29 @@ def test_tensors_that_do_not_fit_are_refused(call):
         args[at] = x
         with pytest.raises(ValueError):
             f(*args)
+
+
+@pytest.mark.parametrize("heads", [(1, 1, 64), (2, 1, 128), (1, 1, 256)])
+@pytest.mark.parametrize("rows", [15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 255, 257])
+def test_attend_around_the_lines_between_the_kernels(heads, rows):
+    """The most rows of a kv head that a request has decide which kernel runs and with how many rows a workgroup."""
+    hq, hk, dim = heads
+    new = -(-rows // hq)
+    for block, past in ((16, 0), (128, 300)):
+        b = Both(2 * (new + past) // block + 6, block, hk, dim, "f16", (new + past) // block + 2, rows, q_heads=hq)
+        attend_both(b, hq, [new, max(1, new // 2)], [new + past, new + past - 7 if past else new])
+
+
+def test_attend_requests_of_one_call_in_two():
+    """A call may cover a part of the requests: rows and requests are those of the whole step."""
+    b = Both(60, 16, 2, 128, "f16", 20, 31, q_heads=8)
+    table = dev(b.g.permutation(60).reshape(3, 20).astype(np.int32))
+    starts, lengths = dev(np.array([0, 1, 2, 102], np.int32)), dev(np.array([200, 310, 100], np.int32))
+    q = rows(b.g, 102, 8, 128, "f16")
+    want = b.c.attend(b.m, q, table, starts, lengths, 100, 310)
+    out = torch.zeros_like(want)
+    b.c.attend(b.m, q, table[:2], starts[:3], lengths[:2], 1, 310, out=out)
+    assert (out[2:] == 0).all()
+    b.c.attend(b.m, q, table[2:], starts[2:], lengths[2:], 100, 100, out=out)
+    # (other kernels sum in another order: a few units of an 11-bit significand)
+    assert ((out - want).abs() <= 2.0 ** -9 * want.abs().amax(-1, keepdim=True)).all()
