@@ -477,6 +477,72 @@ __device__ __forceinline__ void store_values(const uint16_t *x, uint64_t stride,
     }
 }
 
+// The largest of N lanes that follow one another (8, 16 or 32), in all of them.
+template <int N> __device__ __forceinline__ uint32_t group_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));          // lane ^ 1
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));          // lane ^ 2
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));         // the other four of eight
+    if constexpr (N >= 16) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));  // ... eight of sixteen
+    if constexpr (N == 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16));
+    return v;
+}
+
+// A single token, as every request brings one in a step of decoding: D / 8 lanes a head, 512 / D heads at once, since
+// one token's head is too little for a wave and a step's time is its waits, one after the other.  512 tokens on 40
+// heads of 128: 30 us a (token, head) a wave, see k_append for what it is now.
+template <int D, bool BF16, int WHICH>
+__device__ __forceinline__ void store_single(const uint16_t *x, int8_t *codes, float *scale, uint32_t B, uint32_t o, uint32_t h0, uint32_t heads) {
+    constexpr uint32_t LPT = D / 8;
+    const uint32_t lane = threadIdx.x & 63, piece = lane % LPT, h = h0 + lane / LPT;
+    const bool real = h < heads;
+    uint4_t w = {0, 0, 0, 0};
+    float before = 0.0f;
+    if (real) {
+        w = *reinterpret_cast<const uint4_t *>(x + (uint64_t)h * D + 8 * piece);
+        if (o) before = scale[h];
+    }
+    uint32_t most = 0;
+    for (int j = 0; j < 4; ++j) most = max(most, max(w[j] & 0x7FFFu, (w[j] >> 16) & 0x7FFFu));
+    const Scales s = scales_of<BF16>(group_max<LPT>(most), before);
+    if (!real) return;
+    if (piece == 0) scale[h] = s.now;
+    uint32_t q[8];
+    for (int j = 0; j < 4; ++j) {
+        q[2 * j] = code_bits(widen<BF16>(w[j] & 0xFFFFu), s.inverse);
+        q[2 * j + 1] = code_bits(widen<BF16>(w[j] >> 16), s.inverse);
+    }
+    int8_t *mine = codes + (uint64_t)h * B * D;
+    if constexpr (WHICH == 0) {
+        if (s.again)
+            for (uint32_t at = piece * 16; at < o * D; at += LPT * 16) {
+                uint4_t v = *reinterpret_cast<const uint4_t *>(mine + at);
+                for (int i = 0; i < 4; ++i) v[i] = recode(v[i], s.factor);
+                *reinterpret_cast<uint4_t *>(mine + at) = v;
+            }
+        *reinterpret_cast<uint2_t *>(mine + (uint64_t)o * D + 8 * piece) = uint2_t{four_bytes(q[0], q[1], q[2], q[3]), four_bytes(q[4], q[5], q[6], q[7])};
+    } else {
+        mine += (uint64_t)(8 * piece) * B;               // the lane's elements
+        if (!s.again) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mine[e * B + o] = (int8_t)q[e];
+            return;
+        }
+        for (uint32_t c = 0; c <= o; c += 16) {
+            uint4_t v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const uint4_t *>(mine + e * B + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                for (uint32_t i = 0; i < 4; ++i) {
+                    v[e][i] = recode(v[e][i], s.factor);
+                    if (o - c < 16 && (o - c) / 4 == i) v[e][i] = (v[e][i] & ~(0xFFu << (8 * (o & 3)))) | (q[e] & 0xFFu) << (8 * (o & 3));
+                }
+                *reinterpret_cast<uint4_t *>(mine + e * B + c) = v[e];
+            }
+        }
+    }
+}
+
 // A window of rows for waves_each waves: each finds the runs that begin in it, one row a lane, and takes its share of
 // (run, head, keys or values).
 template <int D, bool BF16>
@@ -493,7 +559,29 @@ __global__ __launch_bounds__(256, D == 256 ? 3 : 4) void k_append(AppendArgs a) 
     const bool real = slot >= 0 && ((uint32_t)slot >> a.block_log2) < a.blocks;
     const bool follows = real && ((uint32_t)slot & (B - 1)) && previous == slot - 1;
     const uint64_t leads = __ballot(real && !follows), goes = __ballot(follows);
-    const uint32_t runs = (uint32_t)__builtin_popcountll(leads), each = a.kv_heads * 2;
+    const uint32_t runs = (uint32_t)__builtin_popcountll(leads);
+    // single tokens alone: none follows another, here or behind the window
+    bool follows_on = false;
+    if (lane == a.window - 1 && real && row + 1 < a.tokens) follows_on = a.slots[row + 1] == slot + 1 && ((uint32_t)slot + 1 & (B - 1));
+    if (goes == 0 && __ballot(follows_on) == 0) {
+        constexpr uint32_t AT_ONCE = 512 / D;
+        const uint32_t groups = (a.kv_heads + AT_ONCE - 1) / AT_ONCE, each = groups * 2;
+        uint64_t left = leads;
+        uint32_t nth = 0;
+        for (uint32_t u = (uint32_t)(wave % a.waves_each); u < runs * each; u += a.waves_each) {
+            for (; nth < u / each; ++nth) left &= left - 1;
+            const uint32_t l = (uint32_t)__builtin_ctzll(left), at = of_lane((uint32_t)slot, l), which = u % each & 1, h0 = u % each / 2 * AT_ONCE;
+            const uint64_t block = at >> a.block_log2;
+            if (which == 0)
+                store_single<D, BF16, 0>(static_cast<const uint16_t *>(a.x[0]) + (begin + l) * a.stride[0], a.codes[0] + block * a.kv_heads * B * D,
+                                         a.scale[0] + block * a.kv_heads, B, at & (B - 1), h0, a.kv_heads);
+            else
+                store_single<D, BF16, 1>(static_cast<const uint16_t *>(a.x[1]) + (begin + l) * a.stride[1], a.codes[1] + block * a.kv_heads * B * D,
+                                         a.scale[1] + block * a.kv_heads, B, at & (B - 1), h0, a.kv_heads);
+        }
+        return;
+    }
+    const uint32_t each = a.kv_heads * 2;
     uint32_t nth = ~0u, o = 0, n = 0;
     uint64_t row0 = 0, block = 0;
     uint64_t left = leads;
@@ -574,47 +662,64 @@ __global__ __launch_bounds__(256) void k_gather(GatherArgs a) {
     int32_t block = -1;
     if (owned && position >= 0 && ((uint64_t)position >> a.block_log2) < a.max_blocks) block = a.table[(uint64_t)r * a.max_blocks + nth];
     if ((uint32_t)block >= a.blocks) block = -1;
+    const uint32_t place = (uint32_t)position & (B - 1);
+    // keys: each row by itself, wherever it lies
+    constexpr uint32_t LPT = D / 8, TPI = 64 / LPT, LOADS = 16 / TPI;
+    constexpr int E = D / 64;
+    const uint32_t piece = lane % LPT, sub = lane / LPT;
+    uint32_t key_block[LOADS], key_place[LOADS];
+#pragma unroll
+    for (uint32_t t = 0; t < LOADS; ++t) {
+        key_block[t] = (uint32_t)__shfl(owned ? block : -2, (int)(TPI * t + sub));
+        key_place[t] = (uint32_t)__shfl((int)place, (int)(TPI * t + sub));
+    }
     const uint32_t before_r = (uint32_t)__shfl_up((int)r, 1), before_n = (uint32_t)__shfl_up((int)nth, 1);
     const int before_owned = __shfl_up((int)owned, 1);
     const bool leads = owned && lane < 16 && (lane == 0 || !before_owned || before_r != r || before_n != nth);
-    const uint32_t ours = (uint32_t)__ballot(owned && lane < 16);
-    uint32_t left = (uint32_t)__ballot(leads);
-    while (left) {
-        const uint32_t l = (uint32_t)__builtin_ctz(left);
-        left &= left - 1;
-        // rows of the run: up to the next leader, as far as a request has them
-        const uint32_t reach = left ? (uint32_t)__builtin_ctz(left) : 16u;
-        const uint32_t n = min(reach - l, (uint32_t)__builtin_ctz(~(ours >> l)));
-        const int32_t b = (int32_t)of_lane((uint32_t)block, l);
-        const uint32_t o = of_lane((uint32_t)position, l) & (B - 1);
-        const uint64_t row = begin + l;
-        for (uint32_t h = blockIdx.x % a.waves_each; h < a.kv_heads; h += a.waves_each) {
+    const uint32_t ours = (uint32_t)__ballot(owned && lane < 16), runs = (uint32_t)__ballot(leads);
+    for (uint32_t h = blockIdx.x % a.waves_each; h < a.kv_heads; h += a.waves_each) {
+        uint2_t kw[LOADS];
+        float k_scale[LOADS];
+#pragma unroll
+        for (uint32_t t = 0; t < LOADS; ++t) {
+            const uint64_t head = (uint64_t)((int32_t)key_block[t] < 0 ? 0 : key_block[t]) * a.kv_heads + h;
+            kw[t] = *reinterpret_cast<const uint2_t *>(a.codes[0] + (head * B + key_place[t]) * D + 8 * piece);
+            k_scale[t] = a.scale[0][head];
+        }
+        uint32_t left = runs;
+        bool keys_done = false;
+        do {
+            // values: the rows of a run, which lie in one block at places that follow one another, 16 places of an
+            // element side by side; what the first of them needs is asked for before the keys are written
+            const uint32_t l = left ? (uint32_t)__builtin_ctz(left) : 0;
+            const bool some = left != 0;
+            left &= left - 1;
+            const uint32_t reach = left ? (uint32_t)__builtin_ctz(left) : 16u;
+            const uint32_t n = some ? min(reach - l, (uint32_t)__builtin_ctz(~(ours >> l))) : 0;
+            const int32_t b = some ? (int32_t)of_lane((uint32_t)block, l) : -1;
+            const uint32_t o = of_lane(place, l), first = o / 16 * 16;
             const uint64_t head = (uint64_t)max(b, 0) * a.kv_heads + h;
-            const float k_scale = b < 0 ? __builtin_nanf("") : a.scale[0][head], v_scale = b < 0 ? __builtin_nanf("") : a.scale[1][head];
-            const int8_t *keys = a.codes[0] + head * B * D, *values = a.codes[1] + head * B * D;
-            uint16_t *k_out = static_cast<uint16_t *>(a.out[0]) + row * a.stride[0] + (uint64_t)h * D;
-            uint16_t *v_out = static_cast<uint16_t *>(a.out[1]) + row * a.stride[1] + (uint64_t)h * D;
-            constexpr uint32_t LPT = D / 8, TPI = 64 / LPT, LOADS = 16 / TPI;
-            constexpr int E = D / 64;
-            const uint32_t piece = lane % LPT, sub = lane / LPT, first = o / 16 * 16;
-            uint2_t kw[LOADS];
+            const float v_scale = b < 0 ? __builtin_nanf("") : a.scale[1][head];
+            const int8_t *values = a.codes[1] + (head * D + E * lane) * B + first;
+            uint16_t *v_out = static_cast<uint16_t *>(a.out[1]) + (begin + l) * a.stride[1] + (uint64_t)h * D;
             uint4_t vw[E], vx[E];
 #pragma unroll
-            for (uint32_t t = 0; t < LOADS; ++t)
-                if (TPI * t + sub < n) kw[t] = *reinterpret_cast<const uint2_t *>(keys + (uint64_t)(o + TPI * t + sub) * D + 8 * piece);
-#pragma unroll
             for (int e = 0; e < E; ++e) {
-                const int8_t *at = values + (uint64_t)(E * lane + e) * B + first;
-                vw[e] = *reinterpret_cast<const uint4_t *>(at);
-                if (first + 16 < o + n) vx[e] = *reinterpret_cast<const uint4_t *>(at + 16);
+                vw[e] = *reinterpret_cast<const uint4_t *>(values + e * B);
+                if (first + 16 < o + n) vx[e] = *reinterpret_cast<const uint4_t *>(values + e * B + 16);
             }
+            if (!keys_done) {
+                keys_done = true;
 #pragma unroll
-            for (uint32_t t = 0; t < LOADS; ++t) {
-                if (TPI * t + sub >= n) continue;
-                uint4_t y;
-                for (int e = 0; e < 4; ++e)
-                    y[e] = narrow2<BF16>(code_at(kw[t][e / 2], 2 * (e & 1)) * k_scale, code_at(kw[t][e / 2], 2 * (e & 1) + 1) * k_scale);
-                __builtin_nontemporal_store(y, reinterpret_cast<uint4_t *>(k_out + (TPI * t + sub) * a.stride[0] + 8 * piece));
+                for (uint32_t t = 0; t < LOADS; ++t) {
+                    if ((int32_t)key_block[t] == -2) continue;
+                    const float scale = (int32_t)key_block[t] < 0 ? __builtin_nanf("") : k_scale[t];
+                    uint4_t y;
+                    for (int e = 0; e < 4; ++e)
+                        y[e] = narrow2<BF16>(code_at(kw[t][e / 2], 2 * (e & 1)) * scale, code_at(kw[t][e / 2], 2 * (e & 1) + 1) * scale);
+                    uint16_t *k_out = static_cast<uint16_t *>(a.out[0]) + (begin + TPI * t + sub) * a.stride[0] + (uint64_t)h * D + 8 * piece;
+                    __builtin_nontemporal_store(y, reinterpret_cast<uint4_t *>(k_out));
+                }
             }
             auto put = [&](const uint32_t *w, uint32_t byte, uint32_t t) {     // a token's elements: byte of each w[e]
                 uint16_t *to = v_out + (uint64_t)t * a.stride[1] + E * lane;
@@ -644,7 +749,7 @@ __global__ __launch_bounds__(256) void k_gather(GatherArgs a) {
                     put(w, p & 3, t);
                 }
             }
-        }
+        } while (left);
     }
 }
 

@@ -659,3 +659,31 @@ def test_attend_requests_of_one_call_in_two():
     b.c.attend(b.m, q, table[2:], starts[2:], lengths[2:], 100, 100, out=out)
     # (other kernels sum in another order: a few units of an 11-bit significand)
     assert ((out - want).abs() <= 2.0 ** -9 * want.abs().amax(-1, keepdim=True)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,dim", [(1, 64), (9, 64), (5, 128), (8, 128), (3, 256), (1, 256)])
+@pytest.mark.parametrize("block", [16, 64])
+def test_append_of_single_tokens_of_several_heads(dtype, heads, dim, block):
+    b = Both(20, block, heads, dim, dtype, 1, heads + dim + block)
+    g, filled = b.g, {}
+    for step in range(block + 3):                            # growing and shrinking values: scales that change and that stay
+        ids = g.permutation(20)[:18].tolist()
+        slots = [i * block + filled.get(i, 0) if filled.get(i, 0) < block and g.random() < 0.9 else -1 for i in ids]
+        x = rows(g, 18, heads, dim, dtype, float(g.choice([0.3, 1, 3])) * (1 + step / 20))
+        if step == 5:
+            x[3] = 0
+        b.append(x, rows(g, 18, heads, dim, dtype, 2.0 ** -step), slots)
+        for s in slots:
+            if s >= 0:
+                filled[s // block] = s % block + 1
+        b.same(filled)
+
+
+def test_append_of_a_run_that_begins_at_a_windows_last_row():
+    """A run whose first row ends a window of rows is no single token."""
+    b = Both(40, 16, 2, 128, "f16", 40, 33)
+    x, y = rows(b.g, 40, 2, 128, "f16"), rows(b.g, 40, 2, 128, "f16")
+    slots = [16 * i for i in range(15)] + list(range(16 * 20, 16 * 20 + 16)) + [16 * 30 + 3, 16 * 31 + 5] + [16 * 32 + i for i in range(7)]
+    b.append(x, y, slots)
+    b.same({**{i: 1 for i in range(15)}, 20: 16, 32: 7})
