@@ -162,6 +162,9 @@ tsq_status tsq_cache_gather(const tsq_cache *cache, const tsq_cache_memory *memo
  *   d_lse            f32 [tokens][q_heads] or NULL
  *   d_ws             tsq_cache_attend_workspace_bytes() bytes for the same numbers, 256-byte aligned; needs
  *                    no reset; one call at a time.  NULL where the size is 0
+ * A call may cover a part of a step's requests (d_table, d_starts and d_lengths from the first of them on;
+ * rows stay those of the whole step): requests of one token and long ones of the same step are best given
+ * in calls of their own, since the largest request of a call decides which kernel runs.
  * Products are exact in binary32 sums: codes are whole numbers, queries keep their bits; weights of the
  * values are rounded to 11 bits; softmax statistics and all sums are binary32.
  */

@@ -180,6 +180,10 @@ __device__ __forceinline__ uint64_t row_id(const AttendArgs &a, const Place &p, 
 //   S^T tile t (16 tokens x 16 rows): row 4g + i is token 16g + 4t + i, so that a lane's 16 scores (t, i) are the
 //   16 tokens of its group, in the order of its 16 bytes of a value's row; its row of the softmax is m.
 //   Keys: operand row m is token 16 (m / 4) + 4t + m % 4; the lane's k indices are the elements 64f + 16g .. + 15.
+//
+// The cache's bytes bound it: 64 requests of 1024 to 4096 tokens on 40 heads of 128, blocks of 16, are 1.79 GB and
+// 317 us, 5.6 TB/s.  The same 2 KB pieces read and thrown away take 300 us, 283 with the longest request first; a
+// stream of reads reaches 7.0 TB/s.  One query of 64 heads on 8 over 131072 tokens: 269 MB, 46 us and 4 for the join.
 template <int D, bool BF16, int SETS>
 __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) void k_attend_few(AttendArgs a) {
     constexpr int F = D / 64;                            // 64-element pieces of a head
@@ -375,9 +379,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
     }
 }
 
-// Many rows: 128 of a kv head's in a workgroup of four waves, 32 each.  A tile of 64 tokens goes through registers
-// into LDS, as halves, once for all rows: the waves' threads convert a share of it each while the other buffer is
-// worked on.
+// Many rows: 32 of a kv head's a wave, eight waves a workgroup (four, where a request has no more than 128 rows, and for
+// heads of 256, whose sums and queries take the registers of two).  A tile of 128 tokens (64) goes through registers
+// into LDS, as halves, once for all rows: the threads convert a share of it each, and one barrier a tile is all that
+// they wait for.  A piece from LDS feeds one product of 32 x 32 x 16, so LDS is read at about half its rate.
+//
+// Instruction issue bounds it: a wave's 64 tokens by 32 rows of 128 are 1024 cycles of products, and some 1300 of
+// exponentials, maxima, sums, conversions and addresses, which run beside them only as far as two waves of a SIMD
+// complement each other (a product keeps 12 cycles of issue from the other wave).  8192 queries over as many tokens,
+// causal, 64 heads on 8 of 128: 1.10 PFLOP in 1.12 ms, 0.98 PFLOP/s; a large library product of halves reaches 1.2.
+// Heads of 64 have the exponentials of 128 for half the products: 0.26 PFLOP/s on 12 heads of 4096 tokens.
 // Lane (n = lane % 32, hi = lane / 32).  S^T in two 32 x 32 pieces: register i of a piece is token
 // 8 (i / 4) + 4 hi + i % 4, row n.  P^T as an operand of 16 tokens wants eight of them from each half of the wave:
 // registers 8u .. 8u + 7 are tokens 4 hi + (0..3) and 8 + 4 hi + (0..3) of the 16, so the values' rows in LDS hold

@@ -88,7 +88,8 @@ __device__ __forceinline__ Wants wants_of(const ScheduleArgs &a, uint32_t r, uin
 // requests bring at most kFewNew tokens each, a request's thread writes them; otherwise a token's request is
 // searched for in the sums.
 //
-// Latency is all there is: 512 requests of a token each take 12.6 KB.
+// Latency is all there is: 512 requests, most with a token, some done, are 12.6 KB and 5.5 us; 32 prompts of 82000
+// tokens together 0.8 MB and 8.4 us.  A call in a row with others costs 3.4 us whatever it does.
 __global__ __launch_bounds__(kScheduleThreads) void k_schedule(ScheduleArgs a) {
     __shared__ uint32_t first_row[kMaxScheduleRequests + 1], first_new[kMaxScheduleRequests + 1], first_back[kMaxScheduleRequests + 1];
     __shared__ uint32_t wave_sum[kScheduleThreads / 64][4];
@@ -186,7 +187,9 @@ __global__ __launch_bounds__(kScheduleThreads) void k_schedule(ScheduleArgs a) {
 }
 
 // Norm and rotation.  A lane holds 16 elements of a head in two pieces of 8, chosen so that the pairs that turn
-// together are the lane's own: D / 16 lanes a head, 1024 / D heads a wave at a time.
+// together are the lane's own: D / 16 lanes a head, 1024 / D heads a wave.  The sum of squares, the product with the
+// weight and the rotation stay in registers, in binary32; memory is read and written once, and bounds it: 8192 rows of
+// 72 heads of 128 are 306 MB and 54 us, 5.7 TB/s where a copy reaches 6.2.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void k_norm_rotate(NormRotateArgs a, uint32_t passes, uint32_t waves_each) {
     constexpr int LPH = D / 16, HEADS = 64 / LPH;
@@ -211,8 +214,8 @@ __global__ __launch_bounds__(256) void k_norm_rotate(NormRotateArgs a, uint32_t 
         const float one = (uint32_t)position < a.angle_rows ? 1.0f : __builtin_nanf("");
         for (int i = 0; i < 8; ++i) { c[i] = one; s[i] = one - one; }
     }
-    const uint32_t heads = a.q_heads + a.kv_heads, first_pass = wave % waves_each;
-    for (uint32_t pass = first_pass; pass < passes; pass += waves_each) {
+    const uint32_t heads = a.q_heads + a.kv_heads;
+    for (uint32_t pass = wave % waves_each; pass < passes; pass += waves_each) {
         const uint32_t h = pass * HEADS + sub;
         const bool is_q = h < a.q_heads, here = h < heads;
         const uint64_t in_at = is_q ? (uint64_t)token * a.q_stride + (uint64_t)h * D : (uint64_t)token * a.k_stride + (uint64_t)(h - a.q_heads) * D;
@@ -489,7 +492,7 @@ template <int N> __device__ __forceinline__ uint32_t group_max(uint32_t v) {
 
 // A single token, as every request brings one in a step of decoding: D / 8 lanes a head, 512 / D heads at once, since
 // one token's head is too little for a wave and a step's time is its waits, one after the other.  512 tokens on 40
-// heads of 128: 30 us a (token, head) a wave, see k_append for what it is now.
+// heads of 128: 22 us, with one head a wave 30.
 template <int D, bool BF16, int WHICH>
 __device__ __forceinline__ void store_single(const uint16_t *x, int8_t *codes, float *scale, uint32_t B, uint32_t o, uint32_t h0, uint32_t heads) {
     constexpr uint32_t LPT = D / 8;
@@ -545,6 +548,10 @@ __device__ __forceinline__ void store_single(const uint16_t *x, int8_t *codes, f
 
 // A window of rows for waves_each waves: each finds the runs that begin in it, one row a lane, and takes its share of
 // (run, head, keys or values).
+//
+// Of prompts, memory is the bound: 7200 rows of 32 heads of 128 are 177 MB and 29 us.  Of single tokens it is what the
+// layout makes of them: the keys of a (token, head) are 128 bytes side by side, the values 128 bytes 16 apart, so that
+// 16 lines are written in part; 512 tokens on 40 heads are 16 MB as they come and 22 us.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256, D == 256 ? 3 : 4) void k_append(AppendArgs a) {
     const uint32_t lane = threadIdx.x & 63;
@@ -621,8 +628,12 @@ __global__ __launch_bounds__(256, D == 256 ? 3 : 4) void k_append(AppendArgs a) 
     }
 }
 
-// Sixteen rows of the output for waves_each waves: row i's request, position and block by lane i, then the rows
-// that lie in one block together, a share of the heads each wave.
+// Sixteen rows of the output for waves_each waves: row i's request, position and block by lane i, then a share of the
+// heads each wave.
+//
+// Memory is the bound: 92000 rows of 8 heads of 128 from blocks of 64 tokens are 565 MB and 123 us, 4.6 TB/s where a
+// copy reaches 6.2; the values' 4-byte stores and the scattered blocks keep it from that.  A request of 2048 rows of
+// 32 heads, from blocks of 16, is 50 MB and 8 to 10 us.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void k_gather(GatherArgs a) {
     const uint32_t lane = threadIdx.x & 63, B = a.block_tokens;
@@ -778,7 +789,9 @@ int launch_schedule(const ScheduleArgs &a, void *stream) {
 int launch_norm_rotate(const CacheShape &s, const NormRotateArgs &a, void *stream) {
     const uint32_t at_once = 1024 / s.head_dim, passes = (a.q_heads + a.kv_heads + at_once - 1) / at_once;
     uint32_t grid;
-    const uint32_t each = passes;
+    // three passes a wave load the angles once for them (8192 rows of 72 heads of 128: 54 us against 61, nine passes a
+    // wave 64; 2048 rows 13.6 against 16.0); a pass a wave while there are fewer waves than the device holds at once
+    const uint32_t each = (uint64_t)a.tokens * passes <= 4096 ? passes : (passes + 2) / 3;
     if (int e = workgroups((uint64_t)a.tokens * each, &grid)) return e;
     by_shape(s, [&](auto d, auto bf16) { k_norm_rotate<d(), bf16()><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, passes, each); });
     return (int)hipGetLastError();
