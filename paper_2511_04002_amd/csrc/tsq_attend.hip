@@ -58,6 +58,17 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
         p.r = x / a.tiles_each;
         p.tile = x % a.tiles_each;
         next = a.tiles_each;
+        if (a.by_length) {
+            // the longest request first: p.r counts from the shortest here; each lane ranks one request
+            const uint32_t lane = threadIdx.x & 63;
+            const int32_t mine = lane < a.requests ? a.lengths[lane] : 0;
+            uint32_t below = 0;
+            for (uint32_t j = 0; j < a.requests; ++j) {
+                const int32_t other = __builtin_amdgcn_readlane(mine, (int)j);
+                below += other < mine || (other == mine && j < lane) ? 1 : 0;
+            }
+            p.r = (uint32_t)__builtin_ctzll(__ballot(lane < a.requests && below == p.r));
+        }
     } else {
         // request r begins at tile first(r) = rows before it / ROWS + r, which leaves it at least as many as it needs
         uint32_t lo = 0, hi = a.requests;
@@ -182,7 +193,7 @@ __device__ __forceinline__ uint64_t row_id(const AttendArgs &a, const Place &p, 
 //   Keys: operand row m is token 16 (m / 4) + 4t + m % 4; the lane's k indices are the elements 64f + 16g .. + 15.
 //
 // The cache's bytes bound it: 64 requests of 1024 to 4096 tokens on 40 heads of 128, blocks of 16, are 1.79 GB and
-// 317 us, 5.6 TB/s.  The same 2 KB pieces read and thrown away take 300 us, 283 with the longest request first; a
+// 306 us, 5.8 TB/s.  The same 2 KB pieces read and thrown away take 300 us, 283 with the longest request first; a
 // stream of reads reaches 7.0 TB/s.  One query of 64 heads on 8 over 131072 tokens: 269 MB, 46 us and 4 for the join.
 template <int D, bool BF16, int SETS>
 __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) void k_attend_few(AttendArgs a) {
@@ -790,6 +801,11 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
     // (pieces of whole tiles may be fewer)
     l.splits = (uint32_t)((reach + l.chunk - 1) / l.chunk);
     if (l.splits == 0) l.splits = 1;
+    // Requests of several lengths in many more workgroups than run at once: the longest begin first, so that the last
+    // ones to end are short (64 requests of 1024 to 4096 tokens on 40 heads, 2560 workgroups: 306 us against 318; with
+    // little more than one round the ranking costs more than it brings: 20 requests of 250 to 1000 tokens on 32 heads 29
+    // against 25).  A wave ranks 64 requests.
+    l.by_length = l.tiles_each && requests > 1 && requests <= 64 && units * l.splits >= 4 * slots;
     return l;
 }
 

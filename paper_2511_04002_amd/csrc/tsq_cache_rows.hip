@@ -88,8 +88,8 @@ __device__ __forceinline__ Wants wants_of(const ScheduleArgs &a, uint32_t r, uin
 // requests bring at most kFewNew tokens each, a request's thread writes them; otherwise a token's request is
 // searched for in the sums.
 //
-// Latency is all there is: 512 requests, most with a token, some done, are 12.6 KB and 5.5 us; 32 prompts of 82000
-// tokens together 0.8 MB and 8.4 us.  A call in a row with others costs 3.4 us whatever it does.
+// Latency is all there is: 512 requests, most with a token, some done, are 12.6 KB and 5.5 us; 32 prompts of 96000
+// tokens together 0.8 MB and 8.5 us.  A call in a row with others costs 3.4 us whatever it does.
 __global__ __launch_bounds__(kScheduleThreads) void k_schedule(ScheduleArgs a) {
     __shared__ uint32_t first_row[kMaxScheduleRequests + 1], first_new[kMaxScheduleRequests + 1], first_back[kMaxScheduleRequests + 1];
     __shared__ uint32_t wave_sum[kScheduleThreads / 64][4];
@@ -549,7 +549,7 @@ __device__ __forceinline__ void store_single(const uint16_t *x, int8_t *codes, f
 // A window of rows for waves_each waves: each finds the runs that begin in it, one row a lane, and takes its share of
 // (run, head, keys or values).
 //
-// Of prompts, memory is the bound: 7200 rows of 32 heads of 128 are 177 MB and 29 us.  Of single tokens it is what the
+// Of prompts, memory is the bound: 5600 rows of 32 heads of 128 are 138 MB and 29 us.  Of single tokens it is what the
 // layout makes of them: the keys of a (token, head) are 128 bytes side by side, the values 128 bytes 16 apart, so that
 // 16 lines are written in part; 512 tokens on 40 heads are 16 MB as they come and 22 us.
 template <int D, bool BF16>

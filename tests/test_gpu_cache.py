@@ -687,3 +687,21 @@ def test_append_of_a_run_that_begins_at_a_windows_last_row():
     slots = [16 * i for i in range(15)] + list(range(16 * 20, 16 * 20 + 16)) + [16 * 30 + 3, 16 * 31 + 5] + [16 * 32 + i for i in range(7)]
     b.append(x, y, slots)
     b.same({**{i: 1 for i in range(15)}, 20: 16, 32: 7})
+
+
+@pytest.mark.parametrize("requests", [2, 33, 64, 65])
+def test_attend_of_many_heads_and_lengths_in_more_workgroups_than_run_at_once(requests):
+    """Enough workgroups that they go by the requests' lengths (up to 64 requests), equal and zero lengths among them."""
+    heads = min(1024, 4000 // requests)
+    b = Both(3 * requests, 16, heads, 64, "f16", 4, requests, q_heads=heads)
+    lengths = b.g.integers(0, 45, requests)
+    lengths[0] = lengths[-1] = 44
+    table = b.g.integers(0, 3 * requests, (requests, 4)).astype(np.int32)
+    starts = dev(np.arange(requests + 1, dtype=np.int32))
+    q = rows(b.g, requests, heads, 64, "f16")
+    got = host(b.c.attend(b.m, q, dev(table), starts, dev(lengths.astype(np.int32)), 1, 4000))
+    for h in (0, heads // 2, heads - 1):
+        want, _, spread = O.attend(b.k[:, h:h + 1], b.v[:, h:h + 1], b.ks[:, h:h + 1], b.vs[:, h:h + 1], 16, 4, table, np.arange(requests + 1),
+                                   lengths.astype(np.int32), host(q)[:, h:h + 1], 0.125, True, 0)
+        bound = HALF_ULP["f16"] * np.abs(want) + (2.0 ** -11 + 2.0 ** -14) * spread + TINY["f16"] + 2.0 ** -32 * 45 * 127 * float(b.vs.max())
+        assert (np.abs(got[:, h:h + 1] - want) <= bound).all(), h
