@@ -148,6 +148,8 @@ class Cache:
         import torch
         if dtype not in tsq._DTYPES:
             _refuse("dtype is 'f16' or 'bf16'")
+        if min(blocks, block_tokens, q_heads, kv_heads, head_dim, max_blocks) < 0:
+            _refuse("a cache's numbers are not negative")
         self.kind = torch.float16 if dtype == "f16" else torch.bfloat16
         self.int32, self.int64, self.float32 = torch.int32, torch.int64, torch.float32
         self.blocks, self.block_tokens, self.q_heads, self.kv_heads = blocks, block_tokens, q_heads, kv_heads
@@ -327,6 +329,8 @@ class Cache:
             if not (lse.dtype is self.float32 and lse.is_cuda and lse.is_contiguous() and lse.numel() == tokens * self.q_heads):
                 _refuse("lse is float32 [tokens, q_heads] on the GPU, contiguous")
             lp = lse.data_ptr()
+        if max_new < 0 or max_length < 0 or window < 0:
+            _refuse("max_new, max_length and window are not negative")
         L, wp = self._lib, None
         # (256 tokens are never cut, and then there is no workspace)
         need = 0 if max_length <= 256 else L.tsq_cache_attend_workspace_bytes(self.handle, n, tokens, max_new, max_length, window)

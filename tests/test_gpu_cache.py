@@ -705,3 +705,52 @@ def test_attend_of_many_heads_and_lengths_in_more_workgroups_than_run_at_once(re
                                    lengths.astype(np.int32), host(q)[:, h:h + 1], 0.125, True, 0)
         bound = HALF_ULP["f16"] * np.abs(want) + (2.0 ** -11 + 2.0 ** -14) * spread + TINY["f16"] + 2.0 ** -32 * 45 * 127 * float(b.vs.max())
         assert (np.abs(got[:, h:h + 1] - want) <= bound).all(), h
+
+
+def test_calls_of_no_tokens_do_nothing():
+    b = Both(4, 16, 2, 128, "f16", 2, 40, q_heads=4)
+    none, starts, lengths, table = dev(np.zeros(0, np.int32)), dev(np.zeros(3, np.int32)), dev(np.array([5, 0], np.int32)), dev(np.zeros((2, 2), np.int32))
+    k, v = (torch.empty((0, 2, 128), dtype=torch.float16, device="cuda") for _ in range(2))
+    b.c.append(b.m, k, v, none)
+    b.c.gather(b.m, table, starts, lengths, k, v)
+    q = torch.empty((0, 4, 128), dtype=torch.float16, device="cuda")
+    assert b.c.attend(b.m, q, table, starts, lengths, 0, 5).shape == (0, 4, 128)
+    # a step in which every request is done, or brings nothing
+    schedule_both(np.array([-1, 0], np.int32), np.array([20, 3], np.int32), np.array([[1, 2], [3, -1]], np.int32), np.array([0, 9, 9, 9], np.int32),
+                  np.array([4, 5], np.int64), 16, 2, 0)
+
+
+@pytest.mark.parametrize("name", ["max_new", "max_length", "window"])
+def test_attend_refuses_negative_numbers(name):
+    b = Both(4, 16, 1, 64, "f16", 2, 41)
+    args = dict(max_new=1, max_length=5, window=0)
+    args[name] = -1
+    q, starts, lengths, table = rows(b.g, 1, 1, 64, "f16"), dev(np.array([0, 1], np.int32)), dev(np.array([5], np.int32)), dev(np.zeros((1, 2), np.int32))
+    with pytest.raises(ValueError):
+        b.c.attend(b.m, q, table, starts, lengths, **args)
+
+
+def test_a_long_cache_whose_bytes_pass_32_bits():
+    """5 GB of keys: blocks past the first 4 GB are read, written and gathered where they are."""
+    c = cachelib.Cache(5 * 2 ** 30 // (128 * 256 * 8), 128, 8, 8, 256, "bf16", 8)
+    m = c.new_memory()
+    last = c.blocks - 1
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    k, v, q = (torch.randn((300, 8, 256), device="cuda", generator=g).bfloat16() for _ in range(3))
+    ids = [last, last - 5, 3]
+    table = torch.tensor([ids + [0] * 5], dtype=torch.int32, device="cuda")
+    slots = torch.tensor([ids[t // 128] * 128 + t % 128 for t in range(300)], dtype=torch.int32, device="cuda")
+    c.append(m, k, v, slots)
+    starts, lengths = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 300], [300]))
+    kk, vv = torch.empty_like(k), torch.empty_like(v)
+    c.gather(m, table, starts, lengths, kk, vv)
+    for x, y in ((k, kk), (v, vv)):
+        assert (x.float() - y.float()).abs().max() <= x.abs().float().max() * (0.5 / 127 + 2.0 ** -8)
+    out = c.attend(m, q, table, starts, lengths, 300, 300)
+    few = cachelib.Cache(4, 128, 8, 8, 256, "bf16", 8)
+    small = few.new_memory()
+    few.append(small, k, v, torch.arange(300, dtype=torch.int32, device="cuda"))
+    assert torch.equal(out, few.attend(small, q, torch.arange(8, dtype=torch.int32, device="cuda")[None], starts, lengths, 300, 300))
+    one = c.attend(m, q[-1:].contiguous(), table, torch.tensor([0, 1], dtype=torch.int32, device="cuda"), lengths, 1, 300)
+    assert (one - out[-1:]).abs().max() <= 2.0 ** -6 * out[-1:].abs().max()
