@@ -399,7 +399,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
 // exponentials, maxima, sums, conversions and addresses, which run beside them only as far as two waves of a SIMD
 // complement each other (a product keeps 12 cycles of issue from the other wave).  8192 queries over as many tokens,
 // causal, 64 heads on 8 of 128: 1.10 PFLOP in 1.12 ms, 0.98 PFLOP/s; a large library product of halves reaches 1.2.
-// Heads of 64 have the exponentials of 128 for half the products: 0.26 PFLOP/s on 12 heads of 4096 tokens.
+// Heads of 64 have the exponentials of 128 for half the products: 0.57 PFLOP/s (two requests of 8000 tokens, 20 heads).
+// The maxima could be left out of nearly all tiles, since the sums of the weights show when the reference is too low;
+// the second pass that this needs costs more registers than there are (spilled, 1.44 ms).
 // Lane (n = lane % 32, hi = lane / 32).  S^T in two 32 x 32 pieces: register i of a piece is token
 // 8 (i / 4) + 4 hi + i % 4, row n.  P^T as an operand of 16 tokens wants eight of them from each half of the wave:
 // registers 8u .. 8u + 7 are tokens 4 hi + (0..3) and 8 + 4 hi + (0..3) of the 16, so the values' rows in LDS hold
@@ -410,6 +412,18 @@ struct ManyTile {                                        // rows padded by 16 by
     _Float16 v[D][TOKENS + 8];
     float factor[TOKENS / 16], log_v[TOKENS / 16], back_v[TOKENS / 16];      // of each 16 tokens
 };
+
+// How a block's N loads from LDS and N products are to be issued: four loads, then one behind each product.
+template <int N, int GROUP> __device__ __forceinline__ void loads_among_products() {
+    constexpr int kLoad = 0x100, kProduct = 0x8;
+    __builtin_amdgcn_sched_group_barrier(kLoad, 4, GROUP);
+#pragma unroll
+    for (int i = 0; i < N - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kProduct, 1, GROUP);
+        __builtin_amdgcn_sched_group_barrier(kLoad, 1, GROUP);
+    }
+    __builtin_amdgcn_sched_group_barrier(kProduct, 4, GROUP);
+}
 
 template <int D, bool BF16, int WAVES, int TOKENS>
 __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a) {
@@ -532,32 +546,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
                     for (int e = 0; e < D / 16; ++e)
                         s[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(&t.k[part + 32 * c + n][16 * e + 8 * hi]), q[e], s[c], 0, 0, 0);
                 }
-                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
+                loads_among_products<2 * D / 16, 0>();
                 __builtin_amdgcn_s_setprio(0);
                 const bool whole = __ballot(u0 < from || u0 + 64 > to) == 0;
                 const float4_t ks = *reinterpret_cast<const float4_t *>(t.factor + part / 16), lv = *reinterpret_cast<const float4_t *>(t.log_v + part / 16);
@@ -621,32 +610,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
                         acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t *>(&t.v[32 * d + n][part + 16 * u + 8 * hi]), pw[u], acc[d], 0, 0, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(0x8, 4, 1);
+                loads_among_products<4 * D / 32, 1>();
                 __builtin_amdgcn_s_setprio(0);
             }
             if (t0 + TOKENS < reach.end) put(buffer[at ^ 1]);
