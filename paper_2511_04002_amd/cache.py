@@ -126,11 +126,21 @@ class Memory:
 
 
 class Schedule:
-    """What one step's schedule is written to (see tsq_cache_schedule)."""
+    """What one step's schedule is written to (see tsq_cache_schedule): made by Cache.new_schedule, and kept by a program as it
+    keeps the cache's memory.  Its tensors are looked at once, here, and stay what they are."""
 
     def __init__(self, lengths, counters, starts, positions, slots, status):
-        self.lengths, self.counters, self.starts = lengths, counters, starts
-        self.positions, self.slots, self.status = positions, slots, status
+        import torch
+        n, capacity = lengths.numel(), slots.numel()
+        for x, kind, size in ((lengths, torch.int32, n), (counters, torch.int64, 2), (starts, torch.int32, n + 1), (positions, torch.int32, capacity),
+                              (slots, torch.int32, capacity), (status, torch.int32, 1)):
+            if not (x.is_cuda and x.is_contiguous() and x.dtype is kind and x.numel() == size):
+                _refuse("a schedule's tensors are those of Cache.new_schedule")
+        self.__dict__.update(lengths=lengths, counters=counters, starts=starts, positions=positions, slots=slots, status=status, requests=n,
+                             capacity=capacity, pointers=tuple(x.data_ptr() for x in (lengths, counters, starts, positions, slots, status)))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a schedule's tensors are not replaced")
 
     def check(self) -> None:
         """Raises TsqError if the step could not be taken.  Synchronizes."""
@@ -253,15 +263,16 @@ class Cache:
         """Block tables, slots and positions of a step: new [requests] int32 new tokens of each request (-1: done),
         lengths [requests] int32 what it has.  table and ring are updated; the rest is written to `out`
         (from new_schedule(requests, most new tokens of a step))."""
-        n, i, capacity = new.numel(), self._ints, out.slots.numel()
-        for x in (counters, out.counters):
-            if not (x.dtype is self.int64 and x.is_cuda and x.is_contiguous() and x.numel() == 2):
-                _refuse("counters is int64 (2,) on the GPU, contiguous")
-        status = self._lib.tsq_cache_schedule(
-            self.handle, n, i(new, n, "new"), i(lengths, n, "lengths"), i(table, n * self.max_blocks, "table"),
-            i(ring, self.blocks, "ring"), counters.data_ptr(), capacity, i(out.lengths, n, "out.lengths"),
-            out.counters.data_ptr(), i(out.starts, n + 1, "out.starts"), i(out.positions, capacity, "out.positions"),
-            i(out.slots, capacity, "out.slots"), i(out.status, 1, "out.status"), self._stream())
+        n, i32 = new.numel(), self.int32
+        if not (new.dtype is i32 and lengths.dtype is i32 and table.dtype is i32 and ring.dtype is i32 and counters.dtype is self.int64 and
+                new.is_cuda and lengths.is_cuda and table.is_cuda and ring.is_cuda and counters.is_cuda and
+                new.is_contiguous() and lengths.is_contiguous() and table.is_contiguous() and ring.is_contiguous() and counters.is_contiguous() and
+                lengths.numel() == n and table.numel() == n * self.max_blocks and ring.numel() == self.blocks and counters.numel() == 2 and
+                out.requests == n):
+            _refuse("on the GPU and contiguous: new, lengths int32 [%d], table int32 [%d, %d], ring int32 [%d], counters int64 [2], and a "
+                    "schedule of as many requests" % (n, n, self.max_blocks, self.blocks))
+        status = self._lib.tsq_cache_schedule(self.handle, n, new.data_ptr(), lengths.data_ptr(), table.data_ptr(), ring.data_ptr(),
+                                              counters.data_ptr(), out.capacity, *out.pointers, self._stream())
         if status:
             raise TsqError(status, "tsq_cache_schedule")
         return out

@@ -754,3 +754,14 @@ def test_a_long_cache_whose_bytes_pass_32_bits():
     assert torch.equal(out, few.attend(small, q, torch.arange(8, dtype=torch.int32, device="cuda")[None], starts, lengths, 300, 300))
     one = c.attend(m, q[-1:].contiguous(), table, torch.tensor([0, 1], dtype=torch.int32, device="cuda"), lengths, 1, 300)
     assert (one - out[-1:]).abs().max() <= 2.0 ** -6 * out[-1:].abs().max()
+
+
+def test_a_schedules_tensors_are_not_replaced():
+    c = cachelib.Cache(4, 16, 1, 1, 64, "f16", 2)
+    s = c.new_schedule(2, 5)
+    with pytest.raises(AttributeError):
+        s.lengths = torch.zeros(2, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        cachelib.Schedule(s.lengths, s.counters, s.starts[:2], s.positions, s.slots, s.status)
+    with pytest.raises(ValueError):
+        cachelib.Schedule(s.lengths.long(), s.counters, s.starts, s.positions, s.slots, s.status)
