@@ -184,6 +184,16 @@ __device__ __forceinline__ uint64_t row_id(const AttendArgs &a, const Place &p, 
     return (uint64_t)(p.begin + row / a.group) * a.q_heads + p.h * a.group + row % a.group;
 }
 
+// A piece that lies behind a tile's reach: no row sees anything, and that is all that the join has to know.
+template <int ROWS>
+__device__ __forceinline__ void nothing_seen(const AttendArgs &a, const Place &p, uint32_t tile, int head_dim) {
+    const uint32_t row = tile * ROWS + threadIdx.x;
+    if (threadIdx.x >= ROWS || row >= p.n * a.group) return;
+    float *st = a.parts + a.part_rows * a.splits * head_dim + (row_id(a, p, row) * a.splits + p.split) * 2;
+    st[0] = kNone;
+    st[1] = 0.0f;
+}
+
 // Few rows: 16 of a kv head's, or 32 (SETS = 2, which share the codes once they are halves).  Each of four waves takes
 // every fourth tile of 64 tokens straight from memory to registers and keeps a softmax of its own; they meet in LDS at
 // the end.
@@ -207,6 +217,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
     const uint32_t B = 1u << a.block_log2;
     for (uint32_t tile = p.tile;; ++tile) {
         const uint32_t rows = p.n * a.group;
+        const Reach reach = reach_of<ROWS>(a, p, tile);
+        const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
+        if (a.splits > 1 && reach.begin >= reach.end) {
+            nothing_seen<ROWS>(a, p, tile, D);
+            if (done) return;
+            continue;
+        }
         half8_t q[SETS][F][2];
         float back[SETS];
         uint32_t from[SETS], to[SETS];
@@ -236,7 +253,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
                 for (int e = 0; e < 2; ++e) q[c][f][e] = query_piece<BF16>(w[f][e], factor);
             row_sees(a, p, row, from[c], to[c]);
         }
-        const Reach reach = reach_of<ROWS>(a, p, tile);
 
         float4_t acc[SETS][D / 16];
         float ref[SETS], weight[SETS];
@@ -385,7 +401,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
                 }
             }
         }
-        if (!p.last || (uint64_t)(tile + 1) * ROWS >= rows) return;
+        if (done) return;
         __syncthreads();
     }
 }
@@ -437,6 +453,13 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
     const uint32_t B = 1u << a.block_log2;
     for (uint32_t tile = p.tile;; ++tile) {
         const uint32_t row = tile * ROWS + wave * 32 + n, rows = p.n * a.group;
+        const Reach reach = reach_of<ROWS>(a, p, tile);
+        const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
+        if (a.splits > 1 && reach.begin >= reach.end) {
+            nothing_seen<ROWS>(a, p, tile, D);
+            if (done) return;
+            continue;
+        }
         half8_t q[D / 16];
         float back = 1.0f;
         {
@@ -462,7 +485,6 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
         }
         uint32_t from, to;
         row_sees(a, p, row, from, to);
-        const Reach reach = reach_of<ROWS>(a, p, tile);
 
         float16_t acc[D / 32];
 #pragma unroll
@@ -645,7 +667,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
                 }
             }
         }
-        if (!p.last || (uint64_t)(tile + 1) * ROWS >= rows) return;
+        if (done) return;
     }
 }
 
@@ -696,7 +718,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
     float total = 0.0f;
     float4_t y = {0, 0, 0, 0};
     auto add = [&](float2_t t, float4_t x) {
-        // (of a piece that the row sees nothing of, the sums are 0)
+        if (t[1] == 0.0f) return;                        // nothing seen, and perhaps no sums written (NaN is not 0)
         const float f = pow2(t[0] - top);
         total = __builtin_fmaf(t[1], f, total);
         for (int e = 0; e < 4; ++e) y[e] = __builtin_fmaf(x[e], f, y[e]);
@@ -759,6 +781,10 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
     const uint64_t units = (uint64_t)l.tiles * s.kv_heads, longest = reach <= 256 ? 1 : (reach + least - 1) / least;
     uint64_t splits = slots / (units ? units : 1);
     if (splits > longest) splits = longest;
+    // One request of a batch may be far longer than the others: a piece of k_attend_few has no more than 8192 tokens (63
+    // requests of 2000 tokens and one of 131072, 64 heads on 8: 220 us, and 737 in one piece; 64 requests of 32768 each
+    // 739 and 712).
+    if (l.rows < 128 && splits < (reach + 8191) / 8192) splits = (reach + 8191) / 8192;
     if (splits == 0) splits = 1;
     l.chunk = (uint32_t)(((reach + splits - 1) / splits + 127) / 128 * 128);
     if (l.chunk == 0) l.chunk = 128;

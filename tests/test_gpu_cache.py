@@ -765,3 +765,12 @@ def test_a_schedules_tensors_are_not_replaced():
         cachelib.Schedule(s.lengths, s.counters, s.starts[:2], s.positions, s.slots, s.status)
     with pytest.raises(ValueError):
         cachelib.Schedule(s.lengths.long(), s.counters, s.starts, s.positions, s.slots, s.status)
+
+
+@pytest.mark.parametrize("heads", [(2, 2, 64), (8, 1, 128), (4, 1, 256)])
+def test_attend_one_request_far_longer_than_the_others(heads):
+    hq, hk, dim = heads
+    b = Both(700, 16, hk, dim, "f16", 600, 50, q_heads=hq)
+    attend_both(b, hq, [1, 1, 0, 1], [30, 9001, 7, 0])
+    attend_both(b, hq, [3, 9, 2], [30, 8500, 700], window=300)
+    attend_both(b, hq, [40, 41], [40, 8400])
