@@ -97,7 +97,8 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
     p.beyond = (uint64_t)p.length > most;
     p.seen = p.beyond ? (uint32_t)most : (uint32_t)p.length;
     p.last = p.tile + 1 == next;
-    return (uint64_t)p.tile * ROWS < (uint64_t)p.n * a.group;
+    const uint32_t rows = p.n * a.group;
+    return p.tile * (uint64_t)ROWS < rows && rows >= a.rows_from && rows <= a.rows_to;
 }
 
 // Tokens that any row of a tile sees, the part of them that a split has, and what a row sees.
@@ -750,6 +751,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
 
 }  // namespace
 
+// Rows of a kv head up to which a request is k_attend_few's.
+uint32_t few_rows(const CacheShape &s) { return s.head_dim == 256 ? 32 : 64; }
+
 // Which kernel, how many rows a workgroup, and into how many pieces the cache's length is cut.
 //
 // Rows: a request with at most 64 rows of a kv head goes to k_attend_few, whose time is the cache's bytes as long as
@@ -759,7 +763,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
 // costs its start and its share of the join.
 AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length, uint32_t window) {
     AttendLaunch l;
-    const uint64_t group = s.q_heads / s.kv_heads, most = max_new * group;
+    l.few_tiles = 0;
+    const uint64_t group = s.q_heads / s.kv_heads, most = max_new * group, few = few_rows(s);
     auto tile = [&](uint32_t rows) {
         l.rows = rows;
         const uint64_t each = (most + rows - 1) / rows, packed = tokens * group / rows + requests;
@@ -769,12 +774,18 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
         l.tiles = (uint32_t)(l.tiles_each ? (uint64_t)l.tiles_each * requests : packed);
     };
     uint64_t slots;
-    if (most <= (s.head_dim == 256 ? 32 : 64)) {
+    if (most <= few) {
         tile(most <= 16 || s.head_dim == 256 ? 16 : 32);
         slots = s.head_dim == 256 ? 256 : s.head_dim == 128 || l.rows == 32 ? 512 : 768;
     } else {
         tile(s.head_dim == 256 || most <= 128 ? 128 : 256);
         slots = s.head_dim == 256 || l.rows == 256 ? 256 : 512;
+        // Single tokens beside prompts: where the requests have a quarter of the longest one's rows on average, or less, a
+        // launch of its own takes those of few rows, and this one the others (one token each of 63 requests of 2000 tokens
+        // and a prompt of 512, 64 heads on 8: 99 us, and 174 all by k_attend_many; 15 of 8000 and 2048, 32 on 8: 144 and
+        // 262; 200 of 500 and 1000, 32 on 32: 279 and 508; 3 of 300 and 200, 32 on 8: 21 and 20).  The launches follow one
+        // another, and both are cut by the pieces of this one: two calls by the caller take 86, 148, 208 and 27 us.
+        if (requests > 1 && tokens * group * 4 <= requests * most) l.few_tiles = (uint32_t)(few / (s.head_dim == 256 ? 16 : 32)) * requests;
     }
     uint64_t reach = max_length, least = l.rows >= 128 ? 128 : 256;     // a tile of k_attend_many, one of each wave of k_attend_few
     if (window && reach > (uint64_t)window + max_new) reach = (uint64_t)window + max_new;
@@ -784,7 +795,7 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
     // One request of a batch may be far longer than the others: a piece of k_attend_few has no more than 8192 tokens (63
     // requests of 2000 tokens and one of 131072, 64 heads on 8: 220 us, and 737 in one piece; 64 requests of 32768 each
     // 739 and 712).
-    if (l.rows < 128 && splits < (reach + 8191) / 8192) splits = (reach + 8191) / 8192;
+    if ((l.rows < 128 || l.few_tiles) && splits < (reach + 8191) / 8192) splits = (reach + 8191) / 8192;
     if (splits == 0) splits = 1;
     l.chunk = (uint32_t)(((reach + splits - 1) / splits + 127) / 128 * 128);
     if (l.chunk == 0) l.chunk = 128;
@@ -799,7 +810,9 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
     return l;
 }
 
-int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &a, void *stream) {
+int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &args, void *stream) {
+    AttendArgs a = args;
+    if (l.few_tiles) a.rows_from = few_rows(s) + 1;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const uint32_t grid = l.tiles * l.splits * s.kv_heads;
     by_shape(s, [&](auto d, auto bf16) {
@@ -809,6 +822,16 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
         else if constexpr (d() != 256) k_attend_many<d(), bf16(), 8, 128><<<grid, 512, 0, st>>>(a);
     });
     if (hipError_t e = hipGetLastError()) return (int)e;
+    if (l.few_tiles) {
+        AttendArgs f = a;
+        f.tiles = l.few_tiles;
+        f.tiles_each = l.few_tiles / a.requests;
+        f.by_length = 0;
+        f.rows_from = 0;
+        f.rows_to = few_rows(s);
+        by_shape(s, [&](auto d, auto bf16) { k_attend_few<d(), bf16(), d() == 256 ? 1 : 2><<<l.few_tiles * l.splits * s.kv_heads, 256, 0, st>>>(f); });
+        if (hipError_t e = hipGetLastError()) return (int)e;
+    }
     if (l.splits == 1) return 0;
     // a wave reads a few pieces of a row one after the other; more of them want more waves
     by_shape(s, [&](auto d, auto bf16) {

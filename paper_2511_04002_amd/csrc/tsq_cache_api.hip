@@ -179,7 +179,8 @@ tsq_status tsq_cache_attend(const tsq_cache *c, const tsq_cache_memory *m, uint3
     const uint64_t w = (uint64_t)c->s.q_heads * c->s.head_dim;
     if (bad_rows(d_q, q_stride, w, tokens) || bad_rows(d_out, out_stride, w, tokens)) return TSQ_ERR_INVALID_ARG;
     const AttendLaunch l = attend_launch(c->s, requests, tokens, max_new, max_length, window);
-    if ((uint64_t)l.tiles * l.splits * c->s.kv_heads >= (1ull << 31)) return TSQ_ERR_UNSUPPORTED;
+    if ((uint64_t)l.tiles * l.splits * c->s.kv_heads >= (1ull << 31) || (uint64_t)l.few_tiles * l.splits * c->s.kv_heads >= (1ull << 31))
+        return TSQ_ERR_UNSUPPORTED;
     if (l.splits > 1 && (!d_ws || misaligned(d_ws, 256))) return TSQ_ERR_INVALID_ARG;
     AttendArgs a;
     a.k = static_cast<const int8_t *>(m->d_k); a.v = static_cast<const int8_t *>(m->d_v);
@@ -192,6 +193,7 @@ tsq_status tsq_cache_attend(const tsq_cache *c, const tsq_cache_memory *m, uint3
     a.requests = requests; a.tokens = tokens; a.q_heads = c->s.q_heads; a.kv_heads = c->s.kv_heads;
     a.group = c->s.q_heads / c->s.kv_heads; a.blocks = c->s.blocks; a.block_log2 = c->s.block_log2; a.max_blocks = c->s.max_blocks;
     a.tiles = l.tiles; a.tiles_each = l.tiles_each; a.splits = l.splits; a.chunk = l.chunk; a.by_length = l.by_length;
+    a.rows_from = 0; a.rows_to = ~0u;
     a.window = window; a.causal = causal; a.scale_log2 = scale * 1.44269504088896340736f;
     return hip_rc(launch_attend(c->s, l, a, stream));
 }

@@ -69,6 +69,7 @@ struct AttendArgs {
     uint32_t tiles, tiles_each;  // row tiles of the call; of each request, or 0: they follow one another (see find_tile)
     uint32_t splits, chunk;      // pieces of a tile's reach along the cache, and the tokens of a piece (a multiple of 128)
     uint32_t by_length;          // the requests' workgroups in the order of their lengths, the longest first (2 .. 64 requests)
+    uint32_t rows_from, rows_to; // a launch is for the requests with so many rows of a kv head: rows_from <= rows <= rows_to
     uint32_t window;
     int32_t causal;
     float scale_log2;            // scale * log2(e)
@@ -80,7 +81,10 @@ int launch_append(const CacheShape &s, const AppendArgs &a, void *stream);
 int launch_gather(const CacheShape &s, const GatherArgs &a, void *stream);
 // How an attend call is split: by the shape and the caller's numbers alone, so that the workspace's size and the
 // launch agree.
-struct AttendLaunch { uint32_t rows, tiles, tiles_each, splits, chunk, by_length; };
+struct AttendLaunch {
+    uint32_t rows, tiles, tiles_each, splits, chunk, by_length;
+    uint32_t few_tiles;          // tiles of a second launch, for the requests of few rows among those of many; 0: there is none
+};
 AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length,
                            uint32_t window);
 int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &a, void *stream);

@@ -774,3 +774,20 @@ def test_attend_one_request_far_longer_than_the_others(heads):
     attend_both(b, hq, [1, 1, 0, 1], [30, 9001, 7, 0])
     attend_both(b, hq, [3, 9, 2], [30, 8500, 700], window=300)
     attend_both(b, hq, [40, 41], [40, 8400])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads", [(1, 1, 64), (8, 1, 128), (4, 2, 128), (2, 1, 256)])
+def test_attend_single_tokens_beside_a_prompt(dtype, heads):
+    # requests on both sides of the line between the kernels (64 rows of a kv head, 32 where a head has 256 elements), and
+    # far below the longest one: the outputs begin as 7, so that a request that neither launch takes is seen
+    hq, hk, dim = heads
+    group, few = hq // hk, 32 if dim == 256 else 64
+    line, long = few // group, 5 * few // group + 3
+    b = Both(1200, 16, hk, dim, dtype, 600, 91, q_heads=hq)
+    counts = [1, long, 1, line, 0, 1, line + 1, 2, 1, 1, 1, 1]
+    attend_both(b, hq, counts, [300, long + 17, 1, line + 5, 9, 40, line + 1, 700, 16, 0, 129, 33])
+    attend_both(b, hq, counts, [300, long, 1, line, 0, 40, line + 90, 2, 16, 17, 128, 33], window=21)
+    attend_both(b, hq, counts, [300, long, 1, line, 0, 40, line + 90, 2, 16, 17, 128, 33], causal=False)
+    attend_both(b, hq, [1] * 7 + [long], [5, 8300, 2, 1, 64, 0, 31, long + 1])
+    attend_both(b, hq, [1] * 70 + [long], [1 + 7 * (r % 30) for r in range(70)] + [long], max_new=long + 40)
