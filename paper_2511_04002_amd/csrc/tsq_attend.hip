@@ -127,6 +127,12 @@ __device__ __forceinline__ void row_sees(const AttendArgs &a, const Place &p, ui
     to = hi > lo ? (uint32_t)hi : 0u;
 }
 
+// A row of a request that is longer than its row of the table, and that sees anything of it: NaN, whatever it sees.  (Its
+// window may lie past all that the table holds, so that the tokens which are looked at cannot tell.)
+__device__ __forceinline__ bool is_lost(const AttendArgs &a, const Place &p, uint32_t row) {
+    return p.beyond && (!a.causal || (int64_t)p.length - p.n + row / a.group >= 0);
+}
+
 // The table's entry for the 16 tokens from `token` on, as it is (past the end of a reach: its last one, so that what is
 // asked for ahead of need is always there, and costs no new lines).  It is looked at when it is used, by id_of, so that
 // nothing waits for it before.
@@ -185,14 +191,15 @@ __device__ __forceinline__ uint64_t row_id(const AttendArgs &a, const Place &p, 
     return (uint64_t)(p.begin + row / a.group) * a.q_heads + p.h * a.group + row % a.group;
 }
 
-// A piece that lies behind a tile's reach: no row sees anything, and that is all that the join has to know.
+// A piece that lies behind a tile's reach: no row sees anything, and that is all that the join has to know (of a weight
+// of NaN, too, whatever the sums are).
 template <int ROWS>
 __device__ __forceinline__ void nothing_seen(const AttendArgs &a, const Place &p, uint32_t tile, int head_dim) {
     const uint32_t row = tile * ROWS + threadIdx.x;
     if (threadIdx.x >= ROWS || row >= p.n * a.group) return;
     float *st = a.parts + a.part_rows * a.splits * head_dim + (row_id(a, p, row) * a.splits + p.split) * 2;
     st[0] = kNone;
-    st[1] = 0.0f;
+    st[1] = is_lost(a, p, row) ? __builtin_nanf("") : 0.0f;
 }
 
 // Few rows: 16 of a kv head's, or 32 (SETS = 2, which share the codes once they are halves).  Each of four waves takes
@@ -368,6 +375,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
             const uint32_t out_row = threadIdx.x >> 4, piece = threadIdx.x & 15, o = tile * ROWS + 16 * c + out_row;
             float total = 0.0f, top = fmaxf(fmaxf(stats[0][out_row][0], stats[1][out_row][0]), fmaxf(stats[2][out_row][0], stats[3][out_row][0]));
             for (int w = 0; w < 4; ++w) total += stats[w][out_row][1] * pow2(stats[w][out_row][0] - top);
+            if (is_lost(a, p, o)) total = __builtin_nanf("");
             const uint64_t id = row_id(a, p, o);
             for (int part = 0; part < (D + 127) / 128; ++part) {
                 constexpr int N = D < 128 ? D : 128;     // elements at a time
@@ -642,6 +650,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
             __syncthreads();
         }
         weight += __shfl_xor(weight, 32);
+        if (is_lost(a, p, row)) weight = __builtin_nanf("");
 
         if (row < rows) {
             const uint64_t id = row_id(a, p, row);

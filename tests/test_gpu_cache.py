@@ -791,3 +791,29 @@ def test_attend_single_tokens_beside_a_prompt(dtype, heads):
     attend_both(b, hq, counts, [300, long, 1, line, 0, 40, line + 90, 2, 16, 17, 128, 33], causal=False)
     attend_both(b, hq, [1] * 7 + [long], [5, 8300, 2, 1, 64, 0, 31, long + 1])
     attend_both(b, hq, [1] * 70 + [long], [1 + 7 * (r % 30) for r in range(70)] + [long], max_new=long + 40)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads", [(2, 2, 64), (8, 1, 128), (4, 2, 256)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attend_windows_past_the_table(dtype, heads, causal):
+    hq, hk, dim = heads
+    b = Both(60, 16, hk, dim, dtype, 6, hq + causal, q_heads=hq)
+    table = b.g.permutation(60)[:18].reshape(3, 6).astype(np.int32)
+    more = dict(table=table, causal=causal)
+    for window in (1, 20, 90, 110, 300):
+        attend_both(b, hq, [1, 1, 1], [200, 120, 90], window=window, **more)
+        attend_both(b, hq, [3, 70, 2], [200, 190, 40], window=window, **more)
+    attend_both(b, hq, [3, 70, 120], [200, 190, 97], **more)
+
+
+@pytest.mark.parametrize("heads", [(1, 1, 64), (8, 1, 128), (4, 2, 256)])
+def test_attend_windows_past_the_table_in_pieces(heads):
+    hq, hk, dim = heads
+    b = Both(180, 16, hk, dim, "bf16", 30, 3, q_heads=hq)
+    table = b.g.permutation(180).reshape(6, 30).astype(np.int32)
+    # the third: requests of few rows beside one of many, each in a launch of its own
+    for counts in ([1] * 6, [2, 150, 90, 1, 0, 3], [1, 150, 1, 1, 1, 2]):
+        assert cachelib.tsq_cache_attend_workspace_bytes(b.c.handle, 6, sum(counts), max(counts), 9000, 700) > 0
+        attend_both(b, hq, counts, [2000, 9000, 470, 481, 5, 700], window=700, table=table)
+        attend_both(b, hq, counts, [2000, 2900, 470, 481, 480, 700], window=0, table=table)
