@@ -24,6 +24,8 @@ namespace {
 constexpr float kNone = -1e30f;      // reference of a row that has seen nothing
 constexpr float kRoom = 7.0f;        // the reference is set this far below the largest exponent ...
 constexpr float kSlack = 8.0f;       // ... and kept until one exceeds that by as much
+constexpr float kCoarse = 0x1p22f;   // beyond this a reference's last bit is worth 1/2 or more: the difference of a score that
+                                     // is not rounded and one that is would pass a half's range
 
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
@@ -500,6 +502,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
         for (int d = 0; d < D / 32; ++d)
             for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
         float ref = kNone, weight = 0.0f;
+        bool coarse = false;         // some row's reference is too large for an exponent to be made in one rounding
 
         // staging: what this thread brings of a tile
         // (a thread's places in a block are the same for all tiles, but for the half of a block of 128 tokens)
@@ -606,12 +609,22 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
                     weight *= down;
 #pragma unroll
                     for (int d = 0; d < D / 32; ++d) acc[d] *= down;
+                    coarse = __ballot(fabsf(ref) > kCoarse && ref != kNone) != 0;
                 }
                 half8_t pw[4];
+                if (coarse) {                            // (the reference is rounded: so is, in its row, what it is taken from)
+                    const bool here = fabsf(ref) > kCoarse;
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const float off = lv[b] - ref;
-                    for (int i = 0; i < 8; ++i) s[b / 2][8 * (b & 1) + i] = pow2(__builtin_fmaf(s[b / 2][8 * (b & 1) + i], factor[b], off));
+                    for (int b = 0; b < 4; ++b) {
+                        const float off = here ? lv[b] : lv[b] - ref, less = here ? ref : 0.0f;
+                        for (int i = 0; i < 8; ++i) s[b / 2][8 * (b & 1) + i] = pow2(__builtin_fmaf(s[b / 2][8 * (b & 1) + i], factor[b], off) - less);
+                    }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const float off = lv[b] - ref;
+                        for (int i = 0; i < 8; ++i) s[b / 2][8 * (b & 1) + i] = pow2(__builtin_fmaf(s[b / 2][8 * (b & 1) + i], factor[b], off));
+                    }
                 }
                 if (!whole) {                            // (a factor of 0 or NaN has made NaN of -inf)
 #pragma unroll

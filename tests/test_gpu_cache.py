@@ -817,3 +817,13 @@ def test_attend_windows_past_the_table_in_pieces(heads):
         assert cachelib.tsq_cache_attend_workspace_bytes(b.c.handle, 6, sum(counts), max(counts), 9000, 700) > 0
         attend_both(b, hq, counts, [2000, 9000, 470, 481, 5, 700], window=700, table=table)
         attend_both(b, hq, counts, [2000, 2900, 470, 481, 480, 700], window=0, table=table)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("counts", [[1, 1], [5, 2], [80, 95]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_attend_of_scores_past_the_exponents_resolution(dtype, counts, dim):
+    b = Both(12, 16, 1, dim, dtype, 6, dim, q_heads=2)
+    b.ks *= np.float32(2.0 ** 13)
+    b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
+    attend_both(b, 2, counts, [80, 95], q=rows(b.g, sum(counts), 2, dim, dtype, 2.0 ** 13))
