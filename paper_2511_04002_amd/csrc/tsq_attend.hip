@@ -21,7 +21,7 @@
 namespace tsq {
 namespace {
 
-constexpr float kNone = -1e30f;      // reference of a row that has seen nothing
+constexpr float kNone = -0x1.fffffep127f;      // reference of a row that has seen nothing: below any score
 constexpr float kRoom = 7.0f;        // the reference is set this far below the largest exponent ...
 constexpr float kSlack = 8.0f;       // ... and kept until one exceeds that by as much
 constexpr float kCoarse = 0x1p22f;   // beyond this a reference's last bit is worth 1/2 or more: the difference of a score that

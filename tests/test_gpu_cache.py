@@ -827,3 +827,13 @@ def test_attend_of_scores_past_the_exponents_resolution(dtype, counts, dim):
     b.ks *= np.float32(2.0 ** 13)
     b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
     attend_both(b, 2, counts, [80, 95], q=rows(b.g, sum(counts), 2, dim, dtype, 2.0 ** 13))
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [3, 2], [40, 90]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_attend_of_very_low_scores(counts, dim):
+    b = Both(12, 16, 1, dim, "bf16", 6, dim, q_heads=2)
+    b.k[:], b.ks[:], b.vs[:] = -127, 2.0 ** 45, 0.5
+    b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
+    q = torch.full((sum(counts), 2, dim), 2.0 ** 60, dtype=torch.bfloat16, device="cuda")
+    attend_both(b, 2, counts, [80, 95], q=q)
