@@ -148,15 +148,57 @@ __device__ __forceinline__ bool is_bad(const AttendArgs &a, const Place &p, uint
 // What the tokens of a block have in common for a head: the factor of the scores, and the values' scale as log2 and
 // as reciprocal.  Values that are all 0 weigh nothing whatever their scale is: 2^-60 keeps their tokens in the
 // denominator without touching the reference of the others.
+//
+// A row's exponents hold scales of 2^-60 to 2^40 together, all that values of magnitudes from 2^-53 to 2^47 bring: with
+// scales farther apart, tokens of small ones would be lost from the denominator, and of scales below about 2^-110 it would
+// pass binary32's range.  A tile that meets others is gone through twice more: once for the softmax of the scores
+// alone (kScores), and once for the sums of the values (kValues), each with a reference of its own.
+enum Mode : uint32_t { kAll, kScores, kValues };
+__device__ __forceinline__ bool is_far(float log_v) { return fabsf(log_v + 10.0f) > 50.0f; }
 struct Scale { float k, v; bool bad; };
 __device__ __forceinline__ Scale scale_at(const AttendArgs &a, const Place &p, uint32_t entry) {
     const uint64_t at = (uint64_t)id_of(a, entry) * a.kv_heads + p.h;
     return Scale{a.k_scale[at], a.v_scale[at], is_bad(a, p, entry)};
 }
 struct Block { float c, log_v, back_v; };
-__device__ __forceinline__ Block block_of(Scale s, float row_factor) {
+__device__ __forceinline__ Block block_of(Scale s, float row_factor, uint32_t mode) {
     const float v = s.v == 0.0f ? 0x1p-60f : s.v;
-    return Block{s.bad ? __builtin_nanf("") : s.k * row_factor, log2_of(v), 1.0f / v};
+    Block b{s.bad ? __builtin_nanf("") : s.k * row_factor, log2_of(v), 1.0f / v};
+    if (mode == kScores) { b.log_v = s.v - s.v; b.back_v = 1.0f; }           // (0, or NaN)
+    if (mode == kValues && s.v == 0.0f) b.log_v = -INFINITY;
+    return b;
+}
+struct Softmax { float ref, weight; };                   // of a row, from kScores
+
+// The kernel's arguments, read once more: what only the end of a tile needs then takes no scalar registers in its loop,
+// where a few too many cost k_attend_many the order of its loads and products (7 % of its time).
+__device__ __forceinline__ AttendArgs args_again() {
+    struct Words { uint32_t w[sizeof(AttendArgs) / 4]; } words;
+    auto args = (const __attribute__((address_space(4))) uint32_t *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(args));
+    for (uint32_t i = 0; i < sizeof(AttendArgs) / 4; ++i) words.w[i] = args[i];
+    return __builtin_bit_cast(AttendArgs, words);
+}
+
+// What a row ends with: its statistics, and what its sums are to be multiplied by, f h h (h twice, since binary32 may
+// not hold its square).  The sums of a piece along the cache stay as they are; from kValues they become an average, which
+// goes to the join at 2^-10 of its size, so that the join can add a thousand of them.
+struct Ending { float top, total, f, h; };
+__device__ __forceinline__ Ending ending(const AttendArgs &a, uint32_t mode, float top, float total, Softmax x) {
+    Ending e{top, total, 1.0f, 1.0f};
+    if (mode == kValues) {
+        e.top = x.ref;
+        e.total = x.weight;
+        e.h = x.weight == 0.0f ? 0.0f : pow2(0.5f * (top - x.ref));
+    }
+    const float back = e.total == 0.0f ? 0.0f : 1.0f / e.total;
+    if (a.splits == 1) e.f = back;
+    else if (mode == kValues) {
+        e.f = back * 0x1p-10f;
+        e.top = x.weight == 0.0f ? kNone : x.ref + log2_of(x.weight) + 10.0f;
+        e.total = x.weight * e.f;
+    }
+    return e;
 }
 
 // A query's 16-bit elements as halves, and what the scores are to be multiplied by for it: binary16 as it is,
@@ -221,17 +263,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
     constexpr int ROWS = 16 * SETS;
     __shared__ float sums[4][16][132];
     __shared__ float stats[4][16][2];
+    __shared__ Softmax softmax[ROWS];                    // (of the pass kScores)
+    __shared__ uint32_t far[4];
     Place p;
     if (!find_place<ROWS>(a, p)) return;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
     const uint32_t B = 1u << a.block_log2;
-    for (uint32_t tile = p.tile;; ++tile) {
+    uint32_t mode = kAll;
+    for (uint32_t tile = p.tile;;) {
         const uint32_t rows = p.n * a.group;
         const Reach reach = reach_of<ROWS>(a, p, tile);
         const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
         if (a.splits > 1 && reach.begin >= reach.end) {
             nothing_seen<ROWS>(a, p, tile, D);
             if (done) return;
+            ++tile;
             continue;
         }
         half8_t q[SETS][F][2];
@@ -266,6 +312,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
 
         float4_t acc[SETS][D / 16];
         float ref[SETS], weight[SETS];
+        bool met_far = false;
 #pragma unroll
         for (int c = 0; c < SETS; ++c) {
             for (int d = 0; d < D / 16; ++d) acc[c][d] = float4_t{0, 0, 0, 0};
@@ -309,7 +356,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
                         for (int c = 0; c < SETS; ++c) s[c][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[c][f][e], s[c][t], 0, 0, 0);
                     }
             }
-            const Block b = block_of(scale, a.scale_log2);
+            const Block b = block_of(scale, a.scale_log2, mode);
+            met_far |= is_far(b.log_v);
             const uint32_t entry = next;
             ask_keys(t0 + 256, entry);
             next = table_entry(a, p, t0 + 512 + 16 * g, reach.end);
@@ -365,6 +413,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
         }
 
         // the four waves' sums, at one reference
+        const bool any_far = __ballot(met_far) != 0;
+        if (lane == 0) far[wave] = mode == kAll && any_far;
+        bool again = false;
 #pragma unroll
         for (int c = 0; c < SETS; ++c) {
             weight[c] += __shfl_xor(weight[c], 16);
@@ -372,12 +423,19 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
             if (c) __syncthreads();
             if (g == 0) { stats[wave][m][0] = ref[c]; stats[wave][m][1] = weight[c]; }
             __syncthreads();
+            if (c == 0) again = (far[0] | far[1] | far[2] | far[3]) != 0;
+            if (again) break;
             const float all = fmaxf(fmaxf(stats[0][m][0], stats[1][m][0]), fmaxf(stats[2][m][0], stats[3][m][0]));
             const float mine = pow2(ref[c] - all);
             const uint32_t out_row = threadIdx.x >> 4, piece = threadIdx.x & 15, o = tile * ROWS + 16 * c + out_row;
             float total = 0.0f, top = fmaxf(fmaxf(stats[0][out_row][0], stats[1][out_row][0]), fmaxf(stats[2][out_row][0], stats[3][out_row][0]));
             for (int w = 0; w < 4; ++w) total += stats[w][out_row][1] * pow2(stats[w][out_row][0] - top);
             if (is_lost(a, p, o)) total = __builtin_nanf("");
+            if (mode == kScores) {
+                if (piece == 0) softmax[16 * c + out_row] = Softmax{top, total};
+                continue;
+            }
+            const Ending end = ending(a, mode, top, total, softmax[16 * c + out_row]);
             const uint64_t id = row_id(a, p, o);
             for (int part = 0; part < (D + 127) / 128; ++part) {
                 constexpr int N = D < 128 ? D : 128;     // elements at a time
@@ -386,12 +444,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
                 __syncthreads();
                 if (piece * 8 < N && o < rows) {
                     float y[8];
-                    for (int i = 0; i < 8; ++i)
+                    for (int i = 0; i < 8; ++i) {
                         y[i] = sums[0][out_row][8 * piece + i] + sums[1][out_row][8 * piece + i] + sums[2][out_row][8 * piece + i] + sums[3][out_row][8 * piece + i];
+                        y[i] = y[i] * end.f * end.h * end.h;
+                    }
                     if (a.splits == 1) {
-                        const float f = total == 0.0f ? 0.0f : 1.0f / total;
                         uint4_t w;
-                        for (int i = 0; i < 4; ++i) w[i] = narrow2<BF16>(y[2 * i] * f, y[2 * i + 1] * f);
+                        for (int i = 0; i < 4; ++i) w[i] = narrow2<BF16>(y[2 * i], y[2 * i + 1]);
                         uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)(p.begin + o / a.group) * a.out_stride +
                                         (uint64_t)(p.h * a.group + o % a.group) * D + part * 128 + piece * 8;
                         *reinterpret_cast<uint4_t *>(dst) = w;
@@ -405,14 +464,20 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
             if (piece == 0 && o < rows) {
                 if (a.splits > 1) {
                     float *dst = a.parts + a.part_rows * a.splits * D + (id * a.splits + p.split) * 2;
-                    dst[0] = top;
-                    dst[1] = total;
+                    dst[0] = end.top;
+                    dst[1] = end.total;
                 } else if (a.lse) {
-                    a.lse[id] = total == 0.0f ? -INFINITY : (top + log2_of(total)) * 0.69314718055994530942f;
+                    a.lse[id] = end.total == 0.0f ? -INFINITY : (end.top + log2_of(end.total)) * 0.69314718055994530942f;
                 }
             }
         }
-        if (done) return;
+        if (again || mode == kScores) {
+            mode = again ? kScores : kValues;
+        } else {
+            if (done) return;
+            mode = kAll;
+            ++tile;
+        }
         __syncthreads();
     }
 }
@@ -458,17 +523,21 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
     constexpr int N = TOKENS * D / 16 / THREADS;         // 16-byte pieces of keys, and of values, that a thread stages
     typedef ManyTile<D, TOKENS> Tile;
     __shared__ Tile buffer[2];
+    __shared__ Softmax softmax[ROWS];                    // (of the pass kScores)
+    __shared__ uint32_t far;
     Place p;
     if (!find_place<ROWS>(a, p)) return;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6)), n = lane & 31, hi = lane >> 5;
     const uint32_t B = 1u << a.block_log2;
-    for (uint32_t tile = p.tile;; ++tile) {
+    uint32_t mode = kAll;
+    for (uint32_t tile = p.tile;;) {
         const uint32_t row = tile * ROWS + wave * 32 + n, rows = p.n * a.group;
         const Reach reach = reach_of<ROWS>(a, p, tile);
         const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
         if (a.splits > 1 && reach.begin >= reach.end) {
             nothing_seen<ROWS>(a, p, tile, D);
             if (done) return;
+            ++tile;
             continue;
         }
         half8_t q[D / 16];
@@ -546,14 +615,16 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
                 *reinterpret_cast<half8_t *>(to_v + 8) = __builtin_shufflevector(h[1], h[3], 0, 1, 2, 3, 4, 5, 6, 7);
             }
             if (tid < SUBS) {
-                const Block b = block_of(scale, a.scale_log2);
+                const Block b = block_of(scale, a.scale_log2, mode);
                 t.factor[tid] = b.c;
                 t.log_v[tid] = b.log_v;
                 t.back_v[tid] = b.back_v;
+                if (is_far(b.log_v)) far = 1;
             }
         };
 
         // What a tile brings is asked for a tile ahead and put into the other buffer when the present one is worked on.
+        if (tid == 0) far = 0;       // (the threads that may set it are of this wave)
         if (reach.begin < reach.end) {
             ask_entries(reach.begin);
             ask(reach.begin);
@@ -665,18 +736,25 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
         weight += __shfl_xor(weight, 32);
         if (is_lost(a, p, row)) weight = __builtin_nanf("");
 
-        if (row < rows) {
+        const bool again = mode == kAll && far;
+        Softmax &mine = softmax[wave * 32 + n];          // (of this wave alone)
+        if (mode == kScores) mine = Softmax{ref, weight};
+        else if (!again && row < rows) {
+            const AttendArgs a = args_again();
+            const Ending end = ending(a, mode, ref, weight, mine);
             const uint64_t id = row_id(a, p, row);
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+                for (int i = 0; i < 16; ++i) acc[d][i] = acc[d][i] * end.f * end.h * end.h;
             if (a.splits == 1) {
-                const float f = weight == 0.0f ? 0.0f : 1.0f / weight;
                 uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)(p.begin + row / a.group) * a.out_stride +
                                 (uint64_t)(p.h * a.group + row % a.group) * D + 4 * hi;
 #pragma unroll
                 for (int d = 0; d < D / 32; ++d)
                     for (int b = 0; b < 4; ++b)
                         *reinterpret_cast<uint2_t *>(dst + 32 * d + 8 * b) =
-                            uint2_t{narrow2<BF16>(acc[d][4 * b] * f, acc[d][4 * b + 1] * f), narrow2<BF16>(acc[d][4 * b + 2] * f, acc[d][4 * b + 3] * f)};
-                if (a.lse && hi == 0) a.lse[id] = weight == 0.0f ? -INFINITY : (ref + log2_of(weight)) * 0.69314718055994530942f;
+                            uint2_t{narrow2<BF16>(acc[d][4 * b], acc[d][4 * b + 1]), narrow2<BF16>(acc[d][4 * b + 2], acc[d][4 * b + 3])};
+                if (a.lse && hi == 0) a.lse[id] = end.total == 0.0f ? -INFINITY : (end.top + log2_of(end.total)) * 0.69314718055994530942f;
             } else {
                 float *dst = a.parts + (id * a.splits + p.split) * D + 4 * hi;
 #pragma unroll
@@ -685,12 +763,19 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
                         *reinterpret_cast<float4_t *>(dst + 32 * d + 8 * b) = float4_t{acc[d][4 * b], acc[d][4 * b + 1], acc[d][4 * b + 2], acc[d][4 * b + 3]};
                 if (hi == 0) {
                     float *st = a.parts + a.part_rows * a.splits * D + (id * a.splits + p.split) * 2;
-                    st[0] = ref;
-                    st[1] = weight;
+                    st[0] = end.top;
+                    st[1] = end.total;
                 }
             }
         }
-        if (done) return;
+        if (again || mode == kScores) {
+            mode = again ? kScores : kValues;
+        } else {
+            if (done) return;
+            mode = kAll;
+            ++tile;
+        }
+        __syncthreads();
     }
 }
 

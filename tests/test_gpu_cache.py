@@ -837,3 +837,54 @@ def test_attend_of_very_low_scores(counts, dim):
     b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
     q = torch.full((sum(counts), 2, dim), 2.0 ** 60, dtype=torch.bfloat16, device="cuda")
     attend_both(b, 2, counts, [80, 95], q=q)
+
+
+def far_apart(b, table, kind):
+    n = b.ks.shape[0]
+    if kind in ("zeros beside large", "zeros beside small"):
+        b.vs[:] = np.float32(2.0 ** (100 if kind == "zeros beside large" else -110))
+        b.vs[table[:, ::2]] = 0
+        b.v[table[:, ::2]] = 0
+    elif kind == "small":
+        b.vs[:] = np.float32(2.0 ** -126) * b.g.uniform(1, 2, b.vs.shape).astype(np.float32)
+    elif kind == "large":
+        b.vs[:] = np.float32(2.0 ** 120) * b.g.uniform(1, 1.5, b.vs.shape).astype(np.float32)
+    elif kind == "within":
+        b.vs[:] = np.float32(2.0 ** -60) * b.g.uniform(1, 2, b.vs.shape).astype(np.float32)
+        b.vs[table[:, 1::2]] = np.float32(2.0 ** 40)
+    elif kind == "both":
+        b.vs[:] = np.float32(2.0 ** -110)
+        b.vs[table[:, 1::2]] = np.float32(2.0 ** 90)
+    else:
+        b.vs[:] = np.exp2(b.g.integers(-126, 121, b.vs.shape)).astype(np.float32)
+    b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
+
+
+@pytest.mark.parametrize("kind", ["zeros beside large", "zeros beside small", "small", "large", "within", "both", "any"])
+@pytest.mark.parametrize("heads", [(2, 2, 64), (8, 1, 128), (4, 2, 256)])
+def test_attend_of_value_scales_at_the_ends_of_their_range(kind, heads):
+    hq, hk, dim = heads
+    b = Both(40, 16, hk, dim, "bf16", 20, 60 + dim, q_heads=hq)
+    table = b.g.permutation(40).reshape(2, 20).astype(np.int32)
+    far_apart(b, table, kind)
+    for counts in ([1, 1], [9, 3], [33, 300]):
+        attend_both(b, hq, counts, [301, 317], table=table)
+        attend_both(b, hq, counts, [301, 317], table=table, window=50)
+
+
+@pytest.mark.parametrize("kind", ["zeros beside large", "small", "large", "any"])
+@pytest.mark.parametrize("counts", [[1, 1], [2, 70], [1, 1, 1, 1, 1, 70]])
+def test_attend_of_value_scales_at_the_ends_of_their_range_in_pieces(kind, counts):
+    b = Both(620, 16, 1, 128, "bf16", 300, 70, q_heads=8)
+    table = b.g.integers(0, 620, (len(counts), 300)).astype(np.int32)
+    far_apart(b, table, kind)
+    attend_both(b, 8, counts, [4800, 3333, 0, 9, 3000, 2000][:len(counts) - 1] + [3333], table=table)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_attend_of_small_value_scales_in_binary16(dim):
+    b = Both(40, 16, 1, dim, "f16", 20, 80 + dim, q_heads=3)
+    table = b.g.permutation(40).reshape(2, 20).astype(np.int32)
+    far_apart(b, table, "small")
+    for counts in ([1, 1], [50, 3]):
+        attend_both(b, 3, counts, [301, 317], table=table)
