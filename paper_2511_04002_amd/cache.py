@@ -117,12 +117,22 @@ def tsq_cache_attend_workspace_bytes(cache: int, requests: int, tokens: int, max
 # ------------------------------------------------------------------ convenience over torch tensors
 
 class Memory:
-    """The four tensors of one cache, and the C structure that holds their pointers."""
+    """The four tensors of one cache, and the C structure that holds their pointers: k int8 [blocks, kv_heads, block_tokens,
+    head_dim], v int8 [blocks, kv_heads, head_dim, block_tokens], scales float32 [blocks, kv_heads].  They are looked at once,
+    here, and stay what they are; a cache takes a memory of its own shape only."""
 
     def __init__(self, k, v, k_scale, v_scale):
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.c = tsq_cache_memory(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
-        self.ref = C.byref(self.c)
+        import torch
+        shape = tuple(k.shape)
+        n, h, b, d = shape if len(shape) == 4 else (0, 0, 0, 0)
+        for x, size, kind in ((k, (n, h, b, d), torch.int8), (v, (n, h, d, b), torch.int8), (k_scale, (n, h), torch.float32), (v_scale, (n, h), torch.float32)):
+            if not (x.is_cuda and x.is_contiguous() and tuple(x.shape) == size and x.dtype == kind):
+                _refuse("a cache's tensor is %s on the GPU, contiguous, %s" % (size, kind))
+        c = tsq_cache_memory(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.__dict__.update(k=k, v=v, k_scale=k_scale, v_scale=v_scale, shape=shape, c=c, ref=C.byref(c))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a memory's tensors are not replaced")
 
 
 class Schedule:
@@ -164,6 +174,7 @@ class Cache:
         self.int32, self.int64, self.float32 = torch.int32, torch.int64, torch.float32
         self.blocks, self.block_tokens, self.q_heads, self.kv_heads = blocks, block_tokens, q_heads, kv_heads
         self.head_dim, self.dtype, self.max_blocks = head_dim, dtype, max_blocks
+        self.shape = (blocks, kv_heads, block_tokens, head_dim)
         self.cfg = tsq_cache_config(blocks, block_tokens, q_heads, kv_heads, head_dim, tsq._DTYPES[dtype], max_blocks, 0)
         self.handle = tsq_cache_create(self.cfg)
         self._torch, self._lib = torch, lib()
@@ -192,12 +203,9 @@ class Cache:
     def wrap(self, k, v, k_scale, v_scale) -> Memory:
         """A cache in tensors that are there: k [blocks, kv_heads, block_tokens, head_dim] int8,
         v [blocks, kv_heads, head_dim, block_tokens] int8, scales [blocks, kv_heads] float32."""
-        t = self._torch
-        n, h, b, d = self.blocks, self.kv_heads, self.block_tokens, self.head_dim
-        for x, shape, kind in ((k, (n, h, b, d), t.int8), (v, (n, h, d, b), t.int8), (k_scale, (n, h), t.float32), (v_scale, (n, h), t.float32)):
-            if not (x.is_cuda and x.is_contiguous() and tuple(x.shape) == shape and x.dtype == kind):
-                _refuse("a cache's tensor is %s on the GPU, contiguous, %s" % (shape, kind))
-        return Memory(k, v, k_scale, v_scale)
+        memory = Memory(k, v, k_scale, v_scale)
+        self._memory(memory)
+        return memory
 
     def new_table(self, requests: int):
         return self._torch.full((requests, self.max_blocks), -1, dtype=self.int32, device="cuda")
@@ -219,6 +227,11 @@ class Cache:
 
     # (a step calls these for every tensor of every operator: what a tensor holds is told by its type, place and number
     # of elements, and its shape is looked at only where it is not contiguous)
+
+    def _memory(self, memory):
+        if memory.shape != self.shape:
+            _refuse("the memory is that of a cache of %s, this one is %s (blocks, kv_heads, block_tokens, head_dim)" % (memory.shape, self.shape))
+        return memory.ref
 
     def _ints(self, x, n, what):
         if not (x.dtype is self.int32 and x.is_cuda and x.is_contiguous() and x.numel() == n):
@@ -305,7 +318,7 @@ class Cache:
         tokens = k.shape[0]
         kp, ks = self._rows(k, tokens, self.kv_heads, "k")
         vp, vs = self._rows(v, tokens, self.kv_heads, "v")
-        status = self._lib.tsq_cache_append(self.handle, memory.ref, tokens, kp, ks, vp, vs, self._ints(slots, tokens, "slots"),
+        status = self._lib.tsq_cache_append(self.handle, self._memory(memory), tokens, kp, ks, vp, vs, self._ints(slots, tokens, "slots"),
                                             self._stream())
         if status:
             raise TsqError(status, "tsq_cache_append")
@@ -316,7 +329,7 @@ class Cache:
         tokens, n = k_out.shape[0], lengths.numel()
         kp, ks = self._rows(k_out, tokens, self.kv_heads, "k_out")
         vp, vs = self._rows(v_out, tokens, self.kv_heads, "v_out")
-        status = self._lib.tsq_cache_gather(self.handle, memory.ref, n, *self._requests(table, starts, lengths, n), tokens, kp, ks, vp, vs,
+        status = self._lib.tsq_cache_gather(self.handle, self._memory(memory), n, *self._requests(table, starts, lengths, n), tokens, kp, ks, vp, vs,
                                             self._stream())
         if status:
             raise TsqError(status, "tsq_cache_gather")
@@ -352,7 +365,7 @@ class Cache:
                 _refuse("ws has %d bytes on the GPU, contiguous" % need)
             wp = ws.data_ptr()
         status = L.tsq_cache_attend(
-            self.handle, memory.ref, n, *self._requests(table, starts, lengths, n), tokens, max_new, max_length, qp, qs,
+            self.handle, self._memory(memory), n, *self._requests(table, starts, lengths, n), tokens, max_new, max_length, qp, qs,
             self.head_dim ** -0.5 if scale is None else scale, causal, window, op, os_, lp, wp, self._stream())
         if status:
             raise TsqError(status, "tsq_cache_attend")

@@ -888,3 +888,29 @@ def test_attend_of_small_value_scales_in_binary16(dim):
     far_apart(b, table, "small")
     for counts in ([1, 1], [50, 3]):
         attend_both(b, 3, counts, [301, 317], table=table)
+
+
+@pytest.mark.parametrize("change", [dict(blocks=3), dict(blocks=5), dict(block_tokens=32), dict(kv_heads=1), dict(head_dim=64)])
+def test_a_memory_of_another_cache_is_refused(change):
+    numbers = dict(blocks=4, block_tokens=16, q_heads=4, kv_heads=2, head_dim=128, dtype="f16", max_blocks=2)
+    c, other = cachelib.Cache(**numbers), cachelib.Cache(**{**numbers, **change}).new_memory()
+    q, k = (torch.zeros((3, n, 128), dtype=torch.float16, device="cuda") for n in (4, 2))
+    slots, starts, lengths, table = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in (3, 3, 2, (2, 2)))
+    for call in (lambda: c.append(other, k, k, slots), lambda: c.gather(other, table, starts, lengths, k, k.clone()),
+                 lambda: c.attend(other, q, table, starts, lengths, 1, 20), lambda: c.wrap(other.k, other.v, other.k_scale, other.v_scale)):
+        with pytest.raises(ValueError, match="the memory is that of"):
+            call()
+    c.append(c.wrap(*(getattr(c.new_memory(), n) for n in ("k", "v", "k_scale", "v_scale"))), k, k, slots - 1)
+
+
+def test_a_memorys_tensors_are_looked_at_and_not_replaced():
+    c = cachelib.Cache(4, 16, 1, 1, 64, "f16", 2)
+    m = c.new_memory()
+    with pytest.raises(AttributeError):
+        m.k = m.k.clone()
+    good = [m.k, m.v, m.k_scale, m.v_scale]
+    for at, x in ((0, m.k[0]), (0, m.k.cpu()), (1, m.v[:3]), (2, m.k_scale.double()), (3, m.v_scale[:, :0]), (1, m.k)):
+        args = list(good)
+        args[at] = x
+        with pytest.raises(ValueError):
+            cachelib.Memory(*args)
