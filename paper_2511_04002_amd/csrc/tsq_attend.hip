@@ -271,11 +271,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
     const uint32_t B = 1u << a.block_log2;
     uint32_t mode = kAll;
     for (uint32_t tile = p.tile;;) {
-        const uint32_t rows = p.n * a.group;
-        const Reach reach = reach_of<ROWS>(a, p, tile);
+        const AttendArgs here = args_again();
+        const uint32_t rows = p.n * here.group;
+        const Reach reach = reach_of<ROWS>(here, p, tile);
         const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
-        if (a.splits > 1 && reach.begin >= reach.end) {
-            nothing_seen<ROWS>(a, p, tile, D);
+        if (here.splits > 1 && reach.begin >= reach.end) {
+            nothing_seen<ROWS>(here, p, tile, D);
             if (done) return;
             ++tile;
             continue;
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
                 for (int e = 0; e < 2; ++e) {
                     w[f][e] = uint4_t{0, 0, 0, 0};
                     if (row < rows) {
-                        const uint16_t *src = static_cast<const uint16_t *>(a.q) + (uint64_t)(p.begin + row / a.group) * a.q_stride +
+                        const uint16_t *src = static_cast<const uint16_t *>(here.q) + (uint64_t)(p.begin + row / a.group) * here.q_stride +
                                               (uint64_t)(p.h * a.group + row % a.group) * D + 64 * f + 16 * g + 8 * e;
                         w[f][e] = *reinterpret_cast<const uint4_t *>(src);
                     }
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
             }
             for (int f = 0; f < F; ++f)
                 for (int e = 0; e < 2; ++e) q[c][f][e] = query_piece<BF16>(w[f][e], factor);
-            row_sees(a, p, row, from[c], to[c]);
+            row_sees(here, p, row, from[c], to[c]);
         }
 
         float4_t acc[SETS][D / 16];
@@ -324,9 +325,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
         // when that one's are used up, and its block numbers a tile earlier still.
         uint4_t kw[4][F], vw[D / 16];
         Scale scale = {};
+        const int8_t *my_keys = a.k + (m & 3) * D + 16 * g;
         auto ask_keys = [&](uint32_t t0, uint32_t entry) {
             const uint32_t key_id = (uint32_t)__shfl((int)id_of(a, entry), (int)(m >> 2) << 4), token = t0 + 16 * (m >> 2);
-            const int8_t *keys = a.k + (((uint64_t)key_id * a.kv_heads + p.h) * B + (token & (B - 1)) + (m & 3)) * D + 16 * g;
+            const int8_t *keys = my_keys + (((uint64_t)key_id * a.kv_heads + p.h) * B + (token & (B - 1))) * D;
             scale = scale_at(a, p, entry);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -435,6 +437,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
                 if (piece == 0) softmax[16 * c + out_row] = Softmax{top, total};
                 continue;
             }
+            const AttendArgs a = args_again();
             const Ending end = ending(a, mode, top, total, softmax[16 * c + out_row]);
             const uint64_t id = row_id(a, p, o);
             for (int part = 0; part < (D + 127) / 128; ++part) {
@@ -531,11 +534,12 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
     const uint32_t B = 1u << a.block_log2;
     uint32_t mode = kAll;
     for (uint32_t tile = p.tile;;) {
-        const uint32_t row = tile * ROWS + wave * 32 + n, rows = p.n * a.group;
-        const Reach reach = reach_of<ROWS>(a, p, tile);
+        const AttendArgs b = args_again();
+        const uint32_t row = tile * ROWS + wave * 32 + n, rows = p.n * b.group;
+        const Reach reach = reach_of<ROWS>(b, p, tile);
         const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
-        if (a.splits > 1 && reach.begin >= reach.end) {
-            nothing_seen<ROWS>(a, p, tile, D);
+        if (b.splits > 1 && reach.begin >= reach.end) {
+            nothing_seen<ROWS>(b, p, tile, D);
             if (done) return;
             ++tile;
             continue;
@@ -549,8 +553,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
             for (int s = 0; s < D / 16; ++s) {
                 w[s] = uint4_t{0, 0, 0, 0};
                 if (row < rows) {
-                    const uint16_t *src = static_cast<const uint16_t *>(a.q) + (uint64_t)(p.begin + row / a.group) * a.q_stride +
-                                          (uint64_t)(p.h * a.group + row % a.group) * D + 16 * s + 8 * hi;
+                    const uint16_t *src = static_cast<const uint16_t *>(b.q) + (uint64_t)(p.begin + row / b.group) * b.q_stride +
+                                          (uint64_t)(p.h * b.group + row % b.group) * D + 16 * s + 8 * hi;
                     w[s] = *reinterpret_cast<const uint4_t *>(src);
                 }
                 most = max(most, piece_most(w[s]));
@@ -564,14 +568,14 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
             for (int s = 0; s < D / 16; ++s) q[s] = query_piece<BF16>(w[s], factor);
         }
         uint32_t from, to;
-        row_sees(a, p, row, from, to);
+        row_sees(b, p, row, from, to);
 
         float16_t acc[D / 32];
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
             for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
         float ref = kNone, weight = 0.0f;
-        bool coarse = false;         // some row's reference is too large for an exponent to be made in one rounding
+        bool coarse = false;         // some row's reference, a finite one, is too large for an exponent to be made in one rounding
 
         // staging: what this thread brings of a tile
         // (a thread's places in a block are the same for all tiles, but for the half of a block of 128 tokens)
@@ -654,7 +658,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
                 loads_among_products<2 * D / 16, 0>();
                 __builtin_amdgcn_s_setprio(0);
                 const bool whole = __ballot(u0 < from || u0 + 64 > to) == 0;
-                const float4_t ks = *reinterpret_cast<const float4_t *>(t.factor + part / 16), lv = *reinterpret_cast<const float4_t *>(t.log_v + part / 16);
+                const float4_t ks = *reinterpret_cast<const float4_t *>(t.factor + part / 16);
+                float4_t lv = *reinterpret_cast<const float4_t *>(t.log_v + part / 16);
                 const float4_t bv = *reinterpret_cast<const float4_t *>(t.back_v + part / 16);
                 if (!whole) {
 #pragma unroll
@@ -674,28 +679,31 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
                     top = fmaxf(top, __builtin_fmaf(m, factor[b], lv[b]));
                 }
                 top = max_across_halves(top);
-                if (__ballot(top > ref + (kRoom + kSlack))) {
+                if (coarse || __ballot(top > ref + (kRoom + kSlack))) {
                     const float now = fmaxf(ref, top - kRoom), down = pow2(ref - now);
                     ref = now;
                     weight *= down;
 #pragma unroll
                     for (int d = 0; d < D / 32; ++d) acc[d] *= down;
-                    coarse = __ballot(fabsf(ref) > kCoarse && ref != kNone) != 0;
+                    coarse = __ballot(fabsf(ref) > kCoarse && fabsf(ref) < -kNone) != 0;
+                    if (coarse) {                        // the reference is rounded: so is, in its row, what it is taken from
+                        const bool here = fabsf(ref) > kCoarse;
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            for (int i = 0; i < 8; ++i) {
+                                const float x = s[b / 2][8 * (b & 1) + i];
+                                s[b / 2][8 * (b & 1) + i] = here ? __builtin_fmaf(x, factor[b], lv[b]) - ref : x;
+                            }
+                            factor[b] = here ? 1.0f : factor[b];
+                            lv[b] = here ? ref : lv[b];
+                        }
+                    }
                 }
                 half8_t pw[4];
-                if (coarse) {                            // (the reference is rounded: so is, in its row, what it is taken from)
-                    const bool here = fabsf(ref) > kCoarse;
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const float off = here ? lv[b] : lv[b] - ref, less = here ? ref : 0.0f;
-                        for (int i = 0; i < 8; ++i) s[b / 2][8 * (b & 1) + i] = pow2(__builtin_fmaf(s[b / 2][8 * (b & 1) + i], factor[b], off) - less);
-                    }
-                } else {
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const float off = lv[b] - ref;
-                        for (int i = 0; i < 8; ++i) s[b / 2][8 * (b & 1) + i] = pow2(__builtin_fmaf(s[b / 2][8 * (b & 1) + i], factor[b], off));
-                    }
+                for (int b = 0; b < 4; ++b) {
+                    const float off = lv[b] - ref;
+                    for (int i = 0; i < 8; ++i) s[b / 2][8 * (b & 1) + i] = pow2(__builtin_fmaf(s[b / 2][8 * (b & 1) + i], factor[b], off));
                 }
                 if (!whole) {                            // (a factor of 0 or NaN has made NaN of -inf)
 #pragma unroll
@@ -744,8 +752,11 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
             const Ending end = ending(a, mode, ref, weight, mine);
             const uint64_t id = row_id(a, p, row);
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d)
-                for (int i = 0; i < 16; ++i) acc[d][i] = acc[d][i] * end.f * end.h * end.h;
+            for (int d = 0; d < D / 32; ++d) acc[d] *= end.f;
+            if (mode == kValues) {
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) acc[d] = acc[d] * end.h * end.h;
+            }
             if (a.splits == 1) {
                 uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)(p.begin + row / a.group) * a.out_stride +
                                 (uint64_t)(p.h * a.group + row % a.group) * D + 4 * hi;
