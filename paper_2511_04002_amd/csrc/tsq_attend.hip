@@ -60,6 +60,10 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
         p.r = x / a.tiles_each;
         p.tile = x % a.tiles_each;
         next = a.tiles_each;
+        if (a.by_tile) {
+            p.r = x % a.requests;
+            p.tile = a.tiles_each - 1 - x / a.requests;
+        }
         if (a.by_length) {
             // the longest request first: p.r counts from the shortest here; each lane ranks one request
             const uint32_t lane = threadIdx.x & 63;
@@ -170,7 +174,7 @@ __device__ __forceinline__ Block block_of(Scale s, float row_factor, uint32_t mo
 }
 struct Softmax { float ref, weight; };                   // of a row, from kScores
 
-// The kernel's arguments, read once more: what only the end of a tile needs then takes no scalar registers in its loop,
+// The kernel's arguments (its only parameter), read once more: what only the end of a tile needs then takes no scalar registers in its loop,
 // where a few too many cost k_attend_many the order of its loads and products (7 % of its time).
 __device__ __forceinline__ AttendArgs args_again() {
     struct Words { uint32_t w[sizeof(AttendArgs) / 4]; } words;
@@ -235,13 +239,18 @@ __device__ __forceinline__ uint64_t row_id(const AttendArgs &a, const Place &p, 
     return (uint64_t)(p.begin + row / a.group) * a.q_heads + p.h * a.group + row % a.group;
 }
 
+// ... and its row of the parts.
+__device__ __forceinline__ uint64_t part_row(const AttendArgs &a, const Place &p, uint32_t row) {
+    return a.slots_each ? ((uint64_t)p.r * a.slots_each + row) * a.kv_heads + p.h : row_id(a, p, row);
+}
+
 // A piece that lies behind a tile's reach: no row sees anything, and that is all that the join has to know (of a weight
 // of NaN, too, whatever the sums are).
 template <int ROWS>
 __device__ __forceinline__ void nothing_seen(const AttendArgs &a, const Place &p, uint32_t tile, int head_dim) {
     const uint32_t row = tile * ROWS + threadIdx.x;
     if (threadIdx.x >= ROWS || row >= p.n * a.group) return;
-    float *st = a.parts + a.part_rows * a.splits * head_dim + (row_id(a, p, row) * a.splits + p.split) * 2;
+    float *st = a.parts + a.part_rows * a.splits * head_dim + (part_row(a, p, row) * a.splits + p.split) * 2;
     st[0] = kNone;
     st[1] = is_lost(a, p, row) ? __builtin_nanf("") : 0.0f;
 }
@@ -439,7 +448,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
             }
             const AttendArgs a = args_again();
             const Ending end = ending(a, mode, top, total, softmax[16 * c + out_row]);
-            const uint64_t id = row_id(a, p, o);
+            const uint64_t id = a.splits == 1 ? row_id(a, p, o) : part_row(a, p, o);
             for (int part = 0; part < (D + 127) / 128; ++part) {
                 constexpr int N = D < 128 ? D : 128;     // elements at a time
                 if (part) __syncthreads();
@@ -799,35 +808,56 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
     __shared__ float4_t sums[WAVES > 1 ? WAVES : 1][LANES];
     __shared__ float totals[WAVES > 1 ? WAVES : 1], tops[WAVES > 1 ? WAVES : 1];
     const uint32_t tid = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint64_t id = (uint64_t)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
-    if (id >= a.part_rows) return;
-    const uint32_t token = (uint32_t)(id / a.q_heads), head = (uint32_t)(id % a.q_heads);
+    uint64_t id = (uint64_t)blockIdx.x * ROWS + (WAVES == 1 ? (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) : 0);
+    // the rows of the first launch, then those of the launch for requests of few rows
+    const uint64_t firsts = a.splits == 1 ? 0 : a.part_rows;
+    const bool of_few = id >= firsts;
+    if (of_few) id -= firsts;
+    const uint64_t part_rows = of_few ? a.few_part_rows : a.part_rows;
+    const uint32_t splits = of_few ? a.few_splits : a.splits;
+    const float *all = of_few ? a.few_parts : a.parts;
+    if (id >= part_rows || splits == 1) return;
     // What most rows have is asked for at once: the first pieces of each lane and their statistics.
     const uint32_t part = tid / LANES, piece = tid % LANES;
-    const float *parts = a.parts + id * a.splits * D + 4 * piece, *stats = a.parts + a.part_rows * a.splits * D + id * a.splits * 2;
+    const float *parts = all + id * splits * D + 4 * piece, *stats = all + part_rows * splits * D + id * splits * 2;
     constexpr int KEPT = 4;
     float4_t v[KEPT];
     float2_t st[KEPT];
 #pragma unroll
     for (int u = 0; u < KEPT; ++u) {
-        const uint32_t i = min(part + u * PIECES, a.splits - 1);
+        const uint32_t i = min(part + u * PIECES, splits - 1);
         st[u] = *reinterpret_cast<const float2_t *>(stats + 2 * i);
         v[u] = *reinterpret_cast<const float4_t *>(parts + (uint64_t)i * D);
     }
-    // rows that no request has were not computed and are not written
-    uint32_t lo = 0, hi = a.requests;
-    while (hi - lo > 1) {                                // a wave halves 64 times at once
-        const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-        const uint64_t below = __ballot(at < hi && a.starts[at] <= (int32_t)token);
-        const uint32_t last = 63 - (uint32_t)__builtin_clzll(below | 1);
-        hi = min(hi, lo + (last + 1) * step);
-        lo += last * step;
+    // rows that no request has, or one of the other launch's, were not computed and are not written
+    uint32_t token, head;
+    if (of_few && a.slots_each) {
+        const uint32_t each = a.slots_each * a.kv_heads, r = (uint32_t)(id / each), slot = (uint32_t)(id % each), row = slot / a.kv_heads;
+        const uint32_t b = min((uint32_t)max(a.starts[r], 0), a.tokens), e = min((uint32_t)max(a.starts[r + 1], 0), a.tokens);
+        const uint32_t rows = e > b ? (e - b) * a.group : 0;
+        if (row >= rows || rows >= a.rows_from) return;
+        token = b + row / a.group;
+        head = slot % a.kv_heads * a.group + row % a.group;
+    } else {
+        token = (uint32_t)(id / a.q_heads);
+        head = (uint32_t)(id % a.q_heads);
+        uint32_t lo = 0, hi = a.requests;
+        while (hi - lo > 1) {                            // a wave halves 64 times at once
+            const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+            const uint64_t below = __ballot(at < hi && a.starts[at] <= (int32_t)token);
+            const uint32_t last = 63 - (uint32_t)__builtin_clzll(below | 1);
+            hi = min(hi, lo + (last + 1) * step);
+            lo += last * step;
+        }
+        const int32_t b = max(a.starts[lo], 0), e = a.starts[lo + 1];
+        if ((int32_t)token < b || (int32_t)token >= e) return;
+        const uint32_t rows = (min((uint32_t)e, a.tokens) - (uint32_t)b) * a.group;
+        if (of_few ? rows >= a.rows_from : rows < a.rows_from) return;
     }
-    if ((int32_t)token < a.starts[lo] || (int32_t)token >= a.starts[lo + 1]) return;
     float top = kNone;
 #pragma unroll
     for (int u = 0; u < KEPT; ++u) top = fmaxf(top, st[u][0]);
-    for (uint32_t i = part + KEPT * PIECES; i < a.splits; i += PIECES) top = fmaxf(top, stats[2 * i]);
+    for (uint32_t i = part + KEPT * PIECES; i < splits; i += PIECES) top = fmaxf(top, stats[2 * i]);
     for (uint32_t d = LANES; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, (int)d));
     if constexpr (WAVES > 1) {
         if (lane == 0) tops[wave] = top;
@@ -844,8 +874,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
     };
 #pragma unroll
     for (int u = 0; u < KEPT; ++u)
-        if (part + u * PIECES < a.splits) add(st[u], v[u]);
-    for (uint32_t i = part + KEPT * PIECES; i < a.splits; i += PIECES)
+        if (part + u * PIECES < splits) add(st[u], v[u]);
+    for (uint32_t i = part + KEPT * PIECES; i < splits; i += PIECES)
         add(*reinterpret_cast<const float2_t *>(stats + 2 * i), *reinterpret_cast<const float4_t *>(parts + (uint64_t)i * D));
     for (uint32_t d = LANES; d < 64; d <<= 1) {
         total += __shfl_xor(total, (int)d);
@@ -864,7 +894,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
     const float f = total == 0.0f ? 0.0f : 1.0f / total;
     uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)token * a.out_stride + (uint64_t)head * D + 4 * piece;
     *reinterpret_cast<uint2_t *>(dst) = uint2_t{narrow2<BF16>(y[0] * f, y[1] * f), narrow2<BF16>(y[2] * f, y[3] * f)};
-    if (a.lse && tid == 0) a.lse[id] = total == 0.0f ? -INFINITY : (top + log2_of(total)) * 0.69314718055994530942f;
+    if (a.lse && tid == 0) a.lse[(uint64_t)token * a.q_heads + head] = total == 0.0f ? -INFINITY : (top + log2_of(total)) * 0.69314718055994530942f;
 }
 
 }  // namespace
@@ -878,10 +908,11 @@ uint32_t few_rows(const CacheShape &s) { return s.head_dim == 256 ? 32 : 64; }
 // they are read once or twice (32 requests of 8192 tokens, 64 heads on 8 of 128, 4 queries each: 140 us in two passes
 // of 16 rows, 202 us by k_attend_many).  k_attend_many takes 256 rows a workgroup, 128 where a request has no more.
 // Pieces: `slots` workgroups run at once.  Fewer units than that leave the device partly idle, so each is cut; a piece
-// costs its start and its share of the join.
+// costs its start and its share of the join.  Each launch has its own number of pieces and its own parts: prompts beside
+// single tokens of long requests stay whole, and only the rows of the second launch have pieces to be joined.
 AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length, uint32_t window) {
-    AttendLaunch l;
-    l.few_tiles = 0;
+    AttendLaunch l = {};
+    l.few_splits = 1;
     const uint64_t group = s.q_heads / s.kv_heads, most = max_new * group, few = few_rows(s);
     auto tile = [&](uint32_t rows) {
         l.rows = rows;
@@ -900,26 +931,49 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
         slots = s.head_dim == 256 || l.rows == 256 ? 256 : 512;
         // Single tokens beside prompts: where the requests have a quarter of the longest one's rows on average, or less, a
         // launch of its own takes those of few rows, and this one the others (one token each of 63 requests of 2000 tokens
-        // and a prompt of 512, 64 heads on 8: 99 us, and 174 all by k_attend_many; 15 of 8000 and 2048, 32 on 8: 144 and
-        // 262; 200 of 500 and 1000, 32 on 32: 279 and 508; 3 of 300 and 200, 32 on 8: 21 and 20).  The launches follow one
-        // another, and both are cut by the pieces of this one: two calls by the caller take 86, 148, 208 and 27 us.
+        // and a prompt of 512, 64 heads on 8: 80 us, and 174 all by k_attend_many; 15 of 8000 and 2048, 32 on 8: 135 and
+        // 262; 200 of 500 and 1000, 32 on 32: 283 and 508; 3 of 300 and 200, 32 on 8: 21 and 20).
         if (requests > 1 && tokens * group * 4 <= requests * most) l.few_tiles = (uint32_t)(few / (s.head_dim == 256 ? 16 : 32)) * requests;
     }
-    uint64_t reach = max_length, least = l.rows >= 128 ? 128 : 256;     // a tile of k_attend_many, one of each wave of k_attend_few
+    uint64_t reach = max_length;
     if (window && reach > (uint64_t)window + max_new) reach = (uint64_t)window + max_new;
-    const uint64_t units = (uint64_t)l.tiles * s.kv_heads, longest = reach <= 256 ? 1 : (reach + least - 1) / least;
-    uint64_t splits = slots / (units ? units : 1);
-    if (splits > longest) splits = longest;
+    auto cut = [&](uint64_t units, uint64_t at_once, bool is_few, uint64_t at_least, uint32_t &splits, uint32_t &chunk) {
+        const uint64_t least = is_few ? 256 : 128;       // a tile of each wave of k_attend_few, one of k_attend_many
+        const uint64_t longest = reach <= 256 ? 1 : (reach + least - 1) / least;
+        uint64_t n = at_once / (units ? units : 1);
+        if (n > longest) n = longest;
+        if (n < at_least) n = at_least;
+        chunk = (uint32_t)(((reach + n - 1) / n + 127) / 128 * 128);
+        if (chunk == 0) chunk = 128;
+        // (pieces of whole tiles may be fewer)
+        splits = (uint32_t)((reach + chunk - 1) / chunk);
+        if (splits == 0) splits = 1;
+    };
     // One request of a batch may be far longer than the others: a piece of k_attend_few has no more than 8192 tokens (63
     // requests of 2000 tokens and one of 131072, 64 heads on 8: 220 us, and 737 in one piece; 64 requests of 32768 each
-    // 739 and 712).
-    if ((l.rows < 128 || l.few_tiles) && splits < (reach + 8191) / 8192) splits = (reach + 8191) / 8192;
-    if (splits == 0) splits = 1;
-    l.chunk = (uint32_t)(((reach + splits - 1) / splits + 127) / 128 * 128);
-    if (l.chunk == 0) l.chunk = 128;
-    // (pieces of whole tiles may be fewer)
-    l.splits = (uint32_t)((reach + l.chunk - 1) / l.chunk);
-    if (l.splits == 0) l.splits = 1;
+    // 739 and 712).  The same holds for k_attend_many beside single tokens, whose tiles end at once there, as long as the
+    // other tiles leave the device partly idle (512 tokens after 32256 beside 62 of 2000: 706 us, and 998 in one piece).
+    const uint64_t units = (uint64_t)l.tiles * s.kv_heads, pieces = (reach + 8191) / 8192;
+    uint64_t at_least = 1;
+    if (l.rows < 128) at_least = pieces;
+    else if (l.few_tiles && tokens > requests) {
+        const uint64_t others = ((uint64_t)(tokens - requests) * group + l.rows - 1) / l.rows * s.kv_heads;
+        at_least = pieces < slots / others ? pieces : slots / others;
+    }
+    cut(units, slots, l.rows < 128, at_least ? at_least : 1, l.splits, l.chunk);
+    l.part_rows = (uint64_t)tokens * s.q_heads;
+    auto bytes = [&](uint64_t rows, uint32_t splits) { return splits == 1 ? 0 : rows * splits * (s.head_dim + 2u) * 4u; };
+    l.workspace = bytes(l.part_rows, l.splits);
+    if (l.few_tiles) {
+        // (one tile a request has rows, where they are single tokens)
+        cut((uint64_t)requests * s.kv_heads, s.head_dim == 256 ? 256 : 512, true, pieces, l.few_splits, l.few_chunk);
+        // as many rows as requests of few rows can have, or as the call has, whichever is less
+        l.few_part_rows = (uint64_t)requests * few * s.kv_heads;
+        l.slots_each = (uint32_t)few;
+        if (l.few_part_rows > l.part_rows) { l.few_part_rows = l.part_rows; l.slots_each = 0; }
+        l.few_at = (l.workspace + 255) / 256 * 256;
+        if (l.few_splits > 1) l.workspace = l.few_at + bytes(l.few_part_rows, l.few_splits);
+    }
     // Requests of several lengths in many more workgroups than run at once: the longest begin first, so that the last
     // ones to end are short (64 requests of 1024 to 4096 tokens on 40 heads, 2560 workgroups: 306 us against 318; with
     // little more than one round the ranking costs more than it brings: 20 requests of 250 to 1000 tokens on 32 heads 29
@@ -945,16 +999,24 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
         f.tiles = l.few_tiles;
         f.tiles_each = l.few_tiles / a.requests;
         f.by_length = 0;
+        // (most requests have one tile: the workgroups of the others, which end at once, would take every other place)
+        f.by_tile = 1;
         f.rows_from = 0;
         f.rows_to = few_rows(s);
-        by_shape(s, [&](auto d, auto bf16) { k_attend_few<d(), bf16(), d() == 256 ? 1 : 2><<<l.few_tiles * l.splits * s.kv_heads, 256, 0, st>>>(f); });
+        f.splits = l.few_splits;
+        f.chunk = l.few_chunk;
+        f.parts = a.few_parts;
+        f.part_rows = a.few_part_rows;
+        f.slots_each = a.slots_each = l.slots_each;
+        by_shape(s, [&](auto d, auto bf16) { k_attend_few<d(), bf16(), d() == 256 ? 1 : 2><<<l.few_tiles * l.few_splits * s.kv_heads, 256, 0, st>>>(f); });
         if (hipError_t e = hipGetLastError()) return (int)e;
     }
-    if (l.splits == 1) return 0;
+    const uint64_t joined = (l.splits > 1 ? l.part_rows : 0) + (l.few_splits > 1 ? l.few_part_rows : 0);
+    if (joined == 0) return 0;
     // a wave reads a few pieces of a row one after the other; more of them want more waves
     by_shape(s, [&](auto d, auto bf16) {
-        if (l.splits <= 16) k_attend_join<d(), bf16(), 1><<<(uint32_t)((a.part_rows + 3) / 4), 256, 0, st>>>(a);
-        else k_attend_join<d(), bf16(), 8><<<(uint32_t)a.part_rows, 512, 0, st>>>(a);
+        if (l.splits <= 16 && l.few_splits <= 16) k_attend_join<d(), bf16(), 1><<<(uint32_t)((joined + 3) / 4), 256, 0, st>>>(a);
+        else k_attend_join<d(), bf16(), 8><<<(uint32_t)joined, 512, 0, st>>>(a);
     });
     return (int)hipGetLastError();
 }

@@ -163,8 +163,7 @@ tsq_status tsq_cache_gather(const tsq_cache *c, const tsq_cache_memory *m, uint3
 size_t tsq_cache_attend_workspace_bytes(const tsq_cache *c, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length,
                                         uint32_t window) {
     if (!c || requests == 0 || tokens == 0) return 0;
-    const AttendLaunch l = attend_launch(c->s, requests, tokens, max_new, max_length, window);
-    return l.splits == 1 ? 0 : (size_t)tokens * c->s.q_heads * l.splits * (c->s.head_dim + 2u) * 4u;
+    return attend_launch(c->s, requests, tokens, max_new, max_length, window).workspace;
 }
 
 tsq_status tsq_cache_attend(const tsq_cache *c, const tsq_cache_memory *m, uint32_t requests, const void *d_table,
@@ -179,9 +178,9 @@ tsq_status tsq_cache_attend(const tsq_cache *c, const tsq_cache_memory *m, uint3
     const uint64_t w = (uint64_t)c->s.q_heads * c->s.head_dim;
     if (bad_rows(d_q, q_stride, w, tokens) || bad_rows(d_out, out_stride, w, tokens)) return TSQ_ERR_INVALID_ARG;
     const AttendLaunch l = attend_launch(c->s, requests, tokens, max_new, max_length, window);
-    if ((uint64_t)l.tiles * l.splits * c->s.kv_heads >= (1ull << 31) || (uint64_t)l.few_tiles * l.splits * c->s.kv_heads >= (1ull << 31))
+    if ((uint64_t)l.tiles * l.splits * c->s.kv_heads >= (1ull << 31) || (uint64_t)l.few_tiles * l.few_splits * c->s.kv_heads >= (1ull << 31))
         return TSQ_ERR_UNSUPPORTED;
-    if (l.splits > 1 && (!d_ws || misaligned(d_ws, 256))) return TSQ_ERR_INVALID_ARG;
+    if (l.workspace && (!d_ws || misaligned(d_ws, 256))) return TSQ_ERR_INVALID_ARG;
     AttendArgs a;
     a.k = static_cast<const int8_t *>(m->d_k); a.v = static_cast<const int8_t *>(m->d_v);
     a.k_scale = static_cast<const float *>(m->d_k_scale); a.v_scale = static_cast<const float *>(m->d_v_scale);
@@ -189,10 +188,12 @@ tsq_status tsq_cache_attend(const tsq_cache *c, const tsq_cache_memory *m, uint3
     a.starts = static_cast<const int32_t *>(d_starts);
     a.lengths = static_cast<const int32_t *>(d_lengths);
     a.q = d_q; a.out = d_out; a.lse = static_cast<float *>(d_lse); a.parts = static_cast<float *>(d_ws);
-    a.q_stride = q_stride; a.out_stride = out_stride; a.part_rows = (uint64_t)tokens * c->s.q_heads;
+    a.q_stride = q_stride; a.out_stride = out_stride; a.part_rows = l.part_rows;
+    a.few_parts = l.few_splits == 1 ? nullptr : reinterpret_cast<float *>(static_cast<char *>(d_ws) + l.few_at);
+    a.few_part_rows = l.few_part_rows; a.few_splits = l.few_splits; a.slots_each = 0;
     a.requests = requests; a.tokens = tokens; a.q_heads = c->s.q_heads; a.kv_heads = c->s.kv_heads;
     a.group = c->s.q_heads / c->s.kv_heads; a.blocks = c->s.blocks; a.block_log2 = c->s.block_log2; a.max_blocks = c->s.max_blocks;
-    a.tiles = l.tiles; a.tiles_each = l.tiles_each; a.splits = l.splits; a.chunk = l.chunk; a.by_length = l.by_length;
+    a.tiles = l.tiles; a.tiles_each = l.tiles_each; a.splits = l.splits; a.chunk = l.chunk; a.by_length = l.by_length; a.by_tile = 0;
     a.rows_from = 0; a.rows_to = ~0u;
     a.window = window; a.causal = causal; a.scale_log2 = scale * 1.44269504088896340736f;
     return hip_rc(launch_attend(c->s, l, a, stream));

@@ -63,12 +63,17 @@ struct AttendArgs {
     const void *q;
     void *out;
     float *lse;
-    float *parts;                // binary32 [tokens * q_heads][splits][head_dim] sums, then [..][splits][2] their maximum and weight
+    float *parts;                // binary32 [part_rows][splits][head_dim] sums, then [..][splits][2] their maximum and weight
     uint64_t q_stride, out_stride, part_rows;
+    float *few_parts;            // the same of the launch for the requests of few rows, for the join of both
+    uint64_t few_part_rows;
+    uint32_t few_splits;         // (1: no join)
+    uint32_t slots_each;         // rows of a kv head that a request has in the parts of that launch; 0: part_rows are rows of the output
     uint32_t requests, tokens, q_heads, kv_heads, group, blocks, block_log2, max_blocks;
-    uint32_t tiles, tiles_each;  // row tiles of the call; of each request, or 0: they follow one another (see find_tile)
+    uint32_t tiles, tiles_each;  // row tiles of the call; of each request, or 0: they follow one another (see find_place)
     uint32_t splits, chunk;      // pieces of a tile's reach along the cache, and the tokens of a piece (a multiple of 128)
     uint32_t by_length;          // the requests' workgroups in the order of their lengths, the longest first (2 .. 64 requests)
+    uint32_t by_tile;            // the requests' first tiles before their second ones
     uint32_t rows_from, rows_to; // a launch is for the requests with so many rows of a kv head: rows_from <= rows <= rows_to
     uint32_t window;
     int32_t causal;
@@ -83,7 +88,12 @@ int launch_gather(const CacheShape &s, const GatherArgs &a, void *stream);
 // launch agree.
 struct AttendLaunch {
     uint32_t rows, tiles, tiles_each, splits, chunk, by_length;
-    uint32_t few_tiles;          // tiles of a second launch, for the requests of few rows among those of many; 0: there is none
+    uint64_t part_rows;
+    // a second launch, for the requests of few rows among those of many, with pieces of its own
+    uint32_t few_tiles;          // 0: there is none
+    uint32_t few_splits, few_chunk, slots_each;
+    uint64_t few_part_rows;
+    uint64_t few_at, workspace;  // bytes: where the second launch's parts begin, and of both
 };
 AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length,
                            uint32_t window);

@@ -157,3 +157,16 @@ def test_attend_of_256_tokens_needs_no_workspace(L):
         for tokens, new in ((1, 1), (7, 7), (256, 256), (5000, 1)):
             assert cache.tsq_cache_attend_workspace_bytes(h, 1, tokens, new, 256) == 0
         cache.tsq_cache_destroy(h)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_attend_workspace_of_single_tokens_beside_a_prompt(L, dim):
+    """The rows of the single tokens have pieces along a long cache, the prompt's have none where it would have none alone."""
+    h = cache.tsq_cache_create(cfg(q_heads=64, kv_heads=8, head_dim=dim))
+    f = cache.tsq_cache_attend_workspace_bytes
+    rows = 64 * 8 * (32 if dim == 256 else 64)               # of 64 requests of as few rows of a kv head as go by themselves
+    for prompt in (512, 4096, 8192, 65536):
+        assert f(h, 1, prompt, prompt, 131072) == 0 or prompt < 4096
+        assert 0 < f(h, 64, 63 + prompt, prompt, 131072) <= rows * 16 * (dim + 2) * 4
+    assert f(h, 64, 63 + 8192, 8192, 8192) == 0              # nothing is long: no pieces
+    cache.tsq_cache_destroy(h)

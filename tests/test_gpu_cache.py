@@ -914,3 +914,25 @@ def test_a_memorys_tensors_are_looked_at_and_not_replaced():
         args[at] = x
         with pytest.raises(ValueError):
             cachelib.Memory(*args)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,counts,lengths", [
+    # parts of the few rows by request (both launches cut, in more than 16 pieces) ...
+    ((1, 1, 64), [1] * 7 + [600], [5000, 3, 4097, 700, 1, 0, 300, 650]),
+    ((4, 2, 256), [1, 17, 2, 16, 0, 1, 300], [4500, 17, 2, 1000, 9, 0, 310]),
+    # ... and by row of the call
+    ((8, 1, 128), [1] * 5 + [8, 9, 2] + [1] * 7 + [40], [3000, 1, 2, 63, 64, 1500, 700, 3, 0, 5, 6, 7, 8, 2500, 10, 60]),
+    # the few rows alone cut
+    ((8, 8, 64), [1] * 19 + [300], [40 * r for r in range(19)] + [1000]),
+])
+def test_attend_single_tokens_beside_a_prompt_in_pieces(dtype, heads, counts, lengths):
+    hq, hk, dim = heads
+    b = Both(sum(-(-n // 16) for n in lengths) + 1, 16, hk, dim, dtype, 320, 92, q_heads=hq)
+    need = cachelib.tsq_cache_attend_workspace_bytes(b.c.handle, len(counts), sum(counts), max(counts), max(lengths))
+    assert need > 0
+    attend_both(b, hq, counts, lengths, extra=2)
+    attend_both(b, hq, counts, lengths, window=600)
+    # announced shorter and longer than they are
+    attend_both(b, hq, counts, lengths, max_length=1100)
+    attend_both(b, hq, counts, lengths, max_length=140000)
