@@ -7,7 +7,8 @@
  *
  * Conventions are those of tsq.h: pointers named d_* are device pointers, `stream` is a hipStream_t as
  * void*, calls only enqueue and never synchronize, errors are return codes, the library allocates no
- * device memory.  Calls keep no state between them: any number of them may run at once on different
+ * device memory.  A call whose kernels would have 2^32 threads or more is TSQ_ERR_UNSUPPORTED, and nothing of it
+ * is enqueued.  Calls keep no state between them: any number of them may run at once on different
  * streams, as long as no two write the same memory.
  *
  * One cache is the keys and values of one layer: `blocks` blocks of `block_tokens` tokens.  A request owns

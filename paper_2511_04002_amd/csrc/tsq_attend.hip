@@ -986,7 +986,13 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
     AttendArgs a = args;
     if (l.few_tiles) a.rows_from = few_rows(s) + 1;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const uint32_t grid = l.tiles * l.splits * s.kv_heads;
+    // the workgroups of the three launches
+    const uint64_t all = (uint64_t)l.tiles * l.splits * s.kv_heads, few = (uint64_t)l.few_tiles * l.few_splits * s.kv_heads;
+    const uint64_t joined = (l.splits > 1 ? l.part_rows : 0) + (l.few_splits > 1 ? l.few_part_rows : 0);
+    // (a wave reads a few pieces of a row one after the other; more of them want more waves)
+    const bool one_wave = l.splits <= 16 && l.few_splits <= 16;
+    if (!fits(all, l.rows == 256 ? 512 : 256) || !fits(few, 256) || !(one_wave ? fits((joined + 3) / 4, 256) : fits(joined, 512))) return kTooLarge;
+    const uint32_t grid = (uint32_t)all;
     by_shape(s, [&](auto d, auto bf16) {
         if (l.rows == 16) k_attend_few<d(), bf16(), 1><<<grid, 256, 0, st>>>(a);
         else if (l.rows == 32) { if constexpr (d() != 256) k_attend_few<d(), bf16(), 2><<<grid, 256, 0, st>>>(a); }
@@ -1008,14 +1014,12 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
         f.parts = a.few_parts;
         f.part_rows = a.few_part_rows;
         f.slots_each = a.slots_each = l.slots_each;
-        by_shape(s, [&](auto d, auto bf16) { k_attend_few<d(), bf16(), d() == 256 ? 1 : 2><<<l.few_tiles * l.few_splits * s.kv_heads, 256, 0, st>>>(f); });
+        by_shape(s, [&](auto d, auto bf16) { k_attend_few<d(), bf16(), d() == 256 ? 1 : 2><<<(uint32_t)few, 256, 0, st>>>(f); });
         if (hipError_t e = hipGetLastError()) return (int)e;
     }
-    const uint64_t joined = (l.splits > 1 ? l.part_rows : 0) + (l.few_splits > 1 ? l.few_part_rows : 0);
     if (joined == 0) return 0;
-    // a wave reads a few pieces of a row one after the other; more of them want more waves
     by_shape(s, [&](auto d, auto bf16) {
-        if (l.splits <= 16 && l.few_splits <= 16) k_attend_join<d(), bf16(), 1><<<(uint32_t)((joined + 3) / 4), 256, 0, st>>>(a);
+        if (one_wave) k_attend_join<d(), bf16(), 1><<<(uint32_t)((joined + 3) / 4), 256, 0, st>>>(a);
         else k_attend_join<d(), bf16(), 8><<<(uint32_t)joined, 512, 0, st>>>(a);
     });
     return (int)hipGetLastError();

@@ -16,7 +16,7 @@ struct tsq_cache {
 
 namespace {
 
-tsq_status hip_rc(int e) { return e == 0 ? TSQ_OK : TSQ_ERR_HIP; }
+tsq_status hip_rc(int e) { return e == 0 ? TSQ_OK : e == kTooLarge ? TSQ_ERR_UNSUPPORTED : TSQ_ERR_HIP; }
 bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 // rows of 16-bit elements: 16-byte aligned, a stride of whole 16-byte pieces that holds a row (any for one row)
@@ -178,8 +178,6 @@ tsq_status tsq_cache_attend(const tsq_cache *c, const tsq_cache_memory *m, uint3
     const uint64_t w = (uint64_t)c->s.q_heads * c->s.head_dim;
     if (bad_rows(d_q, q_stride, w, tokens) || bad_rows(d_out, out_stride, w, tokens)) return TSQ_ERR_INVALID_ARG;
     const AttendLaunch l = attend_launch(c->s, requests, tokens, max_new, max_length, window);
-    if ((uint64_t)l.tiles * l.splits * c->s.kv_heads >= (1ull << 31) || (uint64_t)l.few_tiles * l.few_splits * c->s.kv_heads >= (1ull << 31))
-        return TSQ_ERR_UNSUPPORTED;
     if (l.workspace && (!d_ws || misaligned(d_ws, 256))) return TSQ_ERR_INVALID_ARG;
     AttendArgs a;
     a.k = static_cast<const int8_t *>(m->d_k); a.v = static_cast<const int8_t *>(m->d_v);

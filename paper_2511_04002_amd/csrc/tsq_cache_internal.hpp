@@ -80,6 +80,10 @@ struct AttendArgs {
     float scale_log2;            // scale * log2(e)
 };
 
+// A launch counts its threads in 32 bits: one of more is refused before anything is enqueued.
+constexpr int kTooLarge = -1;    // what the functions below return then; 0, or a hipError_t, in all other cases
+inline bool fits(uint64_t workgroups, uint32_t threads) { return workgroups * threads < (1ull << 32); }
+
 int launch_schedule(const ScheduleArgs &a, void *stream);
 int launch_norm_rotate(const CacheShape &s, const NormRotateArgs &a, void *stream);
 int launch_append(const CacheShape &s, const AppendArgs &a, void *stream);

@@ -764,10 +764,10 @@ __global__ __launch_bounds__(256) void k_gather(GatherArgs a) {
     }
 }
 
-// A grid of n waves in workgroups of four; 2^31 workgroups and more are refused.
+// A grid of n waves in workgroups of four.
 int workgroups(uint64_t waves, uint32_t *out) {
     const uint64_t n = (waves + 3) / 4;
-    if (n >= (1ull << 31)) return (int)hipErrorInvalidValue;
+    if (!fits(n, 256)) return kTooLarge;
     *out = (uint32_t)n;
     return 0;
 }
@@ -819,7 +819,7 @@ int launch_gather(const CacheShape &s, const GatherArgs &args, void *stream) {
     uint64_t each = (4096 + groups - 1) / groups;
     if (each > s.kv_heads) each = s.kv_heads;
     a.waves_each = (uint32_t)each;
-    if (groups * each >= (1ull << 31)) return (int)hipErrorInvalidValue;
+    if (!fits(groups * each, 256)) return kTooLarge;
     by_shape(s, [&](auto d, auto bf16) { k_gather<d(), bf16()><<<(uint32_t)(groups * each), 256, 0, static_cast<hipStream_t>(stream)>>>(a); });
     return (int)hipGetLastError();
 }

@@ -171,3 +171,29 @@ def test_attend_workspace_of_single_tokens_beside_a_prompt(L, dim):
         assert 0 < f(h, 64, 63 + prompt, prompt, 131072) <= rows * 16 * (dim + 2) * 4 + alone * (63 + prompt) // prompt + 256
     assert f(h, 64, 63 + 8192, 8192, 8192) == 0              # nothing is long: no pieces
     cache.tsq_cache_destroy(h)
+
+
+def test_calls_of_too_many_threads_are_refused_before_anything_is_enqueued(L):
+    """2^32 threads, in each of the kernels that a call may need, the last one of an attend call among them."""
+    def made(**kw):
+        return cache.tsq_cache_create(cfg(**{**dict(q_heads=1, kv_heads=1, head_dim=64), **kw}))
+
+    h = made()
+    n = 1 << 26
+    assert L.tsq_cache_norm_rotate(h, n, 0x1000, 64, 0x2000, 64, 0x3000, 0x4000, 9, 64, 0, None, None, 1e-6, 0x5000, 64, 0x6000, 64, None) == UNS
+    n = 1 << 30
+    assert L.tsq_cache_append(h, memory(), n, 0x1000, 64, 0x2000, 64, 0x3000, None) == UNS
+    assert L.tsq_cache_gather(h, memory(), 2, 0x1000, 0x2000, 0x3000, n, 0x4000, 64, 0x5000, 64, None) == UNS
+    cache.tsq_cache_destroy(h)
+
+    def attend(h, requests, tokens, max_new, max_length, width):
+        return L.tsq_cache_attend(h, memory(), requests, 0x1000, 0x2000, 0x3000, tokens, max_new, max_length, 0x4000, width, 0.1, 1, 0, 0x5000, width,
+                                  None, 0x10000, None)
+
+    for heads, requests, tokens, new, length in ((1024, 16384, 16384, 1, 64), (1024, 65535, 1 << 17, 1 << 17, 64)):
+        h = made(q_heads=heads, kv_heads=heads)
+        assert attend(h, requests, tokens, new, length, heads * 64) == UNS
+        cache.tsq_cache_destroy(h)
+    h = made(q_heads=64, head_dim=128)                       # the join: 2^23 rows of 512 threads
+    assert attend(h, 65535, 1 << 17, 1, 140000, 64 * 128) == UNS
+    cache.tsq_cache_destroy(h)
