@@ -935,7 +935,7 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
         // 262; 200 of 500 and 1000, 32 on 32: 283 and 508; 3 of 300 and 200, 32 on 8: 21 and 20).
         if (requests > 1 && tokens * group * 4 <= requests * most) l.few_tiles = (uint32_t)(few / (s.head_dim == 256 ? 16 : 32)) * requests;
     }
-    uint64_t reach = max_length;
+    uint64_t reach = max_length < 0x7FFFFFFFu ? max_length : 0x7FFFFFFFu;     // (no request is longer, and a piece's tokens are 32 bits)
     if (window && reach > (uint64_t)window + max_new) reach = (uint64_t)window + max_new;
     auto cut = [&](uint64_t units, uint64_t at_once, bool is_few, uint64_t at_least, uint32_t &splits, uint32_t &chunk) {
         const uint64_t least = is_few ? 256 : 128;       // a tile of each wave of k_attend_few, one of k_attend_many
@@ -944,7 +944,7 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
         if (n > longest) n = longest;
         if (n < at_least) n = at_least;
         chunk = (uint32_t)(((reach + n - 1) / n + 127) / 128 * 128);
-        if (chunk == 0) chunk = 128;
+        if (chunk == 0) chunk = 128;                     // (reach 0)
         // (pieces of whole tiles may be fewer)
         splits = (uint32_t)((reach + chunk - 1) / chunk);
         if (splits == 0) splits = 1;

@@ -197,3 +197,13 @@ def test_calls_of_too_many_threads_are_refused_before_anything_is_enqueued(L):
     h = made(q_heads=64, head_dim=128)                       # the join: 2^23 rows of 512 threads
     assert attend(h, 65535, 1 << 17, 1, 140000, 64 * 128) == UNS
     cache.tsq_cache_destroy(h)
+
+
+def test_attend_workspace_of_a_length_that_no_request_can_have(L):
+    f = cache.tsq_cache_attend_workspace_bytes
+    h = cache.tsq_cache_create(cfg(q_heads=64, kv_heads=8))
+    for requests, tokens, new in ((1, 8192, 8192), (1, 1, 1), (64, 64, 1), (64, 1000, 900)):
+        for length in (2 ** 31, 2 ** 32 - 128, 2 ** 32 - 1):
+            assert f(h, requests, tokens, new, length) == f(h, requests, tokens, new, 2 ** 31 - 1)
+    assert f(h, 1, 8192, 8192, 2 ** 32 - 1) == 0
+    cache.tsq_cache_destroy(h)
