@@ -22,6 +22,7 @@ from . import tsq
 from .tsq import TSQ_OK, TsqError
 
 TSQ_PAIRS_HALVES, TSQ_PAIRS_NEIGHBOURS = 0, 1
+_MOST = 2 ** 32 - 1                                       # (ctypes passes the lower 32 bits of what is larger)
 
 EXPORTS = ("tsq_cache_create", "tsq_cache_destroy", "tsq_cache_memory_sizes", "tsq_cache_schedule", "tsq_cache_norm_rotate",
            "tsq_cache_append", "tsq_cache_gather", "tsq_cache_attend", "tsq_cache_attend_workspace_bytes")
@@ -168,8 +169,9 @@ class Cache:
         import torch
         if dtype not in tsq._DTYPES:
             _refuse("dtype is 'f16' or 'bf16'")
-        if min(blocks, block_tokens, q_heads, kv_heads, head_dim, max_blocks) < 0:
-            _refuse("a cache's numbers are not negative")
+        numbers = (blocks, block_tokens, q_heads, kv_heads, head_dim, max_blocks)
+        if min(numbers) < 0 or max(numbers) > _MOST:
+            _refuse("a cache's numbers are not negative, and have 32 bits")
         self.kind = torch.float16 if dtype == "f16" else torch.bfloat16
         self.int32, self.int64, self.float32 = torch.int32, torch.int64, torch.float32
         self.blocks, self.block_tokens, self.q_heads, self.kv_heads = blocks, block_tokens, q_heads, kv_heads
@@ -337,7 +339,7 @@ class Cache:
 
     def new_workspace(self, requests: int, tokens: int, max_new: int, max_length: int, window: int = 0):
         """A workspace for attend calls of these numbers on one stream; None where they need none."""
-        n = tsq_cache_attend_workspace_bytes(self.handle, requests, tokens, max_new, max_length, window)
+        n = tsq_cache_attend_workspace_bytes(self.handle, requests, tokens, min(max_new, _MOST), min(max_length, _MOST), min(window, _MOST))
         return self._empty(n, self._torch.uint8) if n else None
 
     def attend(self, memory: Memory, q, table, starts, lengths, max_new: int, max_length: int, scale=None, causal: bool = True,
@@ -355,6 +357,8 @@ class Cache:
             lp = lse.data_ptr()
         if max_new < 0 or max_length < 0 or window < 0:
             _refuse("max_new, max_length and window are not negative")
+        # (no request is as long: what is larger says the same)
+        max_new, max_length, window = min(max_new, _MOST), min(max_length, _MOST), min(window, _MOST)
         L, wp = self._lib, None
         # (256 tokens are never cut, and then there is no workspace)
         need = 0 if max_length <= 256 else L.tsq_cache_attend_workspace_bytes(self.handle, n, tokens, max_new, max_length, window)

@@ -207,3 +207,12 @@ def test_attend_workspace_of_a_length_that_no_request_can_have(L):
             assert f(h, requests, tokens, new, length) == f(h, requests, tokens, new, 2 ** 31 - 1)
     assert f(h, 1, 8192, 8192, 2 ** 32 - 1) == 0
     cache.tsq_cache_destroy(h)
+
+
+@pytest.mark.parametrize("at", range(6))
+def test_cache_numbers_past_32_bits_are_refused(L, at):
+    numbers = [4, 16, 4, 2, 64, 2]
+    cache.Cache(*numbers[:5], "f16", numbers[5])
+    numbers[at] += 2 ** 32
+    with pytest.raises(ValueError):
+        cache.Cache(*numbers[:5], "f16", numbers[5])

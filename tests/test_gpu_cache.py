@@ -936,3 +936,9 @@ def test_attend_single_tokens_beside_a_prompt_in_pieces(dtype, heads, counts, le
     # announced shorter and longer than they are
     attend_both(b, hq, counts, lengths, max_length=1100)
     attend_both(b, hq, counts, lengths, max_length=140000)
+
+
+def test_attend_of_a_window_past_32_bits_sees_everything():
+    b = Both(20, 16, 1, 64, "f16", 20, 93, q_heads=2)
+    for counts, lengths in (([1, 2], [100, 200]), ([90, 1], [120, 60])):
+        attend_both(b, 2, counts, lengths, window=2 ** 32 + 5, max_new=2 ** 32 + max(counts), max_length=2 ** 32)
