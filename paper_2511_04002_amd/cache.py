@@ -12,7 +12,7 @@ A step of one layer, for requests of any lengths, new or going on:
     out = c.attend(memory, q, table, s.starts, s.lengths, max_new, max_length)
     lengths, counters = s.lengths, s.counters         # what the next step begins with
 
-All calls run on torch's current stream.  A tensor that is left out is allocated on it.
+All calls run on torch's current stream, and their tensors are on its device.  A tensor that is left out is allocated on it.
 """
 from __future__ import annotations
 
@@ -126,11 +126,12 @@ class Memory:
         import torch
         shape = tuple(k.shape)
         n, h, b, d = shape if len(shape) == 4 else (0, 0, 0, 0)
+        device = k.get_device()
         for x, size, kind in ((k, (n, h, b, d), torch.int8), (v, (n, h, d, b), torch.int8), (k_scale, (n, h), torch.float32), (v_scale, (n, h), torch.float32)):
-            if not (x.is_cuda and x.is_contiguous() and tuple(x.shape) == size and x.dtype == kind):
-                _refuse("a cache's tensor is %s on the GPU, contiguous, %s" % (size, kind))
+            if not (x.is_cuda and x.get_device() == device and x.is_contiguous() and tuple(x.shape) == size and x.dtype == kind):
+                _refuse("a cache's tensor is %s on one GPU, contiguous, %s" % (size, kind))
         c = tsq_cache_memory(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
-        self.__dict__.update(k=k, v=v, k_scale=k_scale, v_scale=v_scale, shape=shape, c=c, ref=C.byref(c))
+        self.__dict__.update(k=k, v=v, k_scale=k_scale, v_scale=v_scale, shape=shape, device=device, c=c, ref=C.byref(c))
 
     def __setattr__(self, name, value):
         raise AttributeError("a memory's tensors are not replaced")
@@ -142,13 +143,13 @@ class Schedule:
 
     def __init__(self, lengths, counters, starts, positions, slots, status):
         import torch
-        n, capacity = lengths.numel(), slots.numel()
+        n, capacity, device = lengths.numel(), slots.numel(), lengths.get_device()
         for x, kind, size in ((lengths, torch.int32, n), (counters, torch.int64, 2), (starts, torch.int32, n + 1), (positions, torch.int32, capacity),
                               (slots, torch.int32, capacity), (status, torch.int32, 1)):
-            if not (x.is_cuda and x.is_contiguous() and x.dtype is kind and x.numel() == size):
+            if not (x.is_cuda and x.get_device() == device and x.is_contiguous() and x.dtype is kind and x.numel() == size):
                 _refuse("a schedule's tensors are those of Cache.new_schedule")
         self.__dict__.update(lengths=lengths, counters=counters, starts=starts, positions=positions, slots=slots, status=status, requests=n,
-                             capacity=capacity, pointers=tuple(x.data_ptr() for x in (lengths, counters, starts, positions, slots, status)))
+                             capacity=capacity, device=device, pointers=tuple(x.data_ptr() for x in (lengths, counters, starts, positions, slots, status)))
 
     def __setattr__(self, name, value):
         raise AttributeError("a schedule's tensors are not replaced")
@@ -160,6 +161,21 @@ class Schedule:
 
 def _refuse(what: str):
     raise ValueError(what)
+
+
+_get_device = None
+
+
+def _device() -> int:
+    """Number of the current device, whose stream the calls use (-2 where there is none: no tensor is there)."""
+    global _get_device
+    if _get_device is None:
+        import torch
+        _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    try:
+        return _get_device()
+    except RuntimeError:
+        return -2
 
 
 class Cache:
@@ -206,7 +222,7 @@ class Cache:
         """A cache in tensors that are there: k [blocks, kv_heads, block_tokens, head_dim] int8,
         v [blocks, kv_heads, head_dim, block_tokens] int8, scales [blocks, kv_heads] float32."""
         memory = Memory(k, v, k_scale, v_scale)
-        self._memory(memory)
+        self._memory(memory, memory.device)
         return memory
 
     def new_table(self, requests: int):
@@ -228,48 +244,51 @@ class Cache:
     # -------------------------------------------------------------- checks
 
     # (a step calls these for every tensor of every operator: what a tensor holds is told by its type, place and number
-    # of elements, and its shape is looked at only where it is not contiguous)
+    # of elements, and its shape is looked at only where it is not contiguous; `device` is the current one)
 
-    def _memory(self, memory):
+    def _memory(self, memory, device):
+        if memory.device != device:
+            _refuse("the memory is on another device than the current one")
         if memory.shape != self.shape:
             _refuse("the memory is that of a cache of %s, this one is %s (blocks, kv_heads, block_tokens, head_dim)" % (memory.shape, self.shape))
         return memory.ref
 
-    def _ints(self, x, n, what):
-        if not (x.dtype is self.int32 and x.is_cuda and x.is_contiguous() and x.numel() == n):
-            _refuse("%s is int32 on the GPU, contiguous, %d elements" % (what, n))
+    def _ints(self, x, n, what, device):
+        if not (x.dtype is self.int32 and x.get_device() == device and x.is_contiguous() and x.numel() == n):
+            _refuse("%s is int32 on the current GPU, contiguous, %d elements" % (what, n))
         return x.data_ptr()
 
-    def _requests(self, table, starts, lengths, n):
+    def _requests(self, table, starts, lengths, n, device):
         i32 = self.int32
-        if not (table.dtype is i32 and starts.dtype is i32 and lengths.dtype is i32 and table.is_cuda and starts.is_cuda and lengths.is_cuda and
+        if not (table.dtype is i32 and starts.dtype is i32 and lengths.dtype is i32 and
+                table.get_device() == device and starts.get_device() == device and lengths.get_device() == device and
                 table.is_contiguous() and starts.is_contiguous() and lengths.is_contiguous() and
                 table.numel() == n * self.max_blocks and starts.numel() == n + 1):
-            _refuse("table, starts and lengths are int32 on the GPU, contiguous, [%d, %d], [%d] and [%d]" % (n, self.max_blocks, n + 1, n))
+            _refuse("table, starts and lengths are int32 on the current GPU, contiguous, [%d, %d], [%d] and [%d]" % (n, self.max_blocks, n + 1, n))
         return table.data_ptr(), starts.data_ptr(), lengths.data_ptr()
 
-    def _rows(self, x, tokens, heads, what):
+    def _rows(self, x, tokens, heads, what, device):
         """x: [tokens, heads, head_dim], or [tokens, heads * head_dim]; rows anywhere, the heads of a row together.
         -> pointer, elements from row to row."""
         width = heads * self.head_dim
-        if x.dtype is self.kind and x.is_cuda and x.numel() == tokens * width:
+        if x.dtype is self.kind and x.get_device() == device and x.numel() == tokens * width:
             if x.is_contiguous():
                 return x.data_ptr(), width
             shape, stride = x.shape, x.stride()
             if shape[0] == tokens and ((len(shape) == 3 and shape[1] == heads and stride[2] == 1 and (heads == 1 or stride[1] == self.head_dim)) or
                                        (len(shape) == 2 and stride[1] == 1)):
                 return x.data_ptr(), (stride[0] if tokens > 1 else width)
-        _refuse("%s is [%d, %d, %d] of %s on the GPU, the heads of a row together" % (what, tokens, heads, self.head_dim, self.kind))
+        _refuse("%s is [%d, %d, %d] of %s on the current GPU, the heads of a row together" % (what, tokens, heads, self.head_dim, self.kind))
 
-    def _into(self, x, tokens, heads, what):
+    def _into(self, x, tokens, heads, what, device):
         x = self._empty((tokens, heads, self.head_dim), self.kind) if x is None else x
-        return (x,) + self._rows(x, tokens, heads, what)
+        return (x,) + self._rows(x, tokens, heads, what, device)
 
-    def _weight(self, w):
+    def _weight(self, w, device):
         if w is None:
             return None
-        if not (w.dtype is self.kind and w.is_cuda and w.is_contiguous() and w.numel() == self.head_dim):
-            _refuse("a norm's weight is [head_dim] of the cache's dtype on the GPU, contiguous")
+        if not (w.dtype is self.kind and w.get_device() == device and w.is_contiguous() and w.numel() == self.head_dim):
+            _refuse("a norm's weight is [head_dim] of the cache's dtype on the current GPU, contiguous")
         return w.data_ptr()
 
     # -------------------------------------------------------------- the operators
@@ -278,13 +297,14 @@ class Cache:
         """Block tables, slots and positions of a step: new [requests] int32 new tokens of each request (-1: done),
         lengths [requests] int32 what it has.  table and ring are updated; the rest is written to `out`
         (from new_schedule(requests, most new tokens of a step))."""
-        n, i32 = new.numel(), self.int32
+        n, i32, device = new.numel(), self.int32, _device()
         if not (new.dtype is i32 and lengths.dtype is i32 and table.dtype is i32 and ring.dtype is i32 and counters.dtype is self.int64 and
-                new.is_cuda and lengths.is_cuda and table.is_cuda and ring.is_cuda and counters.is_cuda and
+                new.get_device() == device and lengths.get_device() == device and table.get_device() == device and ring.get_device() == device and
+                counters.get_device() == device and out.device == device and
                 new.is_contiguous() and lengths.is_contiguous() and table.is_contiguous() and ring.is_contiguous() and counters.is_contiguous() and
                 lengths.numel() == n and table.numel() == n * self.max_blocks and ring.numel() == self.blocks and counters.numel() == 2 and
                 out.requests == n):
-            _refuse("on the GPU and contiguous: new, lengths int32 [%d], table int32 [%d, %d], ring int32 [%d], counters int64 [2], and a "
+            _refuse("on the current GPU and contiguous: new, lengths int32 [%d], table int32 [%d, %d], ring int32 [%d], counters int64 [2], and a "
                     "schedule of as many requests" % (n, n, self.max_blocks, self.blocks))
         status = self._lib.tsq_cache_schedule(self.handle, n, new.data_ptr(), lengths.data_ptr(), table.data_ptr(), ring.data_ptr(),
                                               counters.data_ptr(), out.capacity, *out.pointers, self._stream())
@@ -297,42 +317,42 @@ class Cache:
         """RMS norm of each head of q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim] (weights [head_dim],
         or None: no norm), then the rotation by position: angles [rows, rotary] float32 holds the cosines of a
         position's rotary / 2 angles, then their sines.  q_out, k_out may be q, k themselves."""
-        tokens = q.shape[0]
-        qp, qs = self._rows(q, tokens, self.q_heads, "q")
-        kp, ks = self._rows(k, tokens, self.kv_heads, "k")
-        q_out, qo, qos = self._into(q_out, tokens, self.q_heads, "q_out")
-        k_out, ko, kos = self._into(k_out, tokens, self.kv_heads, "k_out")
-        if not (angles.dtype is self.float32 and angles.is_cuda and angles.is_contiguous() and angles.dim() == 2):
-            _refuse("angles is float32 [rows, rotary] on the GPU, contiguous")
+        tokens, device = q.shape[0], _device()
+        qp, qs = self._rows(q, tokens, self.q_heads, "q", device)
+        kp, ks = self._rows(k, tokens, self.kv_heads, "k", device)
+        q_out, qo, qos = self._into(q_out, tokens, self.q_heads, "q_out", device)
+        k_out, ko, kos = self._into(k_out, tokens, self.kv_heads, "k_out", device)
+        if not (angles.dtype is self.float32 and angles.get_device() == device and angles.is_contiguous() and angles.dim() == 2):
+            _refuse("angles is float32 [rows, rotary] on the current GPU, contiguous")
         if pairs != "halves" and pairs != "neighbours":
             _refuse("pairs is 'halves' or 'neighbours'")
         known, rotary = angles.shape
         status = self._lib.tsq_cache_norm_rotate(
-            self.handle, tokens, qp, qs, kp, ks, self._ints(positions, tokens, "positions"), angles.data_ptr(), known, rotary,
-            TSQ_PAIRS_HALVES if pairs == "halves" else TSQ_PAIRS_NEIGHBOURS, self._weight(q_weight), self._weight(k_weight), eps,
-            qo, qos, ko, kos, self._stream())
+            self.handle, tokens, qp, qs, kp, ks, self._ints(positions, tokens, "positions", device), angles.data_ptr(), known, rotary,
+            TSQ_PAIRS_HALVES if pairs == "halves" else TSQ_PAIRS_NEIGHBOURS, self._weight(q_weight, device), self._weight(k_weight, device),
+            eps, qo, qos, ko, kos, self._stream())
         if status:
             raise TsqError(status, "tsq_cache_norm_rotate")
         return q_out, k_out
 
     def append(self, memory: Memory, k, v, slots) -> None:
         """Stores k and v [tokens, kv_heads, head_dim] at slots [tokens] int32 (from a schedule; -1: not stored)."""
-        tokens = k.shape[0]
-        kp, ks = self._rows(k, tokens, self.kv_heads, "k")
-        vp, vs = self._rows(v, tokens, self.kv_heads, "v")
-        status = self._lib.tsq_cache_append(self.handle, self._memory(memory), tokens, kp, ks, vp, vs, self._ints(slots, tokens, "slots"),
-                                            self._stream())
+        tokens, device = k.shape[0], _device()
+        kp, ks = self._rows(k, tokens, self.kv_heads, "k", device)
+        vp, vs = self._rows(v, tokens, self.kv_heads, "v", device)
+        status = self._lib.tsq_cache_append(self.handle, self._memory(memory, device), tokens, kp, ks, vp, vs,
+                                            self._ints(slots, tokens, "slots", device), self._stream())
         if status:
             raise TsqError(status, "tsq_cache_append")
 
     def gather(self, memory: Memory, table, starts, lengths, k_out, v_out):
         """The last starts[r + 1] - starts[r] tokens of each request r, up to lengths[r], into rows starts[r] ... of k_out
         and v_out [tokens, kv_heads, head_dim] (or [tokens, kv_heads * head_dim], as Plan.compress_batch takes them)."""
-        tokens, n = k_out.shape[0], lengths.numel()
-        kp, ks = self._rows(k_out, tokens, self.kv_heads, "k_out")
-        vp, vs = self._rows(v_out, tokens, self.kv_heads, "v_out")
-        status = self._lib.tsq_cache_gather(self.handle, self._memory(memory), n, *self._requests(table, starts, lengths, n), tokens, kp, ks, vp, vs,
-                                            self._stream())
+        tokens, n, device = k_out.shape[0], lengths.numel(), _device()
+        kp, ks = self._rows(k_out, tokens, self.kv_heads, "k_out", device)
+        vp, vs = self._rows(v_out, tokens, self.kv_heads, "v_out", device)
+        status = self._lib.tsq_cache_gather(self.handle, self._memory(memory, device), n, *self._requests(table, starts, lengths, n, device), tokens,
+                                            kp, ks, vp, vs, self._stream())
         if status:
             raise TsqError(status, "tsq_cache_gather")
         return k_out, v_out
@@ -347,13 +367,13 @@ class Cache:
         """Attention of q [tokens, q_heads, head_dim] over the cache: rows starts[r] .. starts[r + 1] - 1 are the last tokens of
         request r, which has lengths[r] in the cache.  max_new, max_length: the largest of both over the requests (how the
         work is split goes by them).  scale: 1 / sqrt(head_dim) if left out.  lse: float32 [tokens, q_heads] to be written."""
-        tokens, n = q.shape[0], lengths.numel()
-        qp, qs = self._rows(q, tokens, self.q_heads, "q")
-        out, op, os_ = self._into(out, tokens, self.q_heads, "out")
+        tokens, n, device = q.shape[0], lengths.numel(), _device()
+        qp, qs = self._rows(q, tokens, self.q_heads, "q", device)
+        out, op, os_ = self._into(out, tokens, self.q_heads, "out", device)
         lp = None
         if lse is not None:
-            if not (lse.dtype is self.float32 and lse.is_cuda and lse.is_contiguous() and lse.numel() == tokens * self.q_heads):
-                _refuse("lse is float32 [tokens, q_heads] on the GPU, contiguous")
+            if not (lse.dtype is self.float32 and lse.get_device() == device and lse.is_contiguous() and lse.numel() == tokens * self.q_heads):
+                _refuse("lse is float32 [tokens, q_heads] on the current GPU, contiguous")
             lp = lse.data_ptr()
         if max_new < 0 or max_length < 0 or window < 0:
             _refuse("max_new, max_length and window are not negative")
@@ -365,11 +385,11 @@ class Cache:
         if need:
             if ws is None:
                 ws = self._empty(need, self._torch.uint8)
-            if not (ws.is_cuda and ws.is_contiguous() and ws.numel() * ws.element_size() >= need):
-                _refuse("ws has %d bytes on the GPU, contiguous" % need)
+            if not (ws.get_device() == device and ws.is_contiguous() and ws.numel() * ws.element_size() >= need):
+                _refuse("ws has %d bytes on the current GPU, contiguous" % need)
             wp = ws.data_ptr()
         status = L.tsq_cache_attend(
-            self.handle, self._memory(memory), n, *self._requests(table, starts, lengths, n), tokens, max_new, max_length, qp, qs,
+            self.handle, self._memory(memory, device), n, *self._requests(table, starts, lengths, n, device), tokens, max_new, max_length, qp, qs,
             self.head_dim ** -0.5 if scale is None else scale, causal, window, op, os_, lp, wp, self._stream())
         if status:
             raise TsqError(status, "tsq_cache_attend")

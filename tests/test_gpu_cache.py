@@ -942,3 +942,21 @@ def test_attend_of_a_window_past_32_bits_sees_everything():
     b = Both(20, 16, 1, 64, "f16", 20, 93, q_heads=2)
     for counts, lengths in (([1, 2], [100, 200]), ([90, 1], [120, 60])):
         attend_both(b, 2, counts, lengths, window=2 ** 32 + 5, max_new=2 ** 32 + max(counts), max_length=2 ** 32)
+
+
+@pytest.mark.parametrize("call", ["norm_rotate", "append", "gather", "attend", "schedule"])
+def test_tensors_on_another_device_than_the_current_one_are_refused(call, monkeypatch):
+    c = cachelib.Cache(4, 16, 4, 2, 128, "f16", 2)
+    m = c.new_memory()
+    h = lambda *s: torch.zeros(s, dtype=torch.float16, device="cuda")        # noqa: E731
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")          # noqa: E731
+    args = dict(norm_rotate=[h(3, 4, 128), h(3, 2, 128), i(3), torch.zeros((9, 128), device="cuda")],
+                append=[m, h(3, 2, 128), h(3, 2, 128), i(3) - 1],
+                gather=[m, i(2, 2), i(3), i(2), h(3, 2, 128), h(3, 2, 128)],
+                attend=[m, h(3, 4, 128), i(2, 2), i(3), i(2), 2, 9],
+                schedule=[i(2), i(2), i(2, 2), i(4), c.new_counters(), c.new_schedule(2, 5)])[call]
+    getattr(c, call)(*args)
+    # as if another device had been made the current one
+    monkeypatch.setattr(cachelib, "_device", lambda: torch.cuda.current_device() + 1)
+    with pytest.raises(ValueError, match="current"):
+        getattr(c, call)(*args)
