@@ -163,19 +163,12 @@ def _refuse(what: str):
     raise ValueError(what)
 
 
-_get_device = None
-
-
 def _device() -> int:
-    """Number of the current device, whose stream the calls use (-2 where there is none: no tensor is there)."""
-    global _get_device
-    if _get_device is None:
-        import torch
-        _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    try:
-        return _get_device()
-    except RuntimeError:
-        return -2
+    """Number of the current device, whose stream the calls use."""
+    global _device
+    import torch
+    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _device()
 
 
 class Cache:
@@ -247,14 +240,13 @@ class Cache:
     # of elements, and its shape is looked at only where it is not contiguous; `device` is the current one)
 
     def _memory(self, memory, device):
-        if memory.device != device:
-            _refuse("the memory is on another device than the current one")
-        if memory.shape != self.shape:
-            _refuse("the memory is that of a cache of %s, this one is %s (blocks, kv_heads, block_tokens, head_dim)" % (memory.shape, self.shape))
-        return memory.ref
+        if memory.device == device and memory.shape == self.shape:
+            return memory.ref
+        _refuse("the memory is that of a cache of %s on device %d, this one is %s, the current device %d (blocks, kv_heads, block_tokens, head_dim)"
+                % (memory.shape, memory.device, self.shape, device))
 
     def _ints(self, x, n, what, device):
-        if not (x.dtype is self.int32 and x.get_device() == device and x.is_contiguous() and x.numel() == n):
+        if not (x.dtype is self.int32 and x.get_device() == device and x.numel() == n and x.is_contiguous()):
             _refuse("%s is int32 on the current GPU, contiguous, %d elements" % (what, n))
         return x.data_ptr()
 
@@ -375,10 +367,11 @@ class Cache:
             if not (lse.dtype is self.float32 and lse.get_device() == device and lse.is_contiguous() and lse.numel() == tokens * self.q_heads):
                 _refuse("lse is float32 [tokens, q_heads] on the current GPU, contiguous")
             lp = lse.data_ptr()
-        if max_new < 0 or max_length < 0 or window < 0:
-            _refuse("max_new, max_length and window are not negative")
-        # (no request is as long: what is larger says the same)
-        max_new, max_length, window = min(max_new, _MOST), min(max_length, _MOST), min(window, _MOST)
+        if not (0 <= max_new <= 0xFFFFFFFF and 0 <= max_length <= 0xFFFFFFFF and 0 <= window <= 0xFFFFFFFF):
+            if max_new < 0 or max_length < 0 or window < 0:
+                _refuse("max_new, max_length and window are not negative")
+            # (no request is as long: what is larger says the same)
+            max_new, max_length, window = min(max_new, _MOST), min(max_length, _MOST), min(window, _MOST)
         L, wp = self._lib, None
         # (256 tokens are never cut, and then there is no workspace)
         need = 0 if max_length <= 256 else L.tsq_cache_attend_workspace_bytes(self.handle, n, tokens, max_new, max_length, window)

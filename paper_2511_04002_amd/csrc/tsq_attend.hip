@@ -174,8 +174,10 @@ __device__ __forceinline__ Block block_of(Scale s, float row_factor, uint32_t mo
 }
 struct Softmax { float ref, weight; };                   // of a row, from kScores
 
-// The kernel's arguments (its only parameter), read once more: what only the end of a tile needs then takes no scalar registers in its loop,
-// where a few too many cost k_attend_many the order of its loads and products (7 % of its time).
+// The kernel's arguments (its only parameter), read once more: what a tile's begin and end alone need then takes no scalar
+// registers in its loop.  A few too many cost k_attend_many the order of its loads and products (7 % of its time), and
+// k_attend_few with two sets vector registers that it has not (5 to 14 %).  Where there are enough, the first values serve:
+// reading them again is 0.2 us of a single token's 5.
 __device__ __forceinline__ AttendArgs args_again() {
     struct Words { uint32_t w[sizeof(AttendArgs) / 4]; } words;
     auto args = (const __attribute__((address_space(4))) uint32_t *)__builtin_amdgcn_kernarg_segment_ptr();
@@ -280,7 +282,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
     const uint32_t B = 1u << a.block_log2;
     uint32_t mode = kAll;
     for (uint32_t tile = p.tile;;) {
-        const AttendArgs here = args_again();
+        const AttendArgs here = SETS == 2 || D == 256 ? args_again() : a;
         const uint32_t rows = p.n * here.group;
         const Reach reach = reach_of<ROWS>(here, p, tile);
         const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
@@ -446,9 +448,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
                 if (piece == 0) softmax[16 * c + out_row] = Softmax{top, total};
                 continue;
             }
-            const AttendArgs a = args_again();
-            const Ending end = ending(a, mode, top, total, softmax[16 * c + out_row]);
-            const uint64_t id = a.splits == 1 ? row_id(a, p, o) : part_row(a, p, o);
+            const AttendArgs e = SETS == 2 || D == 256 ? args_again() : a;
+            const Ending end = ending(e, mode, top, total, softmax[16 * c + out_row]);
+            const uint64_t id = e.splits == 1 ? row_id(e, p, o) : part_row(e, p, o);
             for (int part = 0; part < (D + 127) / 128; ++part) {
                 constexpr int N = D < 128 ? D : 128;     // elements at a time
                 if (part) __syncthreads();
@@ -460,26 +462,26 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
                         y[i] = sums[0][out_row][8 * piece + i] + sums[1][out_row][8 * piece + i] + sums[2][out_row][8 * piece + i] + sums[3][out_row][8 * piece + i];
                         y[i] = y[i] * end.f * end.h * end.h;
                     }
-                    if (a.splits == 1) {
+                    if (e.splits == 1) {
                         uint4_t w;
                         for (int i = 0; i < 4; ++i) w[i] = narrow2<BF16>(y[2 * i], y[2 * i + 1]);
-                        uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)(p.begin + o / a.group) * a.out_stride +
-                                        (uint64_t)(p.h * a.group + o % a.group) * D + part * 128 + piece * 8;
+                        uint16_t *dst = static_cast<uint16_t *>(e.out) + (uint64_t)(p.begin + o / e.group) * e.out_stride +
+                                        (uint64_t)(p.h * e.group + o % e.group) * D + part * 128 + piece * 8;
                         *reinterpret_cast<uint4_t *>(dst) = w;
                     } else {
-                        float *dst = a.parts + (id * a.splits + p.split) * D + part * 128 + piece * 8;
+                        float *dst = e.parts + (id * e.splits + p.split) * D + part * 128 + piece * 8;
                         *reinterpret_cast<float4_t *>(dst) = float4_t{y[0], y[1], y[2], y[3]};
                         *reinterpret_cast<float4_t *>(dst + 4) = float4_t{y[4], y[5], y[6], y[7]};
                     }
                 }
             }
             if (piece == 0 && o < rows) {
-                if (a.splits > 1) {
-                    float *dst = a.parts + a.part_rows * a.splits * D + (id * a.splits + p.split) * 2;
+                if (e.splits > 1) {
+                    float *dst = e.parts + e.part_rows * e.splits * D + (id * e.splits + p.split) * 2;
                     dst[0] = end.top;
                     dst[1] = end.total;
-                } else if (a.lse) {
-                    a.lse[id] = end.total == 0.0f ? -INFINITY : (end.top + log2_of(end.total)) * 0.69314718055994530942f;
+                } else if (e.lse) {
+                    e.lse[id] = end.total == 0.0f ? -INFINITY : (end.top + log2_of(end.total)) * 0.69314718055994530942f;
                 }
             }
         }
@@ -543,12 +545,11 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
     const uint32_t B = 1u << a.block_log2;
     uint32_t mode = kAll;
     for (uint32_t tile = p.tile;;) {
-        const AttendArgs b = args_again();
-        const uint32_t row = tile * ROWS + wave * 32 + n, rows = p.n * b.group;
-        const Reach reach = reach_of<ROWS>(b, p, tile);
+        const uint32_t row = tile * ROWS + wave * 32 + n, rows = p.n * a.group;
+        const Reach reach = reach_of<ROWS>(a, p, tile);
         const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
-        if (b.splits > 1 && reach.begin >= reach.end) {
-            nothing_seen<ROWS>(b, p, tile, D);
+        if (a.splits > 1 && reach.begin >= reach.end) {
+            nothing_seen<ROWS>(a, p, tile, D);
             if (done) return;
             ++tile;
             continue;
@@ -562,8 +563,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
             for (int s = 0; s < D / 16; ++s) {
                 w[s] = uint4_t{0, 0, 0, 0};
                 if (row < rows) {
-                    const uint16_t *src = static_cast<const uint16_t *>(b.q) + (uint64_t)(p.begin + row / b.group) * b.q_stride +
-                                          (uint64_t)(p.h * b.group + row % b.group) * D + 16 * s + 8 * hi;
+                    const uint16_t *src = static_cast<const uint16_t *>(a.q) + (uint64_t)(p.begin + row / a.group) * a.q_stride +
+                                          (uint64_t)(p.h * a.group + row % a.group) * D + 16 * s + 8 * hi;
                     w[s] = *reinterpret_cast<const uint4_t *>(src);
                 }
                 most = max(most, piece_most(w[s]));
@@ -577,7 +578,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
             for (int s = 0; s < D / 16; ++s) q[s] = query_piece<BF16>(w[s], factor);
         }
         uint32_t from, to;
-        row_sees(b, p, row, from, to);
+        row_sees(a, p, row, from, to);
 
         float16_t acc[D / 32];
 #pragma unroll
