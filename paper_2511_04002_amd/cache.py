@@ -67,7 +67,7 @@ def lib():
     return _lib
 
 
-# ------------------------------------------------------------------ the C entry points, same names
+# ------------------------------------------------------------------ the C entry points that give back a value, same names
 
 def _done(status: int, what: str) -> None:
     if status != TSQ_OK:
@@ -89,26 +89,6 @@ def tsq_cache_memory_sizes(cache: int) -> tsq_cache_sizes:
     out = tsq_cache_sizes()
     _done(lib().tsq_cache_memory_sizes(cache, C.byref(out)), "tsq_cache_memory_sizes")
     return out
-
-
-def tsq_cache_schedule(*args) -> None:
-    _done(lib().tsq_cache_schedule(*args), "tsq_cache_schedule")
-
-
-def tsq_cache_norm_rotate(*args) -> None:
-    _done(lib().tsq_cache_norm_rotate(*args), "tsq_cache_norm_rotate")
-
-
-def tsq_cache_append(*args) -> None:
-    _done(lib().tsq_cache_append(*args), "tsq_cache_append")
-
-
-def tsq_cache_gather(*args) -> None:
-    _done(lib().tsq_cache_gather(*args), "tsq_cache_gather")
-
-
-def tsq_cache_attend(*args) -> None:
-    _done(lib().tsq_cache_attend(*args), "tsq_cache_attend")
 
 
 def tsq_cache_attend_workspace_bytes(cache: int, requests: int, tokens: int, max_new: int, max_length: int, window: int = 0) -> int:
