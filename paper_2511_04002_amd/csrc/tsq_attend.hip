@@ -804,7 +804,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
 // PIECES = 256 WAVES / D pieces are read at once.  Which lanes add which pieces, and in which order the lanes'
 // sums are added, is fixed.
 template <int D, bool BF16, int WAVES>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(AttendArgs a) {
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(JoinArgs j) {
+    const AttendArgs &a = j.a;
     constexpr uint32_t LANES = D / 4, PIECES = 64 * WAVES / LANES, ROWS = WAVES == 1 ? 4 : 1;
     __shared__ float4_t sums[WAVES > 1 ? WAVES : 1][LANES];
     __shared__ float totals[WAVES > 1 ? WAVES : 1], tops[WAVES > 1 ? WAVES : 1];
@@ -814,9 +815,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
     const uint64_t firsts = a.splits == 1 ? 0 : a.part_rows;
     const bool of_few = id >= firsts;
     if (of_few) id -= firsts;
-    const uint64_t part_rows = of_few ? a.few_part_rows : a.part_rows;
-    const uint32_t splits = of_few ? a.few_splits : a.splits;
-    const float *all = of_few ? a.few_parts : a.parts;
+    const uint64_t part_rows = of_few ? j.few_part_rows : a.part_rows;
+    const uint32_t splits = of_few ? j.few_splits : a.splits;
+    const float *all = of_few ? j.few_parts : a.parts;
     if (id >= part_rows || splits == 1) return;
     // What most rows have is asked for at once: the first pieces of each lane and their statistics.
     const uint32_t part = tid / LANES, piece = tid % LANES;
@@ -832,8 +833,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_attend_join(A
     }
     // rows that no request has, or one of the other launch's, were not computed and are not written
     uint32_t token, head;
-    if (of_few && a.slots_each) {
-        const uint32_t each = a.slots_each * a.kv_heads, r = (uint32_t)(id / each), slot = (uint32_t)(id % each), row = slot / a.kv_heads;
+    if (of_few && j.slots_each) {
+        const uint32_t each = j.slots_each * a.kv_heads, r = (uint32_t)(id / each), slot = (uint32_t)(id % each), row = slot / a.kv_heads;
         const uint32_t b = min((uint32_t)max(a.starts[r], 0), a.tokens), e = min((uint32_t)max(a.starts[r + 1], 0), a.tokens);
         const uint32_t rows = e > b ? (e - b) * a.group : 0;
         if (row >= rows || rows >= a.rows_from) return;
@@ -994,6 +995,7 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
     const bool one_wave = l.splits <= 16 && l.few_splits <= 16;
     if (!fits(all, l.rows == 256 ? 512 : 256) || !fits(few, 256) || !(one_wave ? fits((joined + 3) / 4, 256) : fits(joined, 512))) return kTooLarge;
     const uint32_t grid = (uint32_t)all;
+    const JoinArgs j = {a, reinterpret_cast<float *>(reinterpret_cast<char *>(a.parts) + l.few_at), l.few_part_rows, l.few_splits, l.slots_each};
     by_shape(s, [&](auto d, auto bf16) {
         if (l.rows == 16) k_attend_few<d(), bf16(), 1><<<grid, 256, 0, st>>>(a);
         else if (l.rows == 32) { if constexpr (d() != 256) k_attend_few<d(), bf16(), 2><<<grid, 256, 0, st>>>(a); }
@@ -1012,16 +1014,16 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
         f.rows_to = few_rows(s);
         f.splits = l.few_splits;
         f.chunk = l.few_chunk;
-        f.parts = a.few_parts;
-        f.part_rows = a.few_part_rows;
-        f.slots_each = a.slots_each = l.slots_each;
+        f.parts = j.few_parts;
+        f.part_rows = l.few_part_rows;
+        f.slots_each = l.slots_each;
         by_shape(s, [&](auto d, auto bf16) { k_attend_few<d(), bf16(), d() == 256 ? 1 : 2><<<(uint32_t)few, 256, 0, st>>>(f); });
         if (hipError_t e = hipGetLastError()) return (int)e;
     }
     if (joined == 0) return 0;
     by_shape(s, [&](auto d, auto bf16) {
-        if (one_wave) k_attend_join<d(), bf16(), 1><<<(uint32_t)((joined + 3) / 4), 256, 0, st>>>(a);
-        else k_attend_join<d(), bf16(), 8><<<(uint32_t)joined, 512, 0, st>>>(a);
+        if (one_wave) k_attend_join<d(), bf16(), 1><<<(uint32_t)((joined + 3) / 4), 256, 0, st>>>(j);
+        else k_attend_join<d(), bf16(), 8><<<(uint32_t)joined, 512, 0, st>>>(j);
     });
     return (int)hipGetLastError();
 }

@@ -187,8 +187,7 @@ tsq_status tsq_cache_attend(const tsq_cache *c, const tsq_cache_memory *m, uint3
     a.lengths = static_cast<const int32_t *>(d_lengths);
     a.q = d_q; a.out = d_out; a.lse = static_cast<float *>(d_lse); a.parts = static_cast<float *>(d_ws);
     a.q_stride = q_stride; a.out_stride = out_stride; a.part_rows = l.part_rows;
-    a.few_parts = l.few_splits == 1 ? nullptr : reinterpret_cast<float *>(static_cast<char *>(d_ws) + l.few_at);
-    a.few_part_rows = l.few_part_rows; a.few_splits = l.few_splits; a.slots_each = 0;
+    a.slots_each = 0;
     a.requests = requests; a.tokens = tokens; a.q_heads = c->s.q_heads; a.kv_heads = c->s.kv_heads;
     a.group = c->s.q_heads / c->s.kv_heads; a.blocks = c->s.blocks; a.block_log2 = c->s.block_log2; a.max_blocks = c->s.max_blocks;
     a.tiles = l.tiles; a.tiles_each = l.tiles_each; a.splits = l.splits; a.chunk = l.chunk; a.by_length = l.by_length; a.by_tile = 0;

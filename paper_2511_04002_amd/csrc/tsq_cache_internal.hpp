@@ -65,9 +65,6 @@ struct AttendArgs {
     float *lse;
     float *parts;                // binary32 [part_rows][splits][head_dim] sums, then [..][splits][2] their maximum and weight
     uint64_t q_stride, out_stride, part_rows;
-    float *few_parts;            // the same of the launch for the requests of few rows, for the join of both
-    uint64_t few_part_rows;
-    uint32_t few_splits;         // (1: no join)
     uint32_t slots_each;         // rows of a kv head that a request has in the parts of that launch; 0: part_rows are rows of the output
     uint32_t requests, tokens, q_heads, kv_heads, group, blocks, block_log2, max_blocks;
     uint32_t tiles, tiles_each;  // row tiles of the call; of each request, or 0: they follow one another (see find_place)
@@ -83,6 +80,15 @@ struct AttendArgs {
 // A launch counts its threads in 32 bits: one of more is refused before anything is enqueued.
 constexpr int kTooLarge = -1;    // what the functions below return then; 0, or a hipError_t, in all other cases
 inline bool fits(uint64_t workgroups, uint32_t threads) { return workgroups * threads < (1ull << 32); }
+
+// The join has both launches' parts; what the others do not need is no argument of theirs.
+struct JoinArgs {
+    AttendArgs a;                // of the first launch
+    float *few_parts;
+    uint64_t few_part_rows;
+    uint32_t few_splits;         // (1: no join)
+    uint32_t slots_each;         // of the second launch
+};
 
 int launch_schedule(const ScheduleArgs &a, void *stream);
 int launch_norm_rotate(const CacheShape &s, const NormRotateArgs &a, void *stream);
