@@ -164,10 +164,16 @@ tsq_status tsq_cache_gather(const tsq_cache *cache, const tsq_cache_memory *memo
  *   d_ws             tsq_cache_attend_workspace_bytes() bytes for the same numbers, 256-byte aligned; needs
  *                    no reset; one call at a time.  NULL where the size is 0
  * A call may cover a part of a step's requests (d_table, d_starts and d_lengths from the first of them on;
- * rows stay those of the whole step): requests of one token and long ones of the same step are best given
- * in calls of their own, since the largest request of a call decides which kernel runs.
- * Products are exact in binary32 sums: codes are whole numbers, queries keep their bits; weights of the
- * values are rounded to 11 bits; softmax statistics and all sums are binary32.
+ * rows stay those of the whole step).  Requests with up to 64 rows of a kv head (queries times query heads
+ * of one kv head; 32 rows for head_dim 256) and those with more go to different kernels: max_new says which
+ * a call needs.  Where the requests have a quarter of max_new queries on average, or less, both run one
+ * after the other; otherwise one takes all requests.  The workspace holds the pieces that long requests are
+ * cut into, for rows of the first kind of 8192 tokens or less each: it grows with max_length, which should
+ * not be far above the longest request's.
+ * Products are exact in binary32 sums: codes are whole numbers, and queries keep their bits, but for
+ * elements of bfloat16 queries below 2^-27 of the largest of their head, which lose low bits.  scale times
+ * a scale of keys is taken in binary32 and should be a normal number.  Weights of the values are rounded
+ * to 11 bits; softmax statistics and all sums are binary32.
  */
 tsq_status tsq_cache_attend(const tsq_cache *cache, const tsq_cache_memory *memory, uint32_t requests, const void *d_table,
                             const void *d_starts, const void *d_lengths, uint32_t tokens, uint32_t max_new,

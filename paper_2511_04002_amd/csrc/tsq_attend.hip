@@ -8,7 +8,8 @@
 // weight that the values' codes want; the softmax's denominator takes P_t / s_v back, once for 16 tokens.  The
 // reference m follows the largest exponent of a row in steps: it moves only when an exponent is more than 8 above
 // what it was set for, and is then set 7 below the largest.  P is then at most 2^15, in a half's range, and
-// 11-bit weights down to 2^-21 of the row's largest.
+// 11-bit weights down to 2^-21 of the row's largest: the matrix instructions' operands, as fine as an output of binary16
+// and three bits finer than one of bfloat16.  The denominator adds the weights as they are before that rounding.
 //
 // Scores are computed transposed, S^T = K Q^T: a lane then has all its scores in one row of the softmax (a query),
 // and the registers that hold P^T are, in the order they are in, an operand of O^T = V^T P^T.  A matrix
@@ -156,7 +157,7 @@ __device__ __forceinline__ bool is_bad(const AttendArgs &a, const Place &p, uint
 // A row's exponents hold scales of 2^-60 to 2^40 together, all that values of magnitudes from 2^-53 to 2^47 bring: with
 // scales farther apart, tokens of small ones would be lost from the denominator, and of scales below about 2^-110 it would
 // pass binary32's range.  A tile that meets others is gone through twice more: once for the softmax of the scores
-// alone (kScores), and once for the sums of the values (kValues), each with a reference of its own.
+// alone (kScores), and once for the sums of the values (kValues), each with a reference of its own, in 2.4 to 2.7 times the time.
 enum Mode : uint32_t { kAll, kScores, kValues };
 __device__ __forceinline__ bool is_far(float log_v) { return fabsf(log_v + 10.0f) > 50.0f; }
 struct Scale { float k, v; bool bad; };
@@ -267,7 +268,10 @@ __device__ __forceinline__ void nothing_seen(const AttendArgs &a, const Place &p
 //
 // The cache's bytes bound it: 64 requests of 1024 to 4096 tokens on 40 heads of 128, blocks of 16, are 1.79 GB and
 // 306 us, 5.8 TB/s.  The same 2 KB pieces read and thrown away take 300 us, 283 with the longest request first; a
-// stream of reads reaches 7.0 TB/s.  One query of 64 heads on 8 over 131072 tokens: 269 MB, 46 us and 4 for the join.
+// stream of reads reaches 7.0 TB/s.  One query of 64 heads on 8 over 131072 tokens: 269 MB, 46 to 54 us and 5 for the
+// join.  With two sets a wave does twice the exponents, maxima and sums for the same bytes, two waves a SIMD: 4 queries of
+// 32 requests over 8192 tokens, 64 heads on 8, are 537 MB and 130 us, 8 of 16 requests over 4096, in two tiles, 134 MB
+// and 51.
 template <int D, bool BF16, int SETS>
 __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) void k_attend_few(AttendArgs a) {
     constexpr int F = D / 64;                            // 64-element pieces of a head
@@ -504,8 +508,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
 // Instruction issue bounds it: a wave's 64 tokens by 32 rows of 128 are 1024 cycles of products, and some 1300 of
 // exponentials, maxima, sums, conversions and addresses, which run beside them only as far as two waves of a SIMD
 // complement each other (a product keeps 12 cycles of issue from the other wave).  8192 queries over as many tokens,
-// causal, 64 heads on 8 of 128: 1.10 PFLOP in 1.12 ms, 0.98 PFLOP/s; a large library product of halves reaches 1.2.
-// Heads of 64 have the exponentials of 128 for half the products: 0.57 PFLOP/s (two requests of 8000 tokens, 20 heads).
+// causal, 64 heads on 8 of 128: 1.10 PFLOP in 1.12 to 1.15 ms, 0.96 to 0.98 PFLOP/s; a large library product of halves
+// reaches 1.2.  Heads of 64 have the exponentials of 128 for half the products: 0.65 PFLOP/s (two requests of 8000 tokens,
+// 20 heads).  Heads of 256 leave registers for one wave a SIMD, whose products nothing runs beside: 0.58 PFLOP/s (4096
+// tokens, 16 heads on 8).  Chunks: 512 queries after 7680, 64 heads on 8, 168 us, 0.79 PFLOP/s; 300 after 4000 of four
+// requests, 32 on 8, 138 us, 0.59 (160 workgroups for 256 places).
 // The maxima could be left out of nearly all tiles, since the sums of the weights show when the reference is too low;
 // the second pass that this needs costs more registers than there are (spilled, 1.44 ms).
 // Lane (n = lane % 32, hi = lane / 32).  S^T in two 32 x 32 pieces: register i of a piece is token
@@ -907,8 +914,8 @@ uint32_t few_rows(const CacheShape &s) { return s.head_dim == 256 ? 32 : 64; }
 // Which kernel, how many rows a workgroup, and into how many pieces the cache's length is cut.
 //
 // Rows: a request with at most 64 rows of a kv head goes to k_attend_few, whose time is the cache's bytes as long as
-// they are read once or twice (32 requests of 8192 tokens, 64 heads on 8 of 128, 4 queries each: 140 us in two passes
-// of 16 rows, 202 us by k_attend_many).  k_attend_many takes 256 rows a workgroup, 128 where a request has no more.
+// they are read once or twice (32 requests of 8192 tokens, 64 heads on 8 of 128, 4 queries each: 130 us in one pass of
+// 32 rows, 217 us by k_attend_many; 16 of 4096, 8 each: 50 us in two, and 58).  k_attend_many takes 256 rows a workgroup, 128 where a request has no more.
 // Pieces: `slots` workgroups run at once.  Fewer units than that leave the device partly idle, so each is cut; a piece
 // costs its start and its share of the join.  Each launch has its own number of pieces and its own parts: prompts beside
 // single tokens of long requests stay whole, and only the rows of the second launch have pieces to be joined.
@@ -933,8 +940,8 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
         slots = s.head_dim == 256 || l.rows == 256 ? 256 : 512;
         // Single tokens beside prompts: where the requests have a quarter of the longest one's rows on average, or less, a
         // launch of its own takes those of few rows, and this one the others (one token each of 63 requests of 2000 tokens
-        // and a prompt of 512, 64 heads on 8: 80 us, and 174 all by k_attend_many; 15 of 8000 and 2048, 32 on 8: 135 and
-        // 262; 200 of 500 and 1000, 32 on 32: 283 and 508; 3 of 300 and 200, 32 on 8: 21 and 20).
+        // and a prompt of 512, 64 heads on 8: 80 us, and 157 all by k_attend_many; 15 of 8000 and 2048, 32 on 8: 135 and
+        // 251; 200 of 500 and 1000, 32 on 32: 284 and 514; 3 of 300 and 200, 32 on 8: 20 and 20).
         if (requests > 1 && tokens * group * 4 <= requests * most) l.few_tiles = (uint32_t)(few / (s.head_dim == 256 ? 16 : 32)) * requests;
     }
     uint64_t reach = max_length < 0x7FFFFFFFu ? max_length : 0x7FFFFFFFu;     // (no request is longer, and a piece's tokens are 32 bits)
@@ -952,9 +959,9 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
         if (splits == 0) splits = 1;
     };
     // One request of a batch may be far longer than the others: a piece of k_attend_few has no more than 8192 tokens (63
-    // requests of 2000 tokens and one of 131072, 64 heads on 8: 220 us, and 737 in one piece; 64 requests of 32768 each
-    // 739 and 712).  The same holds for k_attend_many beside single tokens, whose tiles end at once there, as long as the
-    // other tiles leave the device partly idle (512 tokens after 32256 beside 62 of 2000: 706 us, and 998 in one piece).
+    // requests of 2000 tokens and one of 131072, 64 heads on 8: 225 us, and 766 in one piece; 64 requests of 32768 each
+    // 738 and 718).  The same holds for k_attend_many beside single tokens, whose tiles end at once there, as long as the
+    // other tiles leave the device partly idle (512 tokens after 32256 beside 62 of 2000: 690 us, and 998 in one piece).
     const uint64_t units = (uint64_t)l.tiles * s.kv_heads, pieces = (reach + 8191) / 8192;
     uint64_t at_least = 1;
     if (l.rows < 128) at_least = pieces;

@@ -550,8 +550,11 @@ __device__ __forceinline__ void store_single(const uint16_t *x, int8_t *codes, f
 // (run, head, keys or values).
 //
 // Of prompts, memory is the bound: 5600 rows of 32 heads of 128 are 138 MB and 29 us.  Of single tokens it is what the
-// layout makes of them: the keys of a (token, head) are 128 bytes side by side, the values 128 bytes 16 apart, so that
-// 16 lines are written in part; 512 tokens on 40 heads are 16 MB as they come and 22 us.
+// layout makes of them: the keys of a (token, head) are 128 bytes side by side, the values 128 bytes a block's tokens
+// apart, so that as many lines of 128 bytes as a block has tokens are written in part.  512 tokens on 40 heads, 16 MB as
+// they come, into blocks of 16, 32, 64 and 128 whose places are spread evenly: 25, 39, 67 and 102 us, with 16, 10, 6 and
+// 3 % of the (token, head) pairs growing past their block's scale, whose codes are read and written again (blocks of
+// 16 without: 22 us).
 template <int D, bool BF16>
 __global__ __launch_bounds__(256, D == 256 ? 3 : 4) void k_append(AppendArgs a) {
     const uint32_t lane = threadIdx.x & 63;
@@ -631,9 +634,11 @@ __global__ __launch_bounds__(256, D == 256 ? 3 : 4) void k_append(AppendArgs a) 
 // Sixteen rows of the output for waves_each waves: row i's request, position and block by lane i, then a share of the
 // heads each wave.
 //
-// Memory is the bound: 92000 rows of 8 heads of 128 from blocks of 64 tokens are 565 MB and 123 us, 4.6 TB/s where a
-// copy reaches 6.2; the values' 4-byte stores and the scattered blocks keep it from that.  A request of 2048 rows of
-// 32 heads, from blocks of 16, is 50 MB and 8 to 10 us.
+// Memory is the bound: 92000 rows of 8 heads of 128 from blocks of 64 tokens are 565 MB and 104 us, 126 where two such
+// calls take turns (a part of one's data stays in the memory's cache otherwise): 5.4 and 4.5 TB/s where a copy reaches
+// 6.1.  The keys alone take 45 us, the values alone 63, and 42 of those if they are only read: a wave reads 16 bytes out
+// of each of 128 rows of 64 bytes, and the other waves of its workgroup the rest of the lines.  A request of 2048 rows of
+// 32 heads, from blocks of 16, is 50 MB and 9 to 10 us.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void k_gather(GatherArgs a) {
     const uint32_t lane = threadIdx.x & 63, B = a.block_tokens;
