@@ -1,5 +1,5 @@
 /*
- * tsq_cache.h — C ABI of the serving side of the library (gfx950): a key/value cache held in 8 bits, in
+ * tsq_cache.h — C ABI of the serving side of the library (gfx950): a key/value cache held in 8 or 4 bits, in
  * blocks, and the operators that fill and read it.  It is where the keys and values of a split model live
  * on the machine that goes on with it: tsq_decompress_batch restores what the other side sent as rows
  * [tokens x kv_heads*head_dim], tsq_cache_append stores such rows, tsq_cache_attend reads them, and
@@ -44,6 +44,12 @@ typedef struct tsq_cache tsq_cache;   /* opaque, host memory, never written afte
  *   d_v       int8  [blocks][kv_heads][head_dim][block_tokens]
  *   d_k_scale f32   [blocks][kv_heads]      a key is code * scale
  *   d_v_scale f32   [blocks][kv_heads]
+ * Of a cache in 4 bits:
+ *   d_k, d_v  uint8 [blocks][kv_heads][block_tokens][head_dim / 2]: byte j has element 2j in its low four bits,
+ *             element 2j + 1 in its high ones.  Codes 0 .. 7 are 0, 0.5, 1, 1.5, 2, 3, 4, 6; 8 .. 15 the same with
+ *             the sign turned
+ *   d_k_scale, d_v_scale  uint8 [blocks][kv_heads][head_dim / 32][block_tokens]: scale s of 32 elements of a token
+ *             says that they are code * 2^(s - 127), or NaN where s is 255
  */
 typedef struct {
     void *d_k, *d_v, *d_k_scale, *d_v_scale;
@@ -54,8 +60,12 @@ typedef struct {
     uint64_t scale_bytes;   /* of d_k_scale, and of d_v_scale                                        */
 } tsq_cache_sizes;
 
-/* Host only; INVALID_ARG / UNSUPPORTED / NO_MEMORY without touching *out. */
+/*
+ * Host only; INVALID_ARG / UNSUPPORTED / NO_MEMORY without touching *out.  tsq_cache_create makes a cache in 8 bits,
+ * tsq_cache_create_bits one in `bits`, 8 or 4.  All functions below take either; what is said of one alone is marked.
+ */
 tsq_status tsq_cache_create(const tsq_cache_config *cfg, tsq_cache **out);
+tsq_status tsq_cache_create_bits(const tsq_cache_config *cfg, uint32_t bits, tsq_cache **out);
 void       tsq_cache_destroy(tsq_cache *cache);
 tsq_status tsq_cache_memory_sizes(const tsq_cache *cache, tsq_cache_sizes *out);
 
@@ -116,24 +126,45 @@ tsq_status tsq_cache_norm_rotate(const tsq_cache *cache, uint32_t tokens, const 
                                  void *d_k_out, uint64_t k_out_stride, void *stream);
 
 /*
- * Stores rows of keys and values.  For each block and head that gets tokens, with s the scale it has (0 if
+ * The same, where a position has a place on each of several axes (time, height and width of an image or a film):
+ * pair i turns by its angle i at the place on axis d_axis[i].
+ *   axes             1 .. 4
+ *   d_positions      int32 [axes][tokens].  A row with a negative place on any axis is not written; one with a place
+ *                    past angle_rows on any axis becomes NaN
+ *   d_axis           uint8 [rotary / 2], 8-byte aligned; a pair of an axis that there is not becomes NaN
+ */
+tsq_status tsq_cache_norm_rotate_axes(const tsq_cache *cache, uint32_t tokens, const void *d_q, uint64_t q_stride, const void *d_k,
+                                      uint64_t k_stride, uint32_t axes, const void *d_positions, const void *d_axis,
+                                      const void *d_angles, uint32_t angle_rows, uint32_t rotary, int32_t pairs,
+                                      const void *d_q_weight, const void *d_k_weight, float eps, void *d_q_out,
+                                      uint64_t q_out_stride, void *d_k_out, uint64_t k_out_stride, void *stream);
+
+/*
+ * Stores rows of keys and values.  In 8 bits: for each block and head that gets tokens, with s the scale it has (0 if
  * the first of them goes to place 0: what a block held before is forgotten) and m the largest magnitude
  * among the new elements:
  *   s' = max(s, m / 127)         (m / 127 below 2^-126 counts as 0; a NaN or infinity among the new
  *                                elements makes s' NaN, and the block's head then reads as NaN)
  *   codes already there become round(code * (s / s')), new ones round(x * (1 / s')), ties to even
  * in binary32.  An element that is stored and not recoded is within s'/2 of its value.
+ * In 4 bits: for each 32 elements of a token, with m the largest magnitude among them, e is the least exponent with
+ *   m <= 7 * 2^e         (0 if m is 0; -23 <= e <= 13 for binary16, -120 <= e <= 125 for bfloat16)
+ * and each element becomes the nearest code * 2^e, of two the one with an even code, 6 * 2^e if it is larger than
+ * that: within 2^e / 4 of values up to 2 * 2^e, 2^e / 2 up to 4 * 2^e, 2^e above (but for magnitudes of binary16 above
+ * 7 * 2^13 and of bfloat16 above 7 * 2^125).  A NaN or infinity among a token's keys or values of a head makes all of
+ * them, keys and values, read as NaN.  A token does not change others.
  *   d_k, d_v         rows of kv_heads heads, strides as in tsq_cache_norm_rotate
  *   d_slots          int32 [tokens]: where each row goes; negative, or past the cache: the row is skipped.
- *                    The tokens of one block must be consecutive rows at consecutive places (as
- *                    tsq_cache_schedule makes them): each such run is stored as one
+ *                    In 8 bits the tokens of one block must be consecutive rows at consecutive places (as
+ *                    tsq_cache_schedule makes them): each such run is stored as one.  In 4 bits they may be in any
+ *                    order, but none twice (its place would get parts of both)
  */
 tsq_status tsq_cache_append(const tsq_cache *cache, const tsq_cache_memory *memory, uint32_t tokens, const void *d_k,
                             uint64_t k_stride, const void *d_v, uint64_t v_stride, const void *d_slots, void *stream);
 
 /*
  * Reads tokens back: rows d_starts[r] .. d_starts[r+1] - 1 receive the last tokens of request r, up to its
- * d_lengths[r], as code * scale rounded to the cache's dtype.  Rows before a request's first token, and
+ * d_lengths[r], as code * scale rounded to the cache's dtype (exact in 4 bits).  Rows before a request's first token, and
  * blocks that the table does not hold (an entry outside the cache, or past max_blocks), read as NaN.
  *   requests         <= 65535
  *   d_table          int32 [requests][max_blocks];  d_starts int32 [requests + 1];  d_lengths int32 [requests]
@@ -150,9 +181,10 @@ tsq_status tsq_cache_gather(const tsq_cache *cache, const tsq_cache_memory *memo
  *   causal: t <= p          window > 0: t > p - window
  * out = sum of softmax(scale * q.k) v over them, and lse the natural logarithm of the softmax's
  * denominator.  A query that sees nothing gets zeros and an lse of -inf.  Out and lse of a query are NaN if
- * it sees a token of a block whose scale of keys or values is NaN for its head, or of a table entry outside
- * the cache, or if its request is longer than max_blocks blocks.  Query head j reads kv head
- * j / (q_heads / kv_heads).  Scales are 0, NaN, or at least 2^-126, as tsq_cache_append leaves them.
+ * it sees a token of a block whose scale of keys or values is NaN for its head (in 4 bits: a token that is marked
+ * as NaN), or of a table entry outside the cache, or if its request is longer than max_blocks blocks.  Query head j
+ * reads kv head j / (q_heads / kv_heads).  Scales are as tsq_cache_append leaves them: 0, NaN, or at least 2^-126, and
+ * in 4 bits within its exponents, or 255 in all of a token's groups, keys and values.
  *   d_q, d_out       rows of q_heads heads, strides as in tsq_cache_norm_rotate; must not overlap
  *   requests         <= 65535
  *   tokens           rows of d_q, d_out and d_lse; rows that no request has are not written
@@ -174,6 +206,8 @@ tsq_status tsq_cache_gather(const tsq_cache *cache, const tsq_cache_memory *memo
  * elements of bfloat16 queries below 2^-27 of the largest of their head, which lose low bits.  scale times
  * a scale of keys is taken in binary32 and should be a normal number.  Weights of the values are rounded
  * to 11 bits; softmax statistics and all sums are binary32.
+ * In 4 bits queries, keys and values are exact in either type; the sums of weights, at most 1 each, times values of
+ * bfloat16 have to stay within binary32's range, and products of weights and values below 2^-126 may count as 0.
  */
 tsq_status tsq_cache_attend(const tsq_cache *cache, const tsq_cache_memory *memory, uint32_t requests, const void *d_table,
                             const void *d_starts, const void *d_lengths, uint32_t tokens, uint32_t max_new,

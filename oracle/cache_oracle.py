@@ -130,16 +130,22 @@ def tokens_of(codes, scale, row, length, block, max_blocks):
 def attend(k, v, k_scale, v_scale, block, max_blocks, table, starts, lengths, q, scale, causal, window):
     """q [tokens, q_heads, dim] -> out, lse and the sum of weight * |value| (what a relative error of the weights
     can do to out), all binary64."""
+    def held(r, length):
+        return (tokens_of(k, k_scale, table[r], length, block, max_blocks),
+                tokens_of(v.swapaxes(2, 3), v_scale, table[r], length, block, max_blocks))
+    return _attend(held, k.shape[1], block, max_blocks, starts, lengths, q, scale, causal, window)
+
+
+def _attend(held, kv_heads, block, max_blocks, starts, lengths, q, scale, causal, window):
+    """held(r, length) -> keys, values [length, kv_heads, dim] of a request."""
     tokens, heads, dim = q.shape
-    kv_heads = k.shape[1]
     out, lse, spread = np.zeros((tokens, heads, dim)), np.full((tokens, heads), -np.inf), np.zeros((tokens, heads, dim))
     for r, length in enumerate(lengths.tolist()):
         n, first = int(starts[r + 1] - starts[r]), int(starts[r])
         if n <= 0:
             continue
         whole = length <= max_blocks * block
-        keys = tokens_of(k, k_scale, table[r], length, block, max_blocks)
-        values = tokens_of(v.swapaxes(2, 3), v_scale, table[r], length, block, max_blocks)
+        keys, values = held(r, length)
         if not whole:
             keys[:] = np.nan
         t = np.arange(length)
@@ -163,3 +169,88 @@ def attend(k, v, k_scale, v_scale, block, max_blocks, table, starts, lengths, q,
                 out[first + i, h] = w @ values[seen, g]
                 spread[first + i, h] = w @ np.abs(values[seen, g])
     return out, lse, spread
+
+
+# ------------------------------------------------------------------ a cache in 4 bits
+#
+# k, v [blocks, kv_heads, block_tokens, head_dim / 2] uint8, scales [blocks, kv_heads, head_dim / 32, block_tokens] uint8.
+
+FOUR = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6])
+
+
+def four_scale(x, dtype):
+    """x [..., 32] float64, finite -> byte of the scale: the least of the type's powers of two with max|x| <= 7 of it."""
+    lowest, highest = (-23, 13) if dtype == "f16" else (-120, 125)
+    most = np.abs(x).max(-1)
+    e = np.full(most.shape, highest)
+    for at in range(highest - 1, lowest - 1, -1):
+        e = np.where(most <= 7 * 2.0 ** at, at, e)
+    return np.where(most == 0, 0, e) + 127
+
+
+def four_code(x, byte):
+    """x [..., 32] float64 -> codes of the nearest values, of two the even one; 6 for what is larger."""
+    a = np.minimum(np.abs(x) * 2.0 ** (127.0 - byte)[..., None], 6.0)
+    off = np.abs(a[..., None] - FOUR[:8])
+    near = off == off.min(-1, keepdims=True)
+    first = near.argmax(-1)
+    second = 7 - near[..., ::-1].argmax(-1)
+    return np.where(first % 2 == 0, first, second) + 8 * np.signbit(x)
+
+
+def four_append(k, v, k_scale, v_scale, new_k, new_v, slots, block, dtype):
+    """new_k, new_v [tokens, heads, dim]; in place."""
+    for token, slot in enumerate(slots.tolist()):
+        b, o = slot // block, slot % block
+        if slot < 0 or b >= k.shape[0]:
+            continue
+        for h in range(k.shape[1]):
+            odd = not (np.isfinite(new_k[token, h]).all() and np.isfinite(new_v[token, h]).all())
+            for codes, scale, x in ((k, k_scale, new_k), (v, v_scale, new_v)):
+                if odd:                          # (the codes of a token that is marked are not looked at)
+                    scale[b, h, :, o] = 255
+                    continue
+                x = x[token, h].astype(np.float64).reshape(-1, 32)
+                byte = four_scale(x, dtype)
+                c = four_code(x, byte.astype(np.float64)).reshape(-1)
+                codes[b, h, o] = c[0::2] + 16 * c[1::2]
+                scale[b, h, :, o] = byte
+
+
+def four_values(codes, scale):
+    """[blocks, heads, block tokens, dim] float64."""
+    x = np.stack((FOUR[codes & 15], FOUR[codes >> 4]), -1).reshape(codes.shape[:3] + (codes.shape[3] // 16, 32))
+    s = np.where(scale == 255, np.nan, 2.0 ** (scale.astype(np.float64) - 127))
+    return (x * s.swapaxes(2, 3)[..., None]).reshape(codes.shape[:3] + (2 * codes.shape[3],))
+
+
+def four_tokens_of(codes, scale, row, length, block, max_blocks):
+    """[length, heads, dim] float64 of a request; what the table does not hold is NaN."""
+    out = np.full((length, codes.shape[1], 2 * codes.shape[3]), np.nan)
+    for j in range(min(-(-length // block), max_blocks)):
+        here = out[j * block:(j + 1) * block]
+        if 0 <= row[j] < codes.shape[0]:
+            one = slice(row[j], row[j] + 1)
+            here[:] = four_values(codes[one], scale[one])[0].swapaxes(0, 1)[:len(here)]
+    return out
+
+
+def four_attend(k, v, k_scale, v_scale, block, max_blocks, table, starts, lengths, q, scale, causal, window):
+    """As attend."""
+    def held(r, length):
+        return (four_tokens_of(k, k_scale, table[r], length, block, max_blocks), four_tokens_of(v, v_scale, table[r], length, block, max_blocks))
+    return _attend(held, k.shape[1], block, max_blocks, starts, lengths, q, scale, causal, window)
+
+
+def norm_rotate_axes(x, weight, eps, angles, positions, axis, rotary, neighbours):
+    """As norm_rotate, with positions [axes, tokens] and the axis that each pair turns by.  Rows with a position past the
+    angles are NaN, and so are pairs of an axis that there is not."""
+    half = rotary // 2
+    known = (positions < len(angles)).all(0)
+    own = np.zeros((x.shape[0], rotary), angles.dtype)
+    for i in range(half):
+        for part in (i, half + i):
+            own[:, part] = np.nan if axis[i] >= len(positions) else angles[np.where(known, positions[axis[i]], 0), part]
+    y = norm_rotate(x, weight, eps, own, np.arange(x.shape[0]), rotary, neighbours)
+    y[~known] = np.nan
+    return y

@@ -13,8 +13,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtsq.so")
 SOURCES = ["tsq_api.hip", "tsq_kernels.hip", "tsq_fused.hip", "tsq_direct.hip", "tsq_entropy.hip", "tsq_rans.hip", "tsq_link.cpp",
-           "tsq_cache_api.hip", "tsq_cache_rows.hip", "tsq_attend.hip"]
-HEADERS = ["tsq_internal.hpp", "tsq_device.hpp", "tsq_pass.hpp", "tsq_ranges.hpp", "tsq_cache_internal.hpp"] + \
+           "tsq_cache_api.hip", "tsq_cache_rows.hip", "tsq_four_rows.hip", "tsq_attend.hip", "tsq_attend_four.hip"]
+HEADERS = ["tsq_internal.hpp", "tsq_device.hpp", "tsq_pass.hpp", "tsq_ranges.hpp", "tsq_cache_internal.hpp", "tsq_attend.hpp", "tsq_four.hpp"] + \
     [os.path.join(ROOT, "include", h) for h in ("tsq.h", "tsq_measure.h", "tsq_ranges.h", "tsq_cache.h")]
 
 # -ffp-contract=off: the quantizer's multiply and every fp64 product of the budget test must

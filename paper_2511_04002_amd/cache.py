@@ -1,4 +1,4 @@
-"""Binding of the serving operators (include/tsq_cache.h): a key/value cache held in 8 bits and what fills and
+"""Binding of the serving operators (include/tsq_cache.h): a key/value cache held in 8 or 4 bits and what fills and
 reads it.  Argument marshalling and checks only; every step runs in the HIP kernels of libtsq.so.
 
 A step of one layer, for requests of any lengths, new or going on:
@@ -12,6 +12,9 @@ A step of one layer, for requests of any lengths, new or going on:
     out = c.attend(memory, q, table, s.starts, s.lengths, max_new, max_length)
     lengths, counters = s.lengths, s.counters         # what the next step begins with
 
+A cache in 4 bits is Cache(..., bits=4), with the same calls.  Where a token stands at a place on each of several axes, as
+those of images do, norm_rotate(..., positions [axes, tokens], ..., axes=c.new_axes(pairs of each axis)).
+
 All calls run on torch's current stream, and their tensors are on its device.  A tensor that is left out is allocated on it.
 """
 from __future__ import annotations
@@ -22,9 +25,11 @@ from . import tsq
 from .tsq import TSQ_OK, TsqError
 
 TSQ_PAIRS_HALVES, TSQ_PAIRS_NEIGHBOURS = 0, 1
+MAX_AXES = 4                                              # of a position
 _MOST = 2 ** 32 - 1                                       # (ctypes passes the lower 32 bits of what is larger)
 
 EXPORTS = ("tsq_cache_create", "tsq_cache_destroy", "tsq_cache_memory_sizes", "tsq_cache_schedule", "tsq_cache_norm_rotate",
+           "tsq_cache_create_bits", "tsq_cache_norm_rotate_axes",
            "tsq_cache_append", "tsq_cache_gather", "tsq_cache_attend", "tsq_cache_attend_workspace_bytes")
 
 
@@ -53,10 +58,12 @@ def lib():
         mem = C.POINTER(tsq_cache_memory)
         for name, res, args in (
                 ("tsq_cache_create", st, [C.POINTER(tsq_cache_config), C.POINTER(vp)]),
+                ("tsq_cache_create_bits", st, [C.POINTER(tsq_cache_config), u32, C.POINTER(vp)]),
                 ("tsq_cache_destroy", None, [vp]),
                 ("tsq_cache_memory_sizes", st, [vp, C.POINTER(tsq_cache_sizes)]),
                 ("tsq_cache_schedule", st, [vp, u32, vp, vp, vp, vp, vp, u32, vp, vp, vp, vp, vp, vp, vp]),
                 ("tsq_cache_norm_rotate", st, [vp, u32, vp, u64, vp, u64, vp, vp, u32, u32, i32, vp, vp, f32, vp, u64, vp, u64, vp]),
+                ("tsq_cache_norm_rotate_axes", st, [vp, u32, vp, u64, vp, u64, u32, vp, vp, vp, u32, u32, i32, vp, vp, f32, vp, u64, vp, u64, vp]),
                 ("tsq_cache_append", st, [vp, mem, u32, vp, u64, vp, u64, vp, vp]),
                 ("tsq_cache_gather", st, [vp, mem, u32, vp, vp, vp, u32, vp, u64, vp, u64, vp]),
                 ("tsq_cache_attend", st, [vp, mem, u32, vp, vp, vp, u32, u32, u32, vp, u64, f32, i32, u32, vp, u64, vp, vp, vp]),
@@ -81,6 +88,13 @@ def tsq_cache_create(cfg: tsq_cache_config) -> int:
     return h.value
 
 
+def tsq_cache_create_bits(cfg: tsq_cache_config, bits: int) -> int:
+    """-> opaque handle (int) of a cache in 8 or 4 bits.  Raises TsqError on a rejected configuration."""
+    h = C.c_void_p()
+    _done(lib().tsq_cache_create_bits(C.byref(cfg), bits, C.byref(h)), "tsq_cache_create_bits")
+    return h.value
+
+
 def tsq_cache_destroy(cache: int) -> None:
     lib().tsq_cache_destroy(cache)
 
@@ -99,19 +113,26 @@ def tsq_cache_attend_workspace_bytes(cache: int, requests: int, tokens: int, max
 
 class Memory:
     """The four tensors of one cache, and the C structure that holds their pointers: k int8 [blocks, kv_heads, block_tokens,
-    head_dim], v int8 [blocks, kv_heads, head_dim, block_tokens], scales float32 [blocks, kv_heads].  They are looked at once,
-    here, and stay what they are; a cache takes a memory of its own shape only."""
+    head_dim], v int8 [blocks, kv_heads, head_dim, block_tokens], scales float32 [blocks, kv_heads]; in 4 bits k and v uint8
+    [blocks, kv_heads, block_tokens, head_dim / 2], scales uint8 [blocks, kv_heads, head_dim / 32, block_tokens].  They are
+    looked at once, here, and stay what they are; a cache takes a memory of its own shape and bits only."""
 
     def __init__(self, k, v, k_scale, v_scale):
         import torch
         shape = tuple(k.shape)
         n, h, b, d = shape if len(shape) == 4 else (0, 0, 0, 0)
         device = k.get_device()
-        for x, size, kind in ((k, (n, h, b, d), torch.int8), (v, (n, h, d, b), torch.int8), (k_scale, (n, h), torch.float32), (v_scale, (n, h), torch.float32)):
+        bits = 4 if k.dtype is torch.uint8 else 8
+        if bits == 4:
+            codes, scales, of_codes, of_scales = (n, h, b, d), (n, h, d // 16, b), torch.uint8, torch.uint8
+            shape = (n, h, b, 2 * d)
+        else:
+            codes, scales, of_codes, of_scales = (n, h, d, b), (n, h), torch.int8, torch.float32
+        for x, size, kind in ((k, (n, h, b, d), of_codes), (v, codes, of_codes), (k_scale, scales, of_scales), (v_scale, scales, of_scales)):
             if not (x.is_cuda and x.get_device() == device and x.is_contiguous() and tuple(x.shape) == size and x.dtype == kind):
                 _refuse("a cache's tensor is %s on one GPU, contiguous, %s" % (size, kind))
         c = tsq_cache_memory(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
-        self.__dict__.update(k=k, v=v, k_scale=k_scale, v_scale=v_scale, shape=shape, device=device, c=c, ref=C.byref(c))
+        self.__dict__.update(k=k, v=v, k_scale=k_scale, v_scale=v_scale, shape=shape, bits=bits, device=device, c=c, ref=C.byref(c))
 
     def __setattr__(self, name, value):
         raise AttributeError("a memory's tensors are not replaced")
@@ -154,20 +175,22 @@ def _device() -> int:
 class Cache:
     """One tsq_cache plus helpers that allocate torch buffers, check them and pass their pointers."""
 
-    def __init__(self, blocks: int, block_tokens: int, q_heads: int, kv_heads: int, head_dim: int, dtype: str, max_blocks: int):
+    def __init__(self, blocks: int, block_tokens: int, q_heads: int, kv_heads: int, head_dim: int, dtype: str, max_blocks: int, bits: int = 8):
         import torch
         if dtype not in tsq._DTYPES:
             _refuse("dtype is 'f16' or 'bf16'")
+        if bits not in (8, 4):
+            _refuse("a cache has 8 or 4 bits")
         numbers = (blocks, block_tokens, q_heads, kv_heads, head_dim, max_blocks)
         if min(numbers) < 0 or max(numbers) > _MOST:
             _refuse("a cache's numbers are not negative, and have 32 bits")
         self.kind = torch.float16 if dtype == "f16" else torch.bfloat16
         self.int32, self.int64, self.float32 = torch.int32, torch.int64, torch.float32
         self.blocks, self.block_tokens, self.q_heads, self.kv_heads = blocks, block_tokens, q_heads, kv_heads
-        self.head_dim, self.dtype, self.max_blocks = head_dim, dtype, max_blocks
+        self.head_dim, self.dtype, self.max_blocks, self.bits = head_dim, dtype, max_blocks, bits
         self.shape = (blocks, kv_heads, block_tokens, head_dim)
         self.cfg = tsq_cache_config(blocks, block_tokens, q_heads, kv_heads, head_dim, tsq._DTYPES[dtype], max_blocks, 0)
-        self.handle = tsq_cache_create(self.cfg)
+        self.handle = tsq_cache_create_bits(self.cfg, bits)
         self._torch, self._lib = torch, lib()
 
     def __del__(self):
@@ -188,12 +211,17 @@ class Cache:
     def new_memory(self) -> Memory:
         t = self._torch
         n, h, b, d = self.blocks, self.kv_heads, self.block_tokens, self.head_dim
+        if self.bits == 4:
+            u8 = t.uint8
+            return Memory(self._empty((n, h, b, d // 2), u8), self._empty((n, h, b, d // 2), u8),
+                          self._empty((n, h, d // 32, b), u8), self._empty((n, h, d // 32, b), u8))
         return Memory(self._empty((n, h, b, d), t.int8), self._empty((n, h, d, b), t.int8),
                       self._empty((n, h), t.float32), self._empty((n, h), t.float32))
 
     def wrap(self, k, v, k_scale, v_scale) -> Memory:
         """A cache in tensors that are there: k [blocks, kv_heads, block_tokens, head_dim] int8,
-        v [blocks, kv_heads, head_dim, block_tokens] int8, scales [blocks, kv_heads] float32."""
+        v [blocks, kv_heads, head_dim, block_tokens] int8, scales [blocks, kv_heads] float32; in 4 bits k, v
+        [blocks, kv_heads, block_tokens, head_dim / 2] and scales [blocks, kv_heads, head_dim / 32, block_tokens], all uint8."""
         memory = Memory(k, v, k_scale, v_scale)
         self._memory(memory, memory.device)
         return memory
@@ -214,16 +242,35 @@ class Cache:
         e, i32 = self._empty, self.int32
         return Schedule(e(requests, i32), e(2, self.int64), e(requests + 1, i32), e(tokens, i32), e(tokens, i32), e(1, i32))
 
+    def new_axes(self, sections, order: str = "runs"):
+        """The axis of each pair of a rotation by positions on several axes: sections[x] pairs turn by axis x, "runs": those of
+        an axis one behind the other, "turns": dealt out in turn to the axes that have pairs left."""
+        left = [int(n) for n in sections]
+        if not 1 <= len(left) <= MAX_AXES or min(left) < 0 or sum(left) > self.head_dim // 2 or sum(left) % 8 or sum(left) == 0:
+            _refuse("sections are up to %d numbers of pairs, together a multiple of 8 of them up to head_dim / 2" % MAX_AXES)
+        if order != "runs" and order != "turns":
+            _refuse("order is 'runs' or 'turns'")
+        out = []
+        if order == "runs":
+            for axis, n in enumerate(left):
+                out += [axis] * n
+        while order == "turns" and any(left):
+            for axis, n in enumerate(left):
+                if n:
+                    out.append(axis)
+                    left[axis] -= 1
+        return self._torch.tensor(out, dtype=self._torch.uint8, device="cuda")
+
     # -------------------------------------------------------------- checks
 
     # (a step calls these for every tensor of every operator: what a tensor holds is told by its type, place and number
     # of elements, and its shape is looked at only where it is not contiguous; `device` is the current one)
 
     def _memory(self, memory, device):
-        if memory.device == device and memory.shape == self.shape:
+        if memory.device == device and memory.shape == self.shape and memory.bits == self.bits:
             return memory.ref
-        _refuse("the memory is that of a cache of %s on device %d, this one is %s, the current device %d (blocks, kv_heads, block_tokens, head_dim)"
-                % (memory.shape, memory.device, self.shape, device))
+        _refuse("the memory is that of a cache of %s in %d bits on device %d, this one is %s in %d, the current device %d (blocks, kv_heads, "
+                "block_tokens, head_dim)" % (memory.shape, memory.bits, memory.device, self.shape, self.bits, device))
 
     def _ints(self, x, n, what, device):
         if not (x.dtype is self.int32 and x.get_device() == device and x.numel() == n and x.is_contiguous()):
@@ -285,10 +332,11 @@ class Cache:
         return out
 
     def norm_rotate(self, q, k, positions, angles, q_weight=None, k_weight=None, eps: float = 1e-6, pairs: str = "halves",
-                    q_out=None, k_out=None):
+                    q_out=None, k_out=None, axes=None):
         """RMS norm of each head of q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim] (weights [head_dim],
         or None: no norm), then the rotation by position: angles [rows, rotary] float32 holds the cosines of a
-        position's rotary / 2 angles, then their sines.  q_out, k_out may be q, k themselves."""
+        position's rotary / 2 angles, then their sines.  q_out, k_out may be q, k themselves.
+        axes: uint8 [rotary / 2], the axis that each pair turns by (from new_axes); positions are then int32 [axes, tokens]."""
         tokens, device = q.shape[0], _device()
         qp, qs = self._rows(q, tokens, self.q_heads, "q", device)
         kp, ks = self._rows(k, tokens, self.kv_heads, "k", device)
@@ -299,12 +347,20 @@ class Cache:
         if pairs != "halves" and pairs != "neighbours":
             _refuse("pairs is 'halves' or 'neighbours'")
         known, rotary = angles.shape
-        status = self._lib.tsq_cache_norm_rotate(
-            self.handle, tokens, qp, qs, kp, ks, self._ints(positions, tokens, "positions", device), angles.data_ptr(), known, rotary,
-            TSQ_PAIRS_HALVES if pairs == "halves" else TSQ_PAIRS_NEIGHBOURS, self._weight(q_weight, device), self._weight(k_weight, device),
-            eps, qo, qos, ko, kos, self._stream())
+        rest = (angles.data_ptr(), known, rotary, TSQ_PAIRS_HALVES if pairs == "halves" else TSQ_PAIRS_NEIGHBOURS,
+                self._weight(q_weight, device), self._weight(k_weight, device), eps, qo, qos, ko, kos, self._stream())
+        if axes is None:
+            status = self._lib.tsq_cache_norm_rotate(self.handle, tokens, qp, qs, kp, ks, self._ints(positions, tokens, "positions", device), *rest)
+        else:
+            n = positions.shape[0] if positions.dim() == 2 else 0
+            if not 1 <= n <= MAX_AXES:
+                _refuse("with axes, positions is [axes, tokens], of 1 to %d axes" % MAX_AXES)
+            if not (axes.dtype is self._torch.uint8 and axes.get_device() == device and axes.is_contiguous() and axes.numel() == rotary // 2):
+                _refuse("axes is uint8 [rotary / 2] on the current GPU, contiguous")
+            status = self._lib.tsq_cache_norm_rotate_axes(self.handle, tokens, qp, qs, kp, ks, n, self._ints(positions, n * tokens, "positions", device),
+                                                          axes.data_ptr(), *rest)
         if status:
-            raise TsqError(status, "tsq_cache_norm_rotate")
+            raise TsqError(status, "tsq_cache_norm_rotate" if axes is None else "tsq_cache_norm_rotate_axes")
         return q_out, k_out
 
     def append(self, memory: Memory, k, v, slots) -> None:

@@ -17,138 +17,15 @@
 // a tile are dealt to the lanes such that nothing has to be moved.
 #include <hip/hip_runtime.h>
 
-#include "tsq_cache_internal.hpp"
+#include "tsq_attend.hpp"
 
 namespace tsq {
 namespace {
 
-constexpr float kNone = -0x1.fffffep127f;      // reference of a row that has seen nothing: below any score
 constexpr float kRoom = 7.0f;        // the reference is set this far below the largest exponent ...
 constexpr float kSlack = 8.0f;       // ... and kept until one exceeds that by as much
 constexpr float kCoarse = 0x1p22f;   // beyond this a reference's last bit is worth 1/2 or more: the difference of a score that
                                      // is not rounded and one that is would pass a half's range
-
-__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
-
-// The larger of a lane's value and that of the lane 32 away.
-__device__ __forceinline__ float max_across_halves(float x) {
-    const uint32_t bits = __builtin_bit_cast(uint32_t, x);
-    const auto r = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
-    const uint32_t a = r[0], b = r[1];                   // (a cast of an element itself would take the first)
-    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
-}
-
-// What a workgroup works on: a row tile of a request (rows: query token and head of the group, the group fastest),
-// a kv head, and a piece of the tile's reach along the cache.
-struct Place {
-    uint32_t h, split, r, tile;
-    uint32_t begin, n;               // the request's rows of the call
-    int32_t length;                  // as the caller gave it
-    uint32_t seen;                   // tokens that the table can hold of them
-    bool beyond, last;
-};
-
-template <int ROWS>
-__device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
-    uint32_t x = blockIdx.x;
-    p.h = x % a.kv_heads;
-    x /= a.kv_heads;
-    p.split = x % a.splits;
-    x = a.tiles - 1 - x / a.splits;  // the tiles with the most tokens before them first
-    uint32_t next;                   // tiles that the request has before the next one's begin
-    if (a.tiles_each) {
-        p.r = x / a.tiles_each;
-        p.tile = x % a.tiles_each;
-        next = a.tiles_each;
-        if (a.by_tile) {
-            p.r = x % a.requests;
-            p.tile = a.tiles_each - 1 - x / a.requests;
-        }
-        if (a.by_length) {
-            // the longest request first: p.r counts from the shortest here; each lane ranks one request
-            const uint32_t lane = threadIdx.x & 63;
-            const int32_t mine = lane < a.requests ? a.lengths[lane] : 0;
-            uint32_t below = 0;
-            for (uint32_t j = 0; j < a.requests; ++j) {
-                const int32_t other = __builtin_amdgcn_readlane(mine, (int)j);
-                below += other < mine || (other == mine && j < lane) ? 1 : 0;
-            }
-            p.r = (uint32_t)__builtin_ctzll(__ballot(lane < a.requests && below == p.r));
-        }
-    } else {
-        // request r begins at tile first(r) = rows before it / ROWS + r, which leaves it at least as many as it needs
-        uint32_t lo = 0, hi = a.requests;
-        const uint32_t lane = threadIdx.x & 63;
-        auto first = [&](uint32_t r) {
-            return (uint32_t)((uint64_t)min((uint32_t)max(a.starts[r], 0), a.tokens) * a.group / ROWS) + r;
-        };
-        while (hi - lo > 1) {        // a wave halves 64 times at once
-            const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-            const uint64_t below = __ballot(at < hi && first(at) <= x);
-            const uint32_t last = 63 - (uint32_t)__builtin_clzll(below | 1);
-            hi = min(hi, lo + (last + 1) * step);
-            lo += last * step;
-        }
-        p.r = lo;
-        const uint32_t f = first(lo);
-        p.tile = x - f;
-        next = first(lo + 1) - f;
-        if (x < f) return false;
-    }
-    const uint32_t b = min((uint32_t)max(a.starts[p.r], 0), a.tokens), e = min((uint32_t)max(a.starts[p.r + 1], 0), a.tokens);
-    p.begin = b;
-    p.n = e > b ? e - b : 0;
-    p.length = max(a.lengths[p.r], 0);
-    const uint64_t most = (uint64_t)a.max_blocks << a.block_log2;
-    p.beyond = (uint64_t)p.length > most;
-    p.seen = p.beyond ? (uint32_t)most : (uint32_t)p.length;
-    p.last = p.tile + 1 == next;
-    const uint32_t rows = p.n * a.group;
-    return p.tile * (uint64_t)ROWS < rows && rows >= a.rows_from && rows <= a.rows_to;
-}
-
-// Tokens that any row of a tile sees, the part of them that a split has, and what a row sees.
-struct Reach { uint32_t begin, end; };
-template <int ROWS>
-__device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Place &p, uint32_t tile) {
-    const int64_t rows = (int64_t)p.n * a.group, first = (int64_t)tile * ROWS, last = min(first + ROWS, rows) - 1;
-    const int64_t p0 = (int64_t)p.length - p.n + first / a.group, p1 = (int64_t)p.length - p.n + last / a.group;
-    int64_t lo = a.window ? max(p0 - (int64_t)a.window + 1, (int64_t)0) : 0;
-    int64_t hi = a.causal ? min(p1 + 1, (int64_t)p.seen) : (int64_t)p.seen;
-    lo &= ~(int64_t)127;             // (a whole tile's, and a block's)
-    const int64_t begin = lo + (int64_t)p.split * a.chunk;
-    if (p.split + 1 < a.splits) hi = min(hi, begin + a.chunk);
-    Reach w;
-    w.begin = (uint32_t)min(begin, (int64_t)0x7FFFFFC0);
-    w.end = hi > begin ? (uint32_t)hi : w.begin;
-    return w;
-}
-__device__ __forceinline__ void row_sees(const AttendArgs &a, const Place &p, uint32_t row, uint32_t &from, uint32_t &to) {
-    // (rows past the request's are computed along and not written: they ask for no mask)
-    if (row >= p.n * a.group) { from = 0; to = ~0u; return; }
-    const int64_t at = (int64_t)p.length - p.n + row / a.group;
-    const int64_t lo = a.window ? max(at - (int64_t)a.window + 1, (int64_t)0) : 0;
-    const int64_t hi = a.causal ? min(at + 1, (int64_t)p.seen) : (int64_t)p.seen;
-    from = (uint32_t)lo;
-    to = hi > lo ? (uint32_t)hi : 0u;
-}
-
-// A row of a request that is longer than its row of the table, and that sees anything of it: NaN, whatever it sees.  (Its
-// window may lie past all that the table holds, so that the tokens which are looked at cannot tell.)
-__device__ __forceinline__ bool is_lost(const AttendArgs &a, const Place &p, uint32_t row) {
-    return p.beyond && (!a.causal || (int64_t)p.length - p.n + row / a.group >= 0);
-}
-
-// The table's entry for the 16 tokens from `token` on, as it is (past the end of a reach: its last one, so that what is
-// asked for ahead of need is always there, and costs no new lines).  It is looked at when it is used, by id_of, so that
-// nothing waits for it before.
-__device__ __forceinline__ uint32_t table_entry(const AttendArgs &a, const Place &p, uint32_t token, uint32_t end) {
-    return (uint32_t)a.table[(uint64_t)p.r * a.max_blocks + (min(token, end - 1) >> a.block_log2)];
-}
-// A block's number, 0 for what is none; is_bad says which tokens are to come out as NaN for that.
-__device__ __forceinline__ uint32_t id_of(const AttendArgs &a, uint32_t entry) { return entry < a.blocks ? entry : 0; }
-__device__ __forceinline__ bool is_bad(const AttendArgs &a, const Place &p, uint32_t entry) { return entry >= a.blocks || p.beyond; }
 
 // What the tokens of a block have in common for a head: the factor of the scores, and the values' scale as log2 and
 // as reciprocal.  Values that are all 0 weigh nothing whatever their scale is: 2^-60 keeps their tokens in the
@@ -163,7 +40,7 @@ __device__ __forceinline__ bool is_far(float log_v) { return fabsf(log_v + 10.0f
 struct Scale { float k, v; bool bad; };
 __device__ __forceinline__ Scale scale_at(const AttendArgs &a, const Place &p, uint32_t entry) {
     const uint64_t at = (uint64_t)id_of(a, entry) * a.kv_heads + p.h;
-    return Scale{a.k_scale[at], a.v_scale[at], is_bad(a, p, entry)};
+    return Scale{static_cast<const float *>(a.k_scale)[at], static_cast<const float *>(a.v_scale)[at], is_bad(a, p, entry)};
 }
 struct Block { float c, log_v, back_v; };
 __device__ __forceinline__ Block block_of(Scale s, float row_factor, uint32_t mode) {
@@ -174,18 +51,6 @@ __device__ __forceinline__ Block block_of(Scale s, float row_factor, uint32_t mo
     return b;
 }
 struct Softmax { float ref, weight; };                   // of a row, from kScores
-
-// The kernel's arguments (its only parameter), read once more: what a tile's begin and end alone need then takes no scalar
-// registers in its loop.  A few too many cost k_attend_many the order of its loads and products (7 % of its time), and
-// k_attend_few with two sets vector registers that it has not (5 to 14 %).  Where there are enough, the first values serve:
-// reading them again is 0.2 us of a single token's 5.
-__device__ __forceinline__ AttendArgs args_again() {
-    struct Words { uint32_t w[sizeof(AttendArgs) / 4]; } words;
-    auto args = (const __attribute__((address_space(4))) uint32_t *)__builtin_amdgcn_kernarg_segment_ptr();
-    asm volatile("" : "+s"(args));
-    for (uint32_t i = 0; i < sizeof(AttendArgs) / 4; ++i) words.w[i] = args[i];
-    return __builtin_bit_cast(AttendArgs, words);
-}
 
 // What a row ends with: its statistics, and what its sums are to be multiplied by, f h h (h twice, since binary32 may
 // not hold its square).  The sums of a piece along the cache stay as they are; from kValues they become an average, which
@@ -235,27 +100,6 @@ __device__ __forceinline__ float query_factor(uint32_t most, float &back) {
     if (e < -100) e = -100;
     back = __builtin_bit_cast(float, (uint32_t)(e - 13 + 127) << 23);
     return __builtin_bit_cast(float, (uint32_t)(13 - e + 127) << 23);
-}
-
-// Where a row's result goes.
-__device__ __forceinline__ uint64_t row_id(const AttendArgs &a, const Place &p, uint32_t row) {
-    return (uint64_t)(p.begin + row / a.group) * a.q_heads + p.h * a.group + row % a.group;
-}
-
-// ... and its row of the parts.
-__device__ __forceinline__ uint64_t part_row(const AttendArgs &a, const Place &p, uint32_t row) {
-    return a.slots_each ? ((uint64_t)p.r * a.slots_each + row) * a.kv_heads + p.h : row_id(a, p, row);
-}
-
-// A piece that lies behind a tile's reach: no row sees anything, and that is all that the join has to know (of a weight
-// of NaN, too, whatever the sums are).
-template <int ROWS>
-__device__ __forceinline__ void nothing_seen(const AttendArgs &a, const Place &p, uint32_t tile, int head_dim) {
-    const uint32_t row = tile * ROWS + threadIdx.x;
-    if (threadIdx.x >= ROWS || row >= p.n * a.group) return;
-    float *st = a.parts + a.part_rows * a.splits * head_dim + (part_row(a, p, row) * a.splits + p.split) * 2;
-    st[0] = kNone;
-    st[1] = is_lost(a, p, row) ? __builtin_nanf("") : 0.0f;
 }
 
 // Few rows: 16 of a kv head's, or 32 (SETS = 2, which share the codes once they are halves).  Each of four waves takes
@@ -340,7 +184,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
         // when that one's are used up, and its block numbers a tile earlier still.
         uint4_t kw[4][F], vw[D / 16];
         Scale scale = {};
-        const int8_t *my_keys = a.k + (m & 3) * D + 16 * g;
+        const int8_t *my_keys = static_cast<const int8_t *>(a.k) + (m & 3) * D + 16 * g;
         auto ask_keys = [&](uint32_t t0, uint32_t entry) {
             const uint32_t key_id = (uint32_t)__shfl((int)id_of(a, entry), (int)(m >> 2) << 4), token = t0 + 16 * (m >> 2);
             const int8_t *keys = my_keys + (((uint64_t)key_id * a.kv_heads + p.h) * B + (token & (B - 1))) * D;
@@ -350,7 +194,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
                 for (int f = 0; f < F; ++f) kw[t][f] = *reinterpret_cast<const uint4_t *>(keys + 4 * t * D + 64 * f);
         };
         auto ask_values = [&](uint32_t t0, uint32_t entry) {
-            const int8_t *values = a.v + (((uint64_t)id_of(a, entry) * a.kv_heads + p.h) * D + m) * B + ((t0 + 16 * g) & (B - 1));
+            const int8_t *values = static_cast<const int8_t *>(a.v) + (((uint64_t)id_of(a, entry) * a.kv_heads + p.h) * D + m) * B + ((t0 + 16 * g) & (B - 1));
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) vw[d] = *reinterpret_cast<const uint4_t *>(values + (uint64_t)(16 * d) * B);
         };
@@ -603,8 +447,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uint32_t e = i * THREADS + tid;
-            keys[i] = a.k + (uint64_t)p.h * B * D + (e / (D / 16) & (B - 1)) * D + 16 * (e % (D / 16));
-            values[i] = a.v + (uint64_t)p.h * B * D + (uint64_t)(e / SUBS) * B + (16 * (tid % SUBS) & (B - 1));
+            keys[i] = static_cast<const int8_t *>(a.k) + (uint64_t)p.h * B * D + (e / (D / 16) & (B - 1)) * D + 16 * (e % (D / 16));
+            values[i] = static_cast<const int8_t *>(a.v) + (uint64_t)p.h * B * D + (uint64_t)(e / SUBS) * B + (16 * (tid % SUBS) & (B - 1));
         }
         Scale scale = {};
         auto ask_entries = [&](uint32_t t0) {
@@ -932,7 +776,7 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
         l.tiles = (uint32_t)(l.tiles_each ? (uint64_t)l.tiles_each * requests : packed);
     };
     uint64_t slots;
-    if (most <= few) {
+    if (most <= few || s.bits == 4) {
         tile(most <= 16 || s.head_dim == 256 ? 16 : 32);
         slots = s.head_dim == 256 ? 256 : s.head_dim == 128 || l.rows == 32 ? 512 : 768;
     } else {
@@ -1003,7 +847,8 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
     if (!fits(all, l.rows == 256 ? 512 : 256) || !fits(few, 256) || !(one_wave ? fits((joined + 3) / 4, 256) : fits(joined, 512))) return kTooLarge;
     const uint32_t grid = (uint32_t)all;
     const JoinArgs j = {a, reinterpret_cast<float *>(reinterpret_cast<char *>(a.parts) + l.few_at), l.few_part_rows, l.few_splits, l.slots_each};
-    by_shape(s, [&](auto d, auto bf16) {
+    if (s.bits == 4) launch_attend_four(s, l.rows, grid, a, stream);
+    else by_shape(s, [&](auto d, auto bf16) {
         if (l.rows == 16) k_attend_few<d(), bf16(), 1><<<grid, 256, 0, st>>>(a);
         else if (l.rows == 32) { if constexpr (d() != 256) k_attend_few<d(), bf16(), 2><<<grid, 256, 0, st>>>(a); }
         else if (l.rows == 128) k_attend_many<d(), bf16(), 4, 64><<<grid, 256, 0, st>>>(a);

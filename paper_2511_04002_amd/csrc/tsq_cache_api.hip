@@ -35,8 +35,10 @@ bool bad_words(const void *p) { return !p || misaligned(p, 4); }
 
 extern "C" {
 
-tsq_status tsq_cache_create(const tsq_cache_config *cfg, tsq_cache **out) {
-    if (!cfg || !out) return TSQ_ERR_INVALID_ARG;
+tsq_status tsq_cache_create(const tsq_cache_config *cfg, tsq_cache **out) { return tsq_cache_create_bits(cfg, 8, out); }
+
+tsq_status tsq_cache_create_bits(const tsq_cache_config *cfg, uint32_t bits, tsq_cache **out) {
+    if (!cfg || !out || (bits != 8 && bits != 4)) return TSQ_ERR_INVALID_ARG;
     if (cfg->blocks == 0 || cfg->q_heads == 0 || cfg->kv_heads == 0 || cfg->head_dim == 0 || cfg->max_blocks == 0 ||
         cfg->block_tokens == 0 || cfg->reserved != 0)
         return TSQ_ERR_INVALID_ARG;
@@ -50,7 +52,7 @@ tsq_status tsq_cache_create(const tsq_cache_config *cfg, tsq_cache **out) {
     tsq_cache *c = new (std::nothrow) tsq_cache();
     if (!c) return TSQ_ERR_NO_MEMORY;
     c->s = CacheShape{cfg->blocks, b, b == 16 ? 4u : b == 32 ? 5u : b == 64 ? 6u : 7u, cfg->q_heads, cfg->kv_heads, d,
-                      cfg->max_blocks, cfg->dtype == TSQ_BF16};
+                      cfg->max_blocks, cfg->dtype == TSQ_BF16, bits};
     *out = c;
     return TSQ_OK;
 }
@@ -59,8 +61,9 @@ void tsq_cache_destroy(tsq_cache *cache) { delete cache; }
 
 tsq_status tsq_cache_memory_sizes(const tsq_cache *c, tsq_cache_sizes *out) {
     if (!c || !out) return TSQ_ERR_INVALID_ARG;
-    out->code_bytes = (uint64_t)c->s.blocks * c->s.kv_heads * c->s.block_tokens * c->s.head_dim;
-    out->scale_bytes = 4ull * c->s.blocks * c->s.kv_heads;
+    const uint64_t heads = (uint64_t)c->s.blocks * c->s.kv_heads, elements = heads * c->s.block_tokens * c->s.head_dim;
+    out->code_bytes = c->s.bits == 4 ? elements / 2 : elements;
+    out->scale_bytes = c->s.bits == 4 ? elements / 32 : 4 * heads;
     return TSQ_OK;
 }
 
@@ -94,10 +97,15 @@ tsq_status tsq_cache_schedule(const tsq_cache *c, uint32_t requests, const void 
     return hip_rc(launch_schedule(a, stream));
 }
 
-tsq_status tsq_cache_norm_rotate(const tsq_cache *c, uint32_t tokens, const void *d_q, uint64_t q_stride, const void *d_k,
-                                 uint64_t k_stride, const void *d_positions, const void *d_angles, uint32_t angle_rows,
-                                 uint32_t rotary, int32_t pairs, const void *d_q_weight, const void *d_k_weight, float eps,
-                                 void *d_q_out, uint64_t q_out_stride, void *d_k_out, uint64_t k_out_stride, void *stream) {
+}  // extern "C"
+
+namespace {
+
+// axes 0: one row of positions, and d_axis is not used
+tsq_status norm_rotate(const tsq_cache *c, uint32_t tokens, const void *d_q, uint64_t q_stride, const void *d_k, uint64_t k_stride,
+                       uint32_t axes, const void *d_positions, const void *d_axis, const void *d_angles, uint32_t angle_rows,
+                       uint32_t rotary, int32_t pairs, const void *d_q_weight, const void *d_k_weight, float eps, void *d_q_out,
+                       uint64_t q_out_stride, void *d_k_out, uint64_t k_out_stride, void *stream) {
     if (!c || (pairs != TSQ_PAIRS_HALVES && pairs != TSQ_PAIRS_NEIGHBOURS) || !(eps >= 0.0f) || std::isinf(eps) || tokens >= (1u << 31))
         return TSQ_ERR_INVALID_ARG;
     const uint32_t d = c->s.head_dim;
@@ -116,7 +124,31 @@ tsq_status tsq_cache_norm_rotate(const tsq_cache *c, uint32_t tokens, const void
     a.q_stride = q_stride; a.k_stride = k_stride; a.q_out_stride = q_out_stride; a.k_out_stride = k_out_stride;
     a.tokens = tokens; a.angle_rows = angle_rows; a.rotary = rotary; a.neighbours = pairs == TSQ_PAIRS_NEIGHBOURS;
     a.q_heads = c->s.q_heads; a.kv_heads = c->s.kv_heads; a.eps = eps;
+    a.axes = axes; a.axis = static_cast<const uint8_t *>(d_axis);
     return hip_rc(launch_norm_rotate(c->s, a, stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+tsq_status tsq_cache_norm_rotate(const tsq_cache *c, uint32_t tokens, const void *d_q, uint64_t q_stride, const void *d_k,
+                                 uint64_t k_stride, const void *d_positions, const void *d_angles, uint32_t angle_rows,
+                                 uint32_t rotary, int32_t pairs, const void *d_q_weight, const void *d_k_weight, float eps,
+                                 void *d_q_out, uint64_t q_out_stride, void *d_k_out, uint64_t k_out_stride, void *stream) {
+    return norm_rotate(c, tokens, d_q, q_stride, d_k, k_stride, 0, d_positions, nullptr, d_angles, angle_rows, rotary, pairs, d_q_weight,
+                       d_k_weight, eps, d_q_out, q_out_stride, d_k_out, k_out_stride, stream);
+}
+
+tsq_status tsq_cache_norm_rotate_axes(const tsq_cache *c, uint32_t tokens, const void *d_q, uint64_t q_stride, const void *d_k,
+                                      uint64_t k_stride, uint32_t axes, const void *d_positions, const void *d_axis,
+                                      const void *d_angles, uint32_t angle_rows, uint32_t rotary, int32_t pairs,
+                                      const void *d_q_weight, const void *d_k_weight, float eps, void *d_q_out,
+                                      uint64_t q_out_stride, void *d_k_out, uint64_t k_out_stride, void *stream) {
+    if (axes == 0 || axes > kMaxAxes) return TSQ_ERR_INVALID_ARG;
+    if (tokens && (!d_axis || misaligned(d_axis, 8))) return TSQ_ERR_INVALID_ARG;
+    return norm_rotate(c, tokens, d_q, q_stride, d_k, k_stride, axes, d_positions, d_axis, d_angles, angle_rows, rotary, pairs, d_q_weight,
+                       d_k_weight, eps, d_q_out, q_out_stride, d_k_out, k_out_stride, stream);
 }
 
 tsq_status tsq_cache_append(const tsq_cache *c, const tsq_cache_memory *m, uint32_t tokens, const void *d_k, uint64_t k_stride,
@@ -125,6 +157,15 @@ tsq_status tsq_cache_append(const tsq_cache *c, const tsq_cache_memory *m, uint3
     if (tokens == 0) return TSQ_OK;
     const uint64_t w = (uint64_t)c->s.kv_heads * c->s.head_dim;
     if (bad_rows(d_k, k_stride, w, tokens) || bad_rows(d_v, v_stride, w, tokens) || bad_words(d_slots)) return TSQ_ERR_INVALID_ARG;
+    if (c->s.bits == 4) {
+        AppendFourArgs a;
+        a.k = d_k; a.v = d_v; a.k_stride = k_stride; a.v_stride = v_stride;
+        a.k_codes = static_cast<uint8_t *>(m->d_k); a.v_codes = static_cast<uint8_t *>(m->d_v);
+        a.k_scale = static_cast<uint8_t *>(m->d_k_scale); a.v_scale = static_cast<uint8_t *>(m->d_v_scale);
+        a.slots = static_cast<const int32_t *>(d_slots);
+        a.tokens = tokens; a.kv_heads = c->s.kv_heads; a.blocks = c->s.blocks; a.block_log2 = c->s.block_log2;
+        return hip_rc(launch_append_four(c->s, a, stream));
+    }
     AppendArgs a;
     a.x[0] = d_k; a.x[1] = d_v;
     a.stride[0] = k_stride; a.stride[1] = v_stride;
@@ -149,15 +190,15 @@ tsq_status tsq_cache_gather(const tsq_cache *c, const tsq_cache_memory *m, uint3
     GatherArgs a;
     a.out[0] = d_k_out; a.out[1] = d_v_out;
     a.stride[0] = k_out_stride; a.stride[1] = v_out_stride;
-    a.codes[0] = static_cast<const int8_t *>(m->d_k); a.codes[1] = static_cast<const int8_t *>(m->d_v);
-    a.scale[0] = static_cast<const float *>(m->d_k_scale); a.scale[1] = static_cast<const float *>(m->d_v_scale);
+    a.codes[0] = m->d_k; a.codes[1] = m->d_v;
+    a.scale[0] = m->d_k_scale; a.scale[1] = m->d_v_scale;
     a.table = static_cast<const int32_t *>(d_table);
     a.starts = static_cast<const int32_t *>(d_starts);
     a.lengths = static_cast<const int32_t *>(d_lengths);
     a.requests = requests; a.tokens = tokens; a.kv_heads = c->s.kv_heads; a.blocks = c->s.blocks;
     a.block_tokens = c->s.block_tokens; a.block_log2 = c->s.block_log2; a.max_blocks = c->s.max_blocks;
     a.waves_each = 0;
-    return hip_rc(launch_gather(c->s, a, stream));
+    return hip_rc(c->s.bits == 4 ? launch_gather_four(c->s, a, stream) : launch_gather(c->s, a, stream));
 }
 
 size_t tsq_cache_attend_workspace_bytes(const tsq_cache *c, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length,
@@ -180,8 +221,7 @@ tsq_status tsq_cache_attend(const tsq_cache *c, const tsq_cache_memory *m, uint3
     const AttendLaunch l = attend_launch(c->s, requests, tokens, max_new, max_length, window);
     if (l.workspace && (!d_ws || misaligned(d_ws, 256))) return TSQ_ERR_INVALID_ARG;
     AttendArgs a;
-    a.k = static_cast<const int8_t *>(m->d_k); a.v = static_cast<const int8_t *>(m->d_v);
-    a.k_scale = static_cast<const float *>(m->d_k_scale); a.v_scale = static_cast<const float *>(m->d_v_scale);
+    a.k = m->d_k; a.v = m->d_v; a.k_scale = m->d_k_scale; a.v_scale = m->d_v_scale;
     a.table = static_cast<const int32_t *>(d_table);
     a.starts = static_cast<const int32_t *>(d_starts);
     a.lengths = static_cast<const int32_t *>(d_lengths);

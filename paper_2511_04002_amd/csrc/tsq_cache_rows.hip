@@ -8,8 +8,6 @@
 namespace tsq {
 namespace {
 
-// a wave's number in its workgroup, as a value that the compiler knows to be the wave's
-__device__ __forceinline__ uint32_t wave_in_group() { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 __device__ __forceinline__ uint32_t of_lane(uint32_t v, uint32_t l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)l); }
 
 constexpr uint32_t kScheduleThreads = 1024;
@@ -190,28 +188,55 @@ __global__ __launch_bounds__(kScheduleThreads) void k_schedule(ScheduleArgs a) {
 // together are the lane's own: D / 16 lanes a head, 1024 / D heads a wave.  The sum of squares, the product with the
 // weight and the rotation stay in registers, in binary32; memory is read and written once, and bounds it: 8192 rows of
 // 72 heads of 128 are 306 MB and 54 us, 5.7 TB/s where a copy reaches 6.2.
-template <int D, bool BF16>
+template <int D, bool BF16, bool AXES>
 __global__ __launch_bounds__(256) void k_norm_rotate(NormRotateArgs a, uint32_t passes, uint32_t waves_each) {
     constexpr int LPH = D / 16, HEADS = 64 / LPH;
     const uint32_t lane = threadIdx.x & 63, wave = blockIdx.x * 4 + wave_in_group();
     const uint32_t token = wave / waves_each;
     if (token >= a.tokens) return;
     const int32_t position = a.positions[token];
-    if (position < 0) return;
+    int32_t others[kMaxAxes - 1];                        // ... and on the axes after the first
+    bool known = (uint32_t)position < a.angle_rows;
+    if constexpr (AXES) {
+        int32_t least = position;
+        for (uint32_t x = 1; x < kMaxAxes; ++x) {
+            others[x - 1] = x < a.axes ? a.positions[(uint64_t)x * a.tokens + token] : 0;
+            least = min(least, others[x - 1]);
+            known &= x >= a.axes || (uint32_t)others[x - 1] < a.angle_rows;
+        }
+        if (least < 0) return;
+    } else if (position < 0) return;
     const uint32_t j = lane % LPH, sub = lane / LPH, turning = a.rotary / 16;
     uint32_t e0, e1;                                    // first elements of the lane's two pieces
     const bool turns = j < turning;
     if (a.neighbours || !turns) { e0 = 16 * j; e1 = 16 * j + 8; }
     else { e0 = 8 * j; e1 = 8 * j + a.rotary / 2; }
     float c[8], s[8];
-    if (turns && (uint32_t)position < a.angle_rows) {
+    if (turns && known) {
         const float *row = a.angles + (uint64_t)position * a.rotary + 8 * j;
-        for (int i = 0; i < 8; i += 4) {
-            *reinterpret_cast<float4_t *>(c + i) = *reinterpret_cast<const float4_t *>(row + i);
-            *reinterpret_cast<float4_t *>(s + i) = *reinterpret_cast<const float4_t *>(row + a.rotary / 2 + i);
+        bool together = true;
+        if constexpr (AXES) {
+            // the pairs' angles are those of their axes' rows; where a lane's eight have one axis, as most have, in two loads
+            const uint2_t axis = *reinterpret_cast<const uint2_t *>(a.axis + 8 * j);
+            auto place_on = [&](uint32_t x) { return x == 0 ? position : x == 1 ? others[0] : x == 2 ? others[1] : others[2]; };
+            const uint32_t first = axis[0] & 0xFFu;
+            together = axis[0] == axis[1] && axis[0] == first * 0x01010101u && first < a.axes;
+            row = a.angles + (uint64_t)(uint32_t)place_on(first) * a.rotary + 8 * j;
+            if (!together)
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t x = axis[i / 4] >> 8 * (i % 4) & 0xFFu;
+                    const float *at = a.angles + (uint64_t)(uint32_t)place_on(x) * a.rotary + 8 * j + i;
+                    c[i] = x < a.axes ? at[0] : __builtin_nanf("");
+                    s[i] = x < a.axes ? at[a.rotary / 2] : __builtin_nanf("");
+                }
         }
+        if (together)
+            for (int i = 0; i < 8; i += 4) {
+                *reinterpret_cast<float4_t *>(c + i) = *reinterpret_cast<const float4_t *>(row + i);
+                *reinterpret_cast<float4_t *>(s + i) = *reinterpret_cast<const float4_t *>(row + a.rotary / 2 + i);
+            }
     } else {
-        const float one = (uint32_t)position < a.angle_rows ? 1.0f : __builtin_nanf("");
+        const float one = known ? 1.0f : __builtin_nanf("");
         for (int i = 0; i < 8; ++i) { c[i] = one; s[i] = one - one; }
     }
     const uint32_t heads = a.q_heads + a.kv_heads;
@@ -641,44 +666,17 @@ __global__ __launch_bounds__(256, D == 256 ? 3 : 4) void k_append(AppendArgs a) 
 // 32 heads, from blocks of 16, is 50 MB and 9 to 10 us.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void k_gather(GatherArgs a) {
+    const int8_t *codes[2] = {static_cast<const int8_t *>(a.codes[0]), static_cast<const int8_t *>(a.codes[1])};
+    const float *scales[2] = {static_cast<const float *>(a.scale[0]), static_cast<const float *>(a.scale[1])};
     const uint32_t lane = threadIdx.x & 63, B = a.block_tokens;
     // the four waves of a workgroup have the same heads of rows that follow one another: of blocks of more than 16
     // tokens they read neighbouring pieces of the same lines
     const uint64_t begin = ((uint64_t)(blockIdx.x / a.waves_each) * 4 + wave_in_group()) * 16;
     if (begin >= a.tokens) return;
-    const uint32_t i = (uint32_t)begin + (lane & 15);
-    // the last request that begins at or before the first row, 64 requests at a time, ...
-    uint32_t lo = 0, hi = a.requests;
-    while (hi - lo > 1) {
-        const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-        const uint64_t below = __ballot(at < hi && a.starts[at] <= (int32_t)begin);
-        const uint32_t last = 63 - (uint32_t)__builtin_clzll(below | 1);
-        hi = min(hi, lo + (last + 1) * step);
-        lo += last * step;
-    }
-    // ... and the others' among the 64 that follow, or by search where those all begin in these rows
-    const int32_t next = lo + 1 + lane < a.requests ? a.starts[lo + 1 + lane] : 0x7FFFFFFF;
-    uint32_t r = lo;
-    if (__builtin_expect(__ballot(next <= (int32_t)(begin + 15)) != ~0ull, 1)) {
-        for (uint32_t j = 0; j < 16; ++j) {
-            const uint32_t passed = (uint32_t)__builtin_popcountll(__ballot(next <= (int32_t)(begin + j)));
-            if ((lane & 15) == j) r = lo + passed;
-        }
-    } else {
-        uint32_t top = a.requests;
-        while (top - r > 1) {
-            const uint32_t mid = (r + top) >> 1;
-            if (a.starts[mid] <= (int32_t)i) r = mid; else top = mid;
-        }
-    }
-    const int32_t s0 = a.starts[r], s1 = a.starts[r + 1];
-    const bool owned = i < a.tokens && s0 >= 0 && (int32_t)i >= s0 && (int32_t)i < s1;
-    const int64_t position = (int64_t)a.lengths[r] - s1 + (int32_t)i;
-    const uint32_t nth = (uint32_t)((uint64_t)position >> a.block_log2);
-    int32_t block = -1;
-    if (owned && position >= 0 && ((uint64_t)position >> a.block_log2) < a.max_blocks) block = a.table[(uint64_t)r * a.max_blocks + nth];
-    if ((uint32_t)block >= a.blocks) block = -1;
-    const uint32_t place = (uint32_t)position & (B - 1);
+    const GatherRow row = gather_row(a, begin);
+    const uint32_t r = row.r, nth = row.nth, place = row.place;
+    const int32_t block = row.block;
+    const bool owned = row.owned;
     // keys: each row by itself, wherever it lies
     constexpr uint32_t LPT = D / 8, TPI = 64 / LPT, LOADS = 16 / TPI;
     constexpr int E = D / 64;
@@ -699,8 +697,8 @@ __global__ __launch_bounds__(256) void k_gather(GatherArgs a) {
 #pragma unroll
         for (uint32_t t = 0; t < LOADS; ++t) {
             const uint64_t head = (uint64_t)((int32_t)key_block[t] < 0 ? 0 : key_block[t]) * a.kv_heads + h;
-            kw[t] = *reinterpret_cast<const uint2_t *>(a.codes[0] + (head * B + key_place[t]) * D + 8 * piece);
-            k_scale[t] = a.scale[0][head];
+            kw[t] = *reinterpret_cast<const uint2_t *>(codes[0] + (head * B + key_place[t]) * D + 8 * piece);
+            k_scale[t] = scales[0][head];
         }
         uint32_t left = runs;
         bool keys_done = false;
@@ -715,8 +713,8 @@ __global__ __launch_bounds__(256) void k_gather(GatherArgs a) {
             const int32_t b = some ? (int32_t)of_lane((uint32_t)block, l) : -1;
             const uint32_t o = of_lane(place, l), first = o / 16 * 16;
             const uint64_t head = (uint64_t)max(b, 0) * a.kv_heads + h;
-            const float v_scale = b < 0 ? __builtin_nanf("") : a.scale[1][head];
-            const int8_t *values = a.codes[1] + (head * D + E * lane) * B + first;
+            const float v_scale = b < 0 ? __builtin_nanf("") : scales[1][head];
+            const int8_t *values = codes[1] + (head * D + E * lane) * B + first;
             uint16_t *v_out = static_cast<uint16_t *>(a.out[1]) + (begin + l) * a.stride[1] + (uint64_t)h * D;
             uint4_t vw[E], vx[E];
 #pragma unroll
@@ -769,14 +767,6 @@ __global__ __launch_bounds__(256) void k_gather(GatherArgs a) {
     }
 }
 
-// A grid of n waves in workgroups of four.
-int workgroups(uint64_t waves, uint32_t *out) {
-    const uint64_t n = (waves + 3) / 4;
-    if (!fits(n, 256)) return kTooLarge;
-    *out = (uint32_t)n;
-    return 0;
-}
-
 }  // namespace
 
 int launch_schedule(const ScheduleArgs &a, void *stream) {
@@ -798,7 +788,10 @@ int launch_norm_rotate(const CacheShape &s, const NormRotateArgs &a, void *strea
     // wave 64; 2048 rows 13.6 against 16.0); a pass a wave while there are fewer waves than the device holds at once
     const uint32_t each = (uint64_t)a.tokens * passes <= 4096 ? passes : (passes + 2) / 3;
     if (int e = workgroups((uint64_t)a.tokens * each, &grid)) return e;
-    by_shape(s, [&](auto d, auto bf16) { k_norm_rotate<d(), bf16()><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, passes, each); });
+    by_shape(s, [&](auto d, auto bf16) {
+        if (a.axes) k_norm_rotate<d(), bf16(), true><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, passes, each);
+        else k_norm_rotate<d(), bf16(), false><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, passes, each);
+    });
     return (int)hipGetLastError();
 }
 

@@ -1,12 +1,13 @@
 """Both ends of a split model's hand-over, with the cache's operators: the sender prefills prompts of several lengths into
-its own 8-bit caches (one a layer), reads the keys and values back, compresses them (TS + TAB-Q, one blob for all layers)
+its own 8-bit or 4-bit caches (one a layer), reads the keys and values back, compresses them (TS + TAB-Q, one blob for all layers)
 and sends the blob; the receiver restores it, stores the rows in caches of its own - other blocks, another block size -
 and goes on with single tokens, next to the sender doing the same, so that the two can be compared.
 
-    python -m paper_2511_04002_amd.serve [--requests 8] [--prompt 700] [--layers 4] [--steps 32] [--dtype bf16]
+    python -m paper_2511_04002_amd.serve [--requests 8] [--prompt 700] [--layers 4] [--steps 32] [--dtype bf16] [--bits 8] [--images]
 
 The layers are attention blocks with random weights (norm of queries and keys, rotation, attention, output projection,
-residual): what is measured is the operators, not a model's answers.
+residual): what is measured is the operators, not a model's answers.  With --images each prompt is a picture between two
+runs of text, whose tokens stand at places of their own in time, height and width.
 """
 from __future__ import annotations
 
@@ -22,8 +23,9 @@ class Side:
         from . import cache
         self.m, self.requests = model, requests
         each = -(-longest // block)
-        self.c = cache.Cache(requests * each, block, model.q_heads, model.kv_heads, model.dim, model.dtype, each)
+        self.c = cache.Cache(requests * each, block, model.q_heads, model.kv_heads, model.dim, model.dtype, each, bits=model.bits)
         self.memory = [self.c.new_memory() for _ in model.qkv]
+        self.axes = None if model.sections is None else self.c.new_axes(model.sections)
         self.table, self.ring = self.c.new_table(requests), self.c.new_ring()
         self.lengths, self.counters = self.c.new_lengths(requests), self.c.new_counters()
 
@@ -41,7 +43,8 @@ class Side:
         for memory, w_qkv, w_out in zip(self.memory, m.qkv, m.out):
             qkv = x @ w_qkv
             q, k = qkv[:, :m.q_width], qkv[:, m.q_width:m.q_width + m.kv_width]
-            q, k = c.norm_rotate(q, k, s.positions, m.angles, m.weight, m.weight)
+            places = s.positions if self.axes is None else m.places(s.positions)
+            q, k = c.norm_rotate(q, k, places, m.angles, m.weight, m.weight, axes=self.axes)
             c.append(memory, k, qkv[:, m.q_width + m.kv_width:], s.slots)
             x = x + c.attend(memory, q, self.table, s.starts, s.lengths, max_new, max_length).flatten(1) @ w_out
         return x
@@ -64,13 +67,13 @@ class Side:
 class Layers:
     """Random weights of the attention blocks."""
 
-    def __init__(self, layers: int, q_heads: int, kv_heads: int, dim: int, dtype: str, longest: int, seed: int = 0):
+    def __init__(self, layers: int, q_heads: int, kv_heads: int, dim: int, dtype: str, longest: int, seed: int = 0, bits: int = 8, images: bool = False):
         import torch
         g = torch.Generator(device="cuda")
         g.manual_seed(seed)
         kind = torch.float16 if dtype == "f16" else torch.bfloat16
         self.q_heads, self.kv_heads, self.dim, self.dtype = q_heads, kv_heads, dim, dtype
-        self.q_width, self.kv_width = q_heads * dim, kv_heads * dim
+        self.q_width, self.kv_width, self.bits, self.sections = q_heads * dim, kv_heads * dim, bits, None
         hidden = self.q_width
 
         def randn(*shape, scale):
@@ -83,10 +86,27 @@ class Layers:
         angle = torch.arange(longest, device="cuda", dtype=torch.float64)[:, None] * rate
         self.angles = torch.cat((angle.cos(), angle.sin()), 1).float()
         self.generator, self.randn = g, randn
+        if images:
+            # time, height and width: a quarter of the pairs, and three eighths each
+            part = dim // 2 // 8
+            self.sections = (2 * part, 3 * part, 3 * part)
+
+    PICTURE = (20, 12, 8)                                 # where it begins, its width and height
+
+    def places(self, positions):
+        """[3, tokens]: the tokens of the picture stand at one time, each at its line and column; text goes on behind them."""
+        import torch
+        first, wide, high = self.PICTURE
+        behind, inside = positions - first - wide * high, positions - first
+        seen = (inside >= 0) & (behind < 0)
+        after = torch.where(behind >= 0, first + max(wide, high) + behind, positions)
+        return torch.stack((torch.where(seen, first, after), torch.where(seen, first + inside // wide, after),
+                            torch.where(seen, first + inside % wide, after))).to(torch.int32)
 
 
 def run(requests: int = 8, prompt: int = 700, layers: int = 4, steps: int = 32, q_heads: int = 32, kv_heads: int = 8,
-        dim: int = 128, dtype: str = "bf16", bits=(4, 6, 8), budget: float = 0.01, seed: int = 0) -> Dict[str, float]:
+        dim: int = 128, dtype: str = "bf16", bits=(4, 6, 8), budget: float = 0.01, seed: int = 0, cache_bits: int = 8,
+        images: bool = False) -> Dict[str, float]:
     """-> what was sent, and how far the receiver's steps are from the sender's."""
     import torch
 
@@ -94,7 +114,7 @@ def run(requests: int = 8, prompt: int = 700, layers: int = 4, steps: int = 32, 
     longest = prompt + steps
     prompts = [max(1, prompt * (r + 1) // requests) for r in range(requests)]
     total = sum(prompts)
-    m = Layers(layers, q_heads, kv_heads, dim, dtype, longest, seed)
+    m = Layers(layers, q_heads, kv_heads, dim, dtype, longest, seed, cache_bits, images)
     sender, receiver = Side(m, requests, longest, 16), Side(m, requests, longest, 32)
 
     s = sender.schedule(prompts)
@@ -127,8 +147,10 @@ def main() -> None:
     for name, value in (("requests", 8), ("prompt", 700), ("layers", 4), ("steps", 32), ("q-heads", 32), ("kv-heads", 8), ("dim", 128)):
         p.add_argument("--" + name, type=int, default=value)
     p.add_argument("--dtype", choices=("f16", "bf16"), default="bf16")
+    p.add_argument("--bits", type=int, choices=(8, 4), default=8, help="of the caches")
+    p.add_argument("--images", action="store_true")
     a = p.parse_args()
-    print(json.dumps(run(a.requests, a.prompt, a.layers, a.steps, a.q_heads, a.kv_heads, a.dim, a.dtype)))
+    print(json.dumps(run(a.requests, a.prompt, a.layers, a.steps, a.q_heads, a.kv_heads, a.dim, a.dtype, cache_bits=a.bits, images=a.images)))
 
 
 if __name__ == "__main__":
