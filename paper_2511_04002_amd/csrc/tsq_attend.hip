@@ -776,7 +776,7 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
         l.tiles = (uint32_t)(l.tiles_each ? (uint64_t)l.tiles_each * requests : packed);
     };
     uint64_t slots;
-    if (most <= few || s.bits == 4) {
+    if (most <= few) {
         tile(most <= 16 || s.head_dim == 256 ? 16 : 32);
         slots = s.head_dim == 256 ? 256 : s.head_dim == 128 || l.rows == 32 ? 512 : 768;
     } else {
@@ -869,7 +869,8 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
         f.parts = j.few_parts;
         f.part_rows = l.few_part_rows;
         f.slots_each = l.slots_each;
-        by_shape(s, [&](auto d, auto bf16) { k_attend_few<d(), bf16(), d() == 256 ? 1 : 2><<<(uint32_t)few, 256, 0, st>>>(f); });
+        if (s.bits == 4) launch_attend_four(s, s.head_dim == 256 ? 16 : 32, (uint32_t)few, f, stream);
+        else by_shape(s, [&](auto d, auto bf16) { k_attend_few<d(), bf16(), d() == 256 ? 1 : 2><<<(uint32_t)few, 256, 0, st>>>(f); });
         if (hipError_t e = hipGetLastError()) return (int)e;
     }
     if (joined == 0) return 0;

@@ -18,6 +18,8 @@
 namespace tsq {
 namespace {
 
+constexpr float kCoarse = 0x1p22f;   // beyond this a reference's last bit is worth 1/2 or more: the difference of a score that
+                                     // is not rounded and one that is would pass a half's range
 template <bool BF16> struct Softmaxes {
     static constexpr float room = BF16 ? -8.0f : 7.0f;   // the reference is set this far below the largest exponent ...
     static constexpr float slack = 8.0f;                 // ... and kept until one exceeds that by as much
@@ -295,13 +297,291 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(Atten
     }
 }
 
+// Many rows: 32 of a kv head's a wave, eight waves a workgroup (four, where a request has no more than 128 rows, and for
+// heads of 256, whose sums and queries take the registers of two).  A tile of 128 tokens (64) goes through registers into
+// LDS, converted, once for all rows; one barrier a tile is all that the waves wait for.  Keys and values lie there token by
+// token; the values' operand, which wants tokens side by side, is read by the transposing loads: of 16 lanes, which
+// point at four tokens' pieces of 16 elements, each gets one element of the four tokens.
+// Lane (n = lane % 32, hi = lane / 32).  S^T in two 32 x 32 pieces: register i of a piece is token
+// 8 (i / 4) + 4 hi + i % 4, row n.  P^T as an operand of 16 tokens: registers 8u .. 8u + 7, tokens 4 hi + (0..3) and
+// 8 + 4 hi + (0..3) of the 16.
+//
+// Weights are halves.  Values of bfloat16 are converted to halves, too, as long as halves hold them exactly (all scales
+// of 2^-23 to 2^13); a workgroup that meets others begins again with bfloat16 values and weights in two parts (SPLIT).
+template <int D, int TOKENS>
+struct FourTile {
+    uint16_t k[TOKENS][D + 8];                           // (neighbours begin four banks apart ...
+    uint16_t v[TOKENS][D + 16];                          // ... and eight)
+};
+
+// How a block's LOADS loads from LDS and PRODUCTS products are to be issued: a few loads, then the others behind the products.
+template <int LOADS, int PRODUCTS, int GROUP> __device__ __forceinline__ void loads_among_products() {
+    constexpr int kLoad = 0x100, kProduct = 0x8, EACH = LOADS / PRODUCTS;
+    __builtin_amdgcn_sched_group_barrier(kLoad, 4 * EACH, GROUP);
+#pragma unroll
+    for (int i = 0; i < PRODUCTS - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kProduct, 1, GROUP);
+        __builtin_amdgcn_sched_group_barrier(kLoad, EACH, GROUP);
+    }
+    __builtin_amdgcn_sched_group_barrier(kProduct, 4, GROUP);
+}
+
+// Products of 32 x 32 x 16.
+template <bool BF16> __device__ __forceinline__ float16_t wide_product(uint4_t x, uint4_t y, float16_t z) {
+    if constexpr (BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, y), z, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, x), __builtin_bit_cast(half8_t, y), z, 0, 0, 0);
+}
+
+// Four tokens' elements of LDS, one element of each (see above).
+__device__ __forceinline__ uint2_t transposed(const uint16_t *at) {
+    typedef short short4_t __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(uint2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t *)at));
+}
+
+template <int D, bool BF16, int WAVES, int TOKENS, bool SPLIT>
+__device__ __forceinline__ bool attend_four_tile(const AttendArgs &a, const Place &p, uint32_t tile, const Reach &reach,
+                                                 FourTile<D, TOKENS> *buffer, uint32_t *outside) {
+    constexpr int ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+    constexpr int E = D == 64 ? 16 : 32, PT = D / E, GROUPS = D / 32;        // elements of a piece, pieces of a token
+    constexpr int N = TOKENS * PT / THREADS;             // pieces of keys, and of values, that a thread stages
+    constexpr bool VALUES_BF16 = BF16 && SPLIT;
+    typedef FourTile<D, TOKENS> Tile;
+    typedef typename std::conditional<E == 16, uint2_t, uint4_t>::type Piece;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6)), n = lane & 31, hi = lane >> 5;
+    const uint32_t B = 1u << a.block_log2;
+    const uint32_t row = tile * ROWS + wave * 32 + n, rows = p.n * a.group;
+    uint4_t q[D / 16];
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+        q[s] = uint4_t{0, 0, 0, 0};
+        if (row < rows) {
+            const uint16_t *src = static_cast<const uint16_t *>(a.q) + (uint64_t)(p.begin + row / a.group) * a.q_stride +
+                                  (uint64_t)(p.h * a.group + row % a.group) * D + 16 * s + 8 * hi;
+            q[s] = *reinterpret_cast<const uint4_t *>(src);
+        }
+    }
+    uint32_t from, to;
+    row_sees(a, p, row, from, to);
+
+    float16_t acc[D / 32];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+        for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
+    float ref = kNone, weight = 0.0f;
+    bool coarse = false;             // some row's reference, a finite one, is too large for an exponent to be made in one rounding
+    constexpr float room = Softmaxes<VALUES_BF16>::room, slack = Softmaxes<VALUES_BF16>::slack;
+
+    // staging: what this thread brings of a tile, asked for a tile ahead, its table entries two
+    uint32_t asked[N], entry[N];
+    Piece kw[N], vw[N];
+    uint32_t ks[N], vs[N];
+    uint32_t code_at[N], scale_at[N];                    // of the thread's pieces in a block, for tiles that begin with one
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t e = i * THREADS + tid, place = e / PT & (B - 1), piece = e % PT;
+        code_at[i] = place * (D / 2) + piece * (E / 2);
+        scale_at[i] = piece * E / 32 * B + place;
+    }
+    const uint8_t *all_k = static_cast<const uint8_t *>(a.k) + (uint64_t)p.h * B * (D / 2), *all_v = static_cast<const uint8_t *>(a.v) + (uint64_t)p.h * B * (D / 2);
+    const uint8_t *all_ks = static_cast<const uint8_t *>(a.k_scale) + (uint64_t)p.h * B * GROUPS, *all_vs = static_cast<const uint8_t *>(a.v_scale) + (uint64_t)p.h * B * GROUPS;
+    auto ask_entries = [&](uint32_t t0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) entry[i] = table_entry(a, p, t0 + (i * THREADS + tid) / PT, reach.end);
+    };
+    auto ask = [&](uint32_t t0) {
+        const uint32_t within = t0 & (B - 1);            // (of blocks longer than a tile)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint64_t head = (uint64_t)id_of(a, entry[i]) * a.kv_heads * B;
+            const uint64_t codes = head * (D / 2) + within * (D / 2) + code_at[i], scale = head * GROUPS + within + scale_at[i];
+            kw[i] = *reinterpret_cast<const Piece *>(all_k + codes);
+            vw[i] = *reinterpret_cast<const Piece *>(all_v + codes);
+            ks[i] = all_ks[scale];
+            vs[i] = all_vs[scale];
+            asked[i] = entry[i];
+        }
+    };
+    auto put = [&](Tile &t) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t e = i * THREADS + tid, token = e / PT, at = e % PT * E;
+            const float k_scale = four_scale(is_bad(a, p, asked[i]) ? kNotANumber : ks[i]);
+            // (no value may bring NaN or infinity into a sum with a weight of 0: see k_attend_four_few)
+            typedef FourScales<VALUES_BF16> Held;
+            if constexpr (BF16 && !SPLIT)
+                if (vs[i] < Held::lowest || vs[i] > Held::highest) *outside = 1;
+            const float v_scale = four_scale(min(vs[i], (uint32_t)Held::highest));
+            for (int j = 0; j < E / 8; ++j) {
+                *reinterpret_cast<uint4_t *>(&t.k[token][at + 8 * j]) = four_eight<BF16>(kw[i][j], k_scale);
+                *reinterpret_cast<uint4_t *>(&t.v[token][at + 8 * j]) = four_eight<VALUES_BF16>(vw[i][j], v_scale);
+            }
+        }
+    };
+    if (reach.begin < reach.end) {
+        ask_entries(reach.begin);
+        ask(reach.begin);
+        ask_entries(reach.begin + TOKENS);
+        put(buffer[0]);
+        ask(reach.begin + TOKENS);
+        ask_entries(reach.begin + 2 * TOKENS);
+    }
+    __syncthreads();
+    uint32_t at = 0;
+    for (uint32_t t0 = reach.begin; t0 < reach.end; t0 += TOKENS, at ^= 1) {
+        const Tile &t = buffer[at];
+#pragma unroll
+        for (uint32_t part = 0; part < TOKENS; part += 64) {
+            const uint32_t u0 = t0 + part;
+            // (a wave whose rows all end before these tokens, or begin behind them, only helps to stage)
+            if (!__ballot(from < u0 + 64 && to > u0)) continue;
+            float16_t s[2];
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                for (int i = 0; i < 16; ++i) s[c][i] = 0.0f;
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e)
+                    s[c] = wide_product<BF16>(*reinterpret_cast<const uint4_t *>(&t.k[part + 32 * c + n][16 * e + 8 * hi]), q[e], s[c]);
+            }
+            loads_among_products<2 * D / 16, 2 * D / 16, 0>();
+            __builtin_amdgcn_s_setprio(0);
+            const bool whole = __ballot(u0 < from || u0 + 64 > to) == 0;
+            if (!whole) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t token = u0 + 32 * c + 8 * (i / 4) + 4 * hi + i % 4;
+                        if (token < from || token >= to) s[c][i] = -INFINITY;
+                    }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[c][i]);
+            top = max_across_halves(top) * a.scale_log2;
+            float factor = a.scale_log2;
+            if (coarse || __ballot(top > ref + (room + slack))) {
+                const float now = fmaxf(ref, top - room), down = pow2(ref - now);
+                ref = now;
+                weight *= down;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) acc[d] *= down;
+                coarse = __ballot(fabsf(ref) > kCoarse && fabsf(ref) < -kNone) != 0;
+                if (coarse) {                            // the reference is rounded: so is what it is taken from
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        for (int i = 0; i < 16; ++i) s[c][i] *= factor;
+                    factor = 1.0f;
+                }
+            }
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            uint4_t pw[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                for (int i = 0; i < 8; i += 2) {
+                    const float e0 = pow2(__builtin_fmaf(s[u / 2][8 * (u & 1) + i], factor, -ref));
+                    const float e1 = pow2(__builtin_fmaf(s[u / 2][8 * (u & 1) + i + 1], factor, -ref));
+                    s[u / 2][8 * (u & 1) + i] = e0;
+                    s[u / 2][8 * (u & 1) + i + 1] = e1;
+                    sum[u] += e0 + e1;
+                    pw[u][i / 2] = narrow2<VALUES_BF16>(e0, e1);
+                }
+            weight += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            for (int pass = 0; pass < (SPLIT ? 2 : 1); ++pass) {
+                if (pass)                                // what the first parts of the weights left
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        for (int i = 0; i < 8; i += 2)
+                            pw[u][i / 2] = narrow2<true>(s[u / 2][8 * (u & 1) + i] - widen<true>(pw[u][i / 2] & 0xFFFFu),
+                                                         s[u / 2][8 * (u & 1) + i + 1] - widen<true>(pw[u][i / 2] >> 16));
+                __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const uint16_t *from_lds = &t.v[part + 16 * u + 4 * hi + (lane & 15) / 4][32 * d + 16 * (n / 16) + 4 * (lane & 3)];
+                        const uint2_t x = transposed(from_lds), y = transposed(from_lds + 8 * (D + 16));
+                        acc[d] = wide_product<VALUES_BF16>(uint4_t{x[0], x[1], y[0], y[1]}, pw[u], acc[d]);
+                    }
+                loads_among_products<8 * D / 32, 4 * D / 32, 1>();
+                __builtin_amdgcn_s_setprio(0);
+            }
+        }
+        if (t0 + TOKENS < reach.end) put(buffer[at ^ 1]);
+        ask(t0 + 2 * TOKENS);
+        ask_entries(t0 + 3 * TOKENS);
+        __syncthreads();
+    }
+    if constexpr (BF16 && !SPLIT)
+        if (*outside) return true;
+    weight += __shfl_xor(weight, 32);
+    if (is_lost(a, p, row)) weight = __builtin_nanf("");
+    if (row < rows) {
+        const uint64_t id = row_id(a, p, row);
+        if (a.splits == 1) {
+            const float back = weight == 0.0f ? 0.0f : 1.0f / weight;
+            uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)(p.begin + row / a.group) * a.out_stride +
+                            (uint64_t)(p.h * a.group + row % a.group) * D + 4 * hi;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+                for (int b = 0; b < 4; ++b)
+                    *reinterpret_cast<uint2_t *>(dst + 32 * d + 8 * b) = uint2_t{narrow2<BF16>(acc[d][4 * b] * back, acc[d][4 * b + 1] * back),
+                                                                                 narrow2<BF16>(acc[d][4 * b + 2] * back, acc[d][4 * b + 3] * back)};
+            if (a.lse && hi == 0) a.lse[id] = weight == 0.0f ? -INFINITY : (ref + log2_of(weight)) * 0.69314718055994530942f;
+        } else {
+            float *dst = a.parts + (id * a.splits + p.split) * D + 4 * hi;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+                for (int b = 0; b < 4; ++b)
+                    *reinterpret_cast<float4_t *>(dst + 32 * d + 8 * b) = float4_t{acc[d][4 * b], acc[d][4 * b + 1], acc[d][4 * b + 2], acc[d][4 * b + 3]};
+            if (hi == 0) {
+                float *st = a.parts + a.part_rows * a.splits * D + (id * a.splits + p.split) * 2;
+                st[0] = ref;
+                st[1] = weight;
+            }
+        }
+    }
+    return false;
+}
+
+template <int D, bool BF16, int WAVES, int TOKENS>
+__global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_four_many(AttendArgs a) {
+    constexpr int ROWS = 32 * WAVES;
+    __shared__ FourTile<D, TOKENS> buffer[2];
+    __shared__ uint32_t outside;     // (some value is one that halves do not hold)
+    Place p;
+    if (!find_place<ROWS>(a, p)) return;
+    for (uint32_t tile = p.tile;; ++tile) {
+        const uint32_t rows = p.n * a.group;
+        const Reach reach = reach_of<ROWS>(a, p, tile);
+        const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
+        if (a.splits > 1 && reach.begin >= reach.end) {
+            nothing_seen<ROWS>(a, p, tile, D);
+            if (done) return;
+            continue;
+        }
+        if constexpr (BF16) {
+            if (threadIdx.x == 0) outside = 0;
+            __syncthreads();
+        }
+        if (attend_four_tile<D, BF16, WAVES, TOKENS, false>(a, p, tile, reach, buffer, &outside)) {
+            __syncthreads();
+            if constexpr (BF16) attend_four_tile<D, BF16, WAVES, TOKENS, true>(a, p, tile, reach, buffer, &outside);
+        }
+        if (done) return;
+        __syncthreads();
+    }
+}
+
 }  // namespace
 
 void launch_attend_four(const CacheShape &s, uint32_t rows, uint32_t grid, const AttendArgs &a, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     by_shape(s, [&](auto d, auto bf16) {
         if (rows == 16) k_attend_four_few<d(), bf16(), 1><<<grid, 256, 0, st>>>(a);
-        else if constexpr (d() != 256) k_attend_four_few<d(), bf16(), 2><<<grid, 256, 0, st>>>(a);
+        else if (rows == 32) { if constexpr (d() != 256) k_attend_four_few<d(), bf16(), 2><<<grid, 256, 0, st>>>(a); }
+        else if (rows == 128) k_attend_four_many<d(), bf16(), 4, 64><<<grid, 256, 0, st>>>(a);
+        else if constexpr (d() != 256) k_attend_four_many<d(), bf16(), 8, 128><<<grid, 512, 0, st>>>(a);
     });
 }
 

@@ -234,11 +234,12 @@ def attend_both(b, q_heads, counts, lengths, causal=True, window=0, table=None, 
     size = np.nan_to_num(np.abs(O.four_values(b.k[blocks], b.ks[blocks]))).max(initial=0.0, axis=(0, 1, 2))
     most = float((np.nan_to_num(np.abs(host(q)[:total]).astype(np.float64), posinf=0.0) @ size).max(initial=0.0)) * scale
     off = 2.0 ** -11 + 2 * most * 2.0 ** -24 * (6 if exact_scores else dim + 6)
-    # (weights below 2^-14 are rounded to 2^-25 where the largest is at least 2^7; those of bfloat16 values, whose largest is at
-    # least 2^-16 - 8 below the reference, and 8 more until that moves - are lost below 2^-126, binary32's and bfloat16's least
-    # normal number: 2^-110 of the largest)
-    largest = 6 * 2.0 ** (float(b.vs[b.vs != 255].max(initial=0)) - 127)
-    least = (2.0 ** -32 if dtype == "f16" else 2.0 ** -110) * lengths.max() * largest
+    # (weights that are halves, of values that halves hold, are rounded to 2^-25 below 2^-14 where the largest is at least 2^7;
+    # those of other values, whose largest is at least 2^-16 - 8 below the reference, and 8 more until that moves - are lost below
+    # 2^-126, binary32's and bfloat16's least normal number: 2^-110 of the largest)
+    held = b.vs[b.vs != 255]
+    largest = 6 * 2.0 ** (float(held.max(initial=0)) - 127)
+    least = (2.0 ** -32 if dtype == "f16" or (held.min(initial=255) >= 104 and held.max(initial=0) <= 140) else 2.0 ** -110) * lengths.max() * largest
     # (sums of binary32: their order, and the parts that are joined)
     fine = ~np.isnan(want)
     bound = HALF_ULP[dtype] * np.abs(want) + (off + 2.0 ** -24 * (lengths.max() + 64)) * spread + TINY[dtype] + least
