@@ -189,9 +189,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(Atten
                     for (int i = 0; i < 4; i += 2) {
                         const float e0 = pow2(s[c][t][i] - ref[c]), e1 = pow2(s[c][t][i + 1] - ref[c]);
                         sum += e0 + e1;
-                        const uint32_t w = narrow2<BF16>(e0, e1);
+                        const uint32_t w = pack_two<BF16>(e0, e1);
                         pw[c][t / 2][2 * (t & 1) + i / 2] = w;
-                        if constexpr (BF16) rest[c][t / 2][2 * (t & 1) + i / 2] = narrow2<true>(e0 - widen<true>(w & 0xFFFFu), e1 - widen<true>(w >> 16));
+                        if constexpr (BF16) rest[c][t / 2][2 * (t & 1) + i / 2] = pack_two<true>(e0 - widen<true>(w & 0xFFFFu), e1 - widen<true>(w >> 16));
                     }
                 weight[c] += sum;
             }
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(Atten
                     }
                     if (a.splits == 1) {
                         uint4_t w;
-                        for (int i = 0; i < 4; ++i) w[i] = narrow2<BF16>(y[2 * i], y[2 * i + 1]);
+                        for (int i = 0; i < 4; ++i) w[i] = pack_two<BF16>(y[2 * i], y[2 * i + 1]);
                         uint16_t *dst = static_cast<uint16_t *>(a.out) + (uint64_t)(p.begin + o / a.group) * a.out_stride +
                                         (uint64_t)(p.h * a.group + o % a.group) * D + part * 128 + piece * 8;
                         *reinterpret_cast<uint4_t *>(dst) = w;
@@ -339,12 +339,13 @@ __device__ __forceinline__ uint2_t transposed(const uint16_t *at) {
 }
 
 template <int D, bool BF16, int WAVES, int TOKENS, bool SPLIT>
-__device__ __forceinline__ bool attend_four_tile(const AttendArgs &a, const Place &p, uint32_t tile, const Reach &reach,
+__device__ __forceinline__ void attend_four_tile(const AttendArgs &a, const Place &p, uint32_t tile, const Reach &reach,
                                                  FourTile<D, TOKENS> *buffer, uint32_t *outside) {
     constexpr int ROWS = 32 * WAVES, THREADS = 64 * WAVES;
     constexpr int E = D == 64 ? 16 : 32, PT = D / E, GROUPS = D / 32;        // elements of a piece, pieces of a token
     constexpr int N = TOKENS * PT / THREADS;             // pieces of keys, and of values, that a thread stages
     constexpr bool VALUES_BF16 = BF16 && SPLIT;
+    constexpr int SUB = SPLIT || TOKENS == 32 ? 32 : 64, C = SUB / 32;   // tokens whose scores a wave has at once
     typedef FourTile<D, TOKENS> Tile;
     typedef typename std::conditional<E == 16, uint2_t, uint4_t>::type Piece;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6)), n = lane & 31, hi = lane >> 5;
@@ -424,96 +425,92 @@ __device__ __forceinline__ bool attend_four_tile(const AttendArgs &a, const Plac
         put(buffer[0]);
         ask(reach.begin + TOKENS);
         ask_entries(reach.begin + 2 * TOKENS);
-    }
-    __syncthreads();
-    uint32_t at = 0;
-    for (uint32_t t0 = reach.begin; t0 < reach.end; t0 += TOKENS, at ^= 1) {
-        const Tile &t = buffer[at];
+        __syncthreads();
+        uint32_t at = 0, t0 = reach.begin;
+        do {                         // (not a loop that may be left out: its loads would be waited for along with the queries')
+            const Tile &t = buffer[at];
+#pragma unroll SPLIT ? 1 : TOKENS / SUB
+            for (uint32_t part = 0; part < TOKENS; part += SUB) {
+                const uint32_t u0 = t0 + part;
+                // (a wave whose rows all end before these tokens, or begin behind them, only helps to stage)
+                if (!__ballot(from < u0 + SUB && to > u0)) continue;
+                float16_t s[C];
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (uint32_t part = 0; part < TOKENS; part += 64) {
-            const uint32_t u0 = t0 + part;
-            // (a wave whose rows all end before these tokens, or begin behind them, only helps to stage)
-            if (!__ballot(from < u0 + 64 && to > u0)) continue;
-            float16_t s[2];
-            __builtin_amdgcn_s_setprio(1);
+                for (int c = 0; c < C; ++c) {
+                    for (int i = 0; i < 16; ++i) s[c][i] = 0.0f;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                for (int i = 0; i < 16; ++i) s[c][i] = 0.0f;
+                    for (int e = 0; e < D / 16; ++e)
+                        s[c] = wide_product<BF16>(*reinterpret_cast<const uint4_t *>(&t.k[part + 32 * c + n][16 * e + 8 * hi]), q[e], s[c]);
+                }
+                loads_among_products<C * D / 16, C * D / 16, 0>();
+                __builtin_amdgcn_s_setprio(0);
+                const bool whole = __ballot(u0 < from || u0 + SUB > to) == 0;
+                if (!whole) {
 #pragma unroll
-                for (int e = 0; e < D / 16; ++e)
-                    s[c] = wide_product<BF16>(*reinterpret_cast<const uint4_t *>(&t.k[part + 32 * c + n][16 * e + 8 * hi]), q[e], s[c]);
-            }
-            loads_among_products<2 * D / 16, 2 * D / 16, 0>();
-            __builtin_amdgcn_s_setprio(0);
-            const bool whole = __ballot(u0 < from || u0 + 64 > to) == 0;
-            if (!whole) {
+                    for (int c = 0; c < C; ++c)
+                        for (int i = 0; i < 16; ++i) {
+                            const uint32_t token = u0 + 32 * c + 8 * (i / 4) + 4 * hi + i % 4;
+                            if (token < from || token >= to) s[c][i] = -INFINITY;
+                        }
+                }
+                float top = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    for (int i = 0; i < 16; ++i) {
-                        const uint32_t token = u0 + 32 * c + 8 * (i / 4) + 4 * hi + i % 4;
-                        if (token < from || token >= to) s[c][i] = -INFINITY;
+                for (int c = 0; c < C; ++c)
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[c][i]);
+                top = max_across_halves(top) * a.scale_log2;
+                float factor = a.scale_log2;
+                if (coarse || __ballot(top > ref + (room + slack))) {
+                    const float now = fmaxf(ref, top - room), down = pow2(ref - now);
+                    ref = now;
+                    weight *= down;
+#pragma unroll
+                    for (int d = 0; d < D / 32; ++d) acc[d] *= down;
+                    coarse = __ballot(fabsf(ref) > kCoarse && fabsf(ref) < -kNone) != 0;
+                    if (coarse) {                            // the reference is rounded: so is what it is taken from
+#pragma unroll
+                        for (int c = 0; c < C; ++c)
+                            for (int i = 0; i < 16; ++i) s[c][i] *= factor;
+                        factor = 1.0f;
                     }
-            }
-            float top = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[c][i]);
-            top = max_across_halves(top) * a.scale_log2;
-            float factor = a.scale_log2;
-            if (coarse || __ballot(top > ref + (room + slack))) {
-                const float now = fmaxf(ref, top - room), down = pow2(ref - now);
-                ref = now;
-                weight *= down;
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d) acc[d] *= down;
-                coarse = __ballot(fabsf(ref) > kCoarse && fabsf(ref) < -kNone) != 0;
-                if (coarse) {                            // the reference is rounded: so is what it is taken from
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-                        for (int i = 0; i < 16; ++i) s[c][i] *= factor;
-                    factor = 1.0f;
                 }
-            }
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            uint4_t pw[4];
+                float sum[2 * C];
+                uint4_t pw[2 * C], rest[2 * C];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                for (int i = 0; i < 8; i += 2) {
-                    const float e0 = pow2(__builtin_fmaf(s[u / 2][8 * (u & 1) + i], factor, -ref));
-                    const float e1 = pow2(__builtin_fmaf(s[u / 2][8 * (u & 1) + i + 1], factor, -ref));
-                    s[u / 2][8 * (u & 1) + i] = e0;
-                    s[u / 2][8 * (u & 1) + i + 1] = e1;
-                    sum[u] += e0 + e1;
-                    pw[u][i / 2] = narrow2<VALUES_BF16>(e0, e1);
+                for (int u = 0; u < 2 * C; ++u) {
+                    sum[u] = 0.0f;
+                    for (int i = 0; i < 8; i += 2) {
+                        const float e0 = pow2(__builtin_fmaf(s[u / 2][8 * (u & 1) + i], factor, -ref)), e1 = pow2(__builtin_fmaf(s[u / 2][8 * (u & 1) + i + 1], factor, -ref));
+                        sum[u] += e0 + e1;
+                        const uint32_t w = pack_two<VALUES_BF16>(e0, e1);
+                        pw[u][i / 2] = w;
+                        if constexpr (SPLIT) rest[u][i / 2] = pack_two<true>(e0 - widen<true>(w & 0xFFFFu), e1 - widen<true>(w >> 16));
+                    }
                 }
-            weight += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            for (int pass = 0; pass < (SPLIT ? 2 : 1); ++pass) {
-                if (pass)                                // what the first parts of the weights left
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        for (int i = 0; i < 8; i += 2)
-                            pw[u][i / 2] = narrow2<true>(s[u / 2][8 * (u & 1) + i] - widen<true>(pw[u][i / 2] & 0xFFFFu),
-                                                         s[u / 2][8 * (u & 1) + i + 1] - widen<true>(pw[u][i / 2] >> 16));
+                for (int u = 1; u < 2 * C; ++u) sum[0] += sum[u];
+                weight += sum[0];
                 __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
+                    for (int u = 0; u < 2 * C; ++u) {
                         const uint16_t *from_lds = &t.v[part + 16 * u + 4 * hi + (lane & 15) / 4][32 * d + 16 * (n / 16) + 4 * (lane & 3)];
                         const uint2_t x = transposed(from_lds), y = transposed(from_lds + 8 * (D + 16));
-                        acc[d] = wide_product<VALUES_BF16>(uint4_t{x[0], x[1], y[0], y[1]}, pw[u], acc[d]);
+                        const uint4_t v = {x[0], x[1], y[0], y[1]};
+                        acc[d] = wide_product<VALUES_BF16>(v, pw[u], acc[d]);
+                        if constexpr (SPLIT) acc[d] = wide_product<true>(v, rest[u], acc[d]);
                     }
-                loads_among_products<8 * D / 32, 4 * D / 32, 1>();
+                if constexpr (!SPLIT) loads_among_products<4 * C * D / 32, 2 * C * D / 32, 1>();
                 __builtin_amdgcn_s_setprio(0);
             }
-        }
-        if (t0 + TOKENS < reach.end) put(buffer[at ^ 1]);
-        ask(t0 + 2 * TOKENS);
-        ask_entries(t0 + 3 * TOKENS);
-        __syncthreads();
+            if (t0 + TOKENS < reach.end) put(buffer[at ^ 1]);
+            ask(t0 + 2 * TOKENS);
+            ask_entries(t0 + 3 * TOKENS);
+            __syncthreads();
+            t0 += TOKENS;
+            at ^= 1;
+        } while (t0 < reach.end);
     }
-    if constexpr (BF16 && !SPLIT)
-        if (*outside) return true;
     weight += __shfl_xor(weight, 32);
     if (is_lost(a, p, row)) weight = __builtin_nanf("");
     if (row < rows) {
@@ -525,8 +522,8 @@ __device__ __forceinline__ bool attend_four_tile(const AttendArgs &a, const Plac
 #pragma unroll
             for (int d = 0; d < D / 32; ++d)
                 for (int b = 0; b < 4; ++b)
-                    *reinterpret_cast<uint2_t *>(dst + 32 * d + 8 * b) = uint2_t{narrow2<BF16>(acc[d][4 * b] * back, acc[d][4 * b + 1] * back),
-                                                                                 narrow2<BF16>(acc[d][4 * b + 2] * back, acc[d][4 * b + 3] * back)};
+                    *reinterpret_cast<uint2_t *>(dst + 32 * d + 8 * b) = uint2_t{pack_two<BF16>(acc[d][4 * b] * back, acc[d][4 * b + 1] * back),
+                                                                                 pack_two<BF16>(acc[d][4 * b + 2] * back, acc[d][4 * b + 3] * back)};
             if (a.lse && hi == 0) a.lse[id] = weight == 0.0f ? -INFINITY : (ref + log2_of(weight)) * 0.69314718055994530942f;
         } else {
             float *dst = a.parts + (id * a.splits + p.split) * D + 4 * hi;
@@ -541,35 +538,51 @@ __device__ __forceinline__ bool attend_four_tile(const AttendArgs &a, const Plac
             }
         }
     }
-    return false;
 }
 
-template <int D, bool BF16, int WAVES, int TOKENS>
-__global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_four_many(AttendArgs a) {
+// A workgroup's tiles: one, or what is left of a request with more rows than were announced.
+template <int D, bool BF16, int WAVES, int TOKENS, bool SPLIT>
+__device__ __forceinline__ void attend_four_tiles(const AttendArgs &a, FourTile<D, TOKENS> *buffer, uint32_t *outside) {
     constexpr int ROWS = 32 * WAVES;
-    __shared__ FourTile<D, TOKENS> buffer[2];
-    __shared__ uint32_t outside;     // (some value is one that halves do not hold)
     Place p;
     if (!find_place<ROWS>(a, p)) return;
     for (uint32_t tile = p.tile;; ++tile) {
         const uint32_t rows = p.n * a.group;
         const Reach reach = reach_of<ROWS>(a, p, tile);
         const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
-        if (a.splits > 1 && reach.begin >= reach.end) {
-            nothing_seen<ROWS>(a, p, tile, D);
-            if (done) return;
-            continue;
-        }
-        if constexpr (BF16) {
-            if (threadIdx.x == 0) outside = 0;
-            __syncthreads();
-        }
-        if (attend_four_tile<D, BF16, WAVES, TOKENS, false>(a, p, tile, reach, buffer, &outside)) {
-            __syncthreads();
-            if constexpr (BF16) attend_four_tile<D, BF16, WAVES, TOKENS, true>(a, p, tile, reach, buffer, &outside);
-        }
+        if (a.splits > 1 && reach.begin >= reach.end) nothing_seen<ROWS>(a, p, tile, D);
+        else attend_four_tile<D, BF16, WAVES, TOKENS, SPLIT>(a, p, tile, reach, buffer, outside);
         if (done) return;
         __syncthreads();
+    }
+}
+
+// All of them once more.  Not inlined, and the last thing that a workgroup does: what this pass keeps in registers would be
+// taken from the first one's loop, which then loads its operands one by one.
+template <int D, int WAVES, int TOKENS>
+__device__ __attribute__((noinline)) void attend_four_again(const __attribute__((address_space(4))) void *args,
+                                                            __attribute__((address_space(3))) FourTile<D, TOKENS> *buffer) {
+    struct Words { uint32_t w[sizeof(AttendArgs) / 4]; } words;
+    const uint64_t bits = (uint64_t)args;
+    const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)bits);
+    for (uint32_t i = 0; i < sizeof(AttendArgs) / 4; ++i) words.w[i] = ((const __attribute__((address_space(4))) uint32_t *)from)[i];
+    attend_four_tiles<D, true, WAVES, TOKENS, true>(__builtin_bit_cast(AttendArgs, words), (FourTile<D, TOKENS> *)buffer, nullptr);
+}
+
+template <int D, bool BF16, int WAVES, int TOKENS>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_four_many(AttendArgs a) {
+    __shared__ FourTile<D, TOKENS> buffer[2];
+    __shared__ uint32_t outside;     // (some value is one that halves do not hold)
+    if constexpr (BF16) {
+        if (threadIdx.x == 0) outside = 0;
+        __syncthreads();
+    }
+    attend_four_tiles<D, BF16, WAVES, TOKENS, false>(a, buffer, &outside);
+    if constexpr (BF16) {
+        __syncthreads();
+        if (__builtin_amdgcn_readfirstlane((int)outside))
+            attend_four_again<D, WAVES, TOKENS>((const __attribute__((address_space(4))) void *)__builtin_amdgcn_kernarg_segment_ptr(),
+                                                (__attribute__((address_space(3))) FourTile<D, TOKENS> *)buffer);
     }
 }
 
@@ -580,7 +593,7 @@ void launch_attend_four(const CacheShape &s, uint32_t rows, uint32_t grid, const
     by_shape(s, [&](auto d, auto bf16) {
         if (rows == 16) k_attend_four_few<d(), bf16(), 1><<<grid, 256, 0, st>>>(a);
         else if (rows == 32) { if constexpr (d() != 256) k_attend_four_few<d(), bf16(), 2><<<grid, 256, 0, st>>>(a); }
-        else if (rows == 128) k_attend_four_many<d(), bf16(), 4, 64><<<grid, 256, 0, st>>>(a);
+        else if (rows == 128) k_attend_four_many<d(), bf16(), 4, d() == 256 ? 32 : 64><<<grid, 256, 0, st>>>(a);
         else if constexpr (d() != 256) k_attend_four_many<d(), bf16(), 8, 128><<<grid, 512, 0, st>>>(a);
     });
 }

@@ -34,5 +34,11 @@ template <bool BF16> __device__ __forceinline__ uint4_t four_eight(uint32_t w, f
     return uint4_t{four_pair<BF16, 0>(w, scale), four_pair<BF16, 1>(w, scale), four_pair<BF16, 2>(w, scale), four_pair<BF16, 3>(w, scale)};
 }
 
+// Two binary32 numbers rounded to a 16-bit type each, in one instruction.
+template <bool BF16> __device__ __forceinline__ uint32_t pack_two(float a, float b) {
+    if constexpr (BF16) return __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)a, (__bf16)b});
+    else return __builtin_bit_cast(uint32_t, half2_t{(_Float16)a, (_Float16)b});
+}
+
 }  // namespace
 }  // namespace tsq
