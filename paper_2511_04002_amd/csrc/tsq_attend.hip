@@ -847,7 +847,7 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
     if (!fits(all, l.rows == 256 ? 512 : 256) || !fits(few, 256) || !(one_wave ? fits((joined + 3) / 4, 256) : fits(joined, 512))) return kTooLarge;
     const uint32_t grid = (uint32_t)all;
     const JoinArgs j = {a, reinterpret_cast<float *>(reinterpret_cast<char *>(a.parts) + l.few_at), l.few_part_rows, l.few_splits, l.slots_each};
-    if (s.bits == 4) launch_attend_four(s, l.rows, grid, a, stream);
+    if (s.bits == 4) launch_attend_four(s, l.rows, l.tiles_each == 1, grid, a, stream);
     else by_shape(s, [&](auto d, auto bf16) {
         if (l.rows == 16) k_attend_few<d(), bf16(), 1><<<grid, 256, 0, st>>>(a);
         else if (l.rows == 32) { if constexpr (d() != 256) k_attend_few<d(), bf16(), 2><<<grid, 256, 0, st>>>(a); }
@@ -869,7 +869,7 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
         f.parts = j.few_parts;
         f.part_rows = l.few_part_rows;
         f.slots_each = l.slots_each;
-        if (s.bits == 4) launch_attend_four(s, s.head_dim == 256 ? 16 : 32, (uint32_t)few, f, stream);
+        if (s.bits == 4) launch_attend_four(s, s.head_dim == 256 ? 16 : 32, true, (uint32_t)few, f, stream);
         else by_shape(s, [&](auto d, auto bf16) { k_attend_few<d(), bf16(), d() == 256 ? 1 : 2><<<(uint32_t)few, 256, 0, st>>>(f); });
         if (hipError_t e = hipGetLastError()) return (int)e;
     }

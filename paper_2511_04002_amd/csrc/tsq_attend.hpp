@@ -51,12 +51,10 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
         if (a.by_length) {
             // the longest request first: p.r counts from the shortest here; each lane ranks one request
             const uint32_t lane = threadIdx.x & 63;
-            const int32_t mine = lane < a.requests ? a.lengths[lane] : 0;
+            // (its length and number in one word: they all differ, and lengths past 2^26 may change places)
+            const uint32_t mine = min((uint32_t)max(lane < a.requests ? a.lengths[lane] : 0, 0), (1u << 26) - 1) << 6 | lane;
             uint32_t below = 0;
-            for (uint32_t j = 0; j < a.requests; ++j) {
-                const int32_t other = __builtin_amdgcn_readlane(mine, (int)j);
-                below += other < mine || (other == mine && j < lane) ? 1 : 0;
-            }
+            for (uint32_t j = 0; j < a.requests; ++j) below += (uint32_t)__builtin_amdgcn_readlane((int)mine, (int)j) < mine ? 1 : 0;
             p.r = (uint32_t)__builtin_ctzll(__ballot(lane < a.requests && below == p.r));
         }
     } else {

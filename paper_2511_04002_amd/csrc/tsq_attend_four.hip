@@ -27,6 +27,20 @@ template <bool BF16> struct Softmaxes {
 
 __device__ __forceinline__ uint32_t byte_of(uint32_t w, uint32_t shift) { return __builtin_amdgcn_ubfe(w, shift, 8); }
 
+// Codes, with a streaming load where they are read once.
+template <bool ONCE, typename T> __device__ __forceinline__ T codes_at(const uint8_t *at) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const T *>(at));
+    else return *reinterpret_cast<const T *>(at);
+}
+
+// The larger of a lane's value and that of the lane 16 away.
+__device__ __forceinline__ float max_across_sixteen(float x) {
+    const uint32_t bits = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(bits, bits, false, false);
+    const uint32_t a = r[0], b = r[1];
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
 // Products of 16 x 16 x 32 with binary32 sums.
 template <bool BF16> __device__ __forceinline__ float4_t product(uint4_t x, uint4_t y, float4_t z) {
     if constexpr (BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, y), z, 0, 0, 0);
@@ -40,20 +54,36 @@ template <bool BF16> __device__ __forceinline__ float4_t product(uint4_t x, uint
 //   16 tokens of its group; its row of the softmax is m.
 //   Keys: operand row m is token 16 (m / 4) + 4t + m % 4; the lane's elements are g D/4 .. + D/4 - 1, eight a product.
 //   Values: a lane has elements m D/16 .. + D/16 - 1 of its group's 16 tokens; row m of product j is element m D/16 + j.
-template <int D, bool BF16, int SETS>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(AttendArgs a) {
+struct FewShared {
+    float sums[4][16][132], stats[4][16][2];
+    uint32_t odd[4];                                     // of each wave: some value is one that the first pass cannot take
+};
+
+// Scales of 108 to 139, which the first pass takes (2^-19 to 2^12): the bytes of a word less 108 are below 32 each.  (Where one is
+// not, those above it may be off by its borrow, but it shows itself.)
+__device__ __forceinline__ uint32_t odd_scales(uint4_t s) {
+    constexpr uint32_t lowest = 0x6C6C6C6Cu;
+    return ((s[0] - lowest) | (s[1] - lowest) | (s[2] - lowest) | (s[3] - lowest)) & 0xE0E0E0E0u;
+}
+
+// CAREFUL: the second pass, for values that halves do not hold, or that are NaN and not seen by all rows.
+// -> whether the second pass is wanted.
+template <int D, bool BF16, int SETS, bool ONCE, bool CAREFUL>
+__device__ __forceinline__ bool attend_four_few(const AttendArgs &a, FewShared &shared) {
     constexpr int ROWS = 16 * SETS;
     constexpr int KW = D / 32;                           // words of a lane's keys of a token, and products of a score
     constexpr int KS = D == 256 ? 2 : 1;                 // scales of them
     constexpr int VE = D / 16;                           // elements of a lane's values of a token: 4, 8 or 16
     constexpr int VW = D == 256 ? 2 : 1;                 // words of them
     constexpr int GROUPS = D / 32;
-    __shared__ float sums[4][16][132];
-    __shared__ float stats[4][16][2];
+    constexpr bool VALUES_BF16 = BF16 && CAREFUL;
+    auto &sums = shared.sums;
+    auto &stats = shared.stats;
     Place p;
-    if (!find_place<ROWS>(a, p)) return;
+    if (!find_place<ROWS>(a, p)) return false;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
     const uint32_t B = 1u << a.block_log2;
+    uint32_t again = 0;
     const uint8_t *all_k = static_cast<const uint8_t *>(a.k), *all_v = static_cast<const uint8_t *>(a.v);
     const uint8_t *all_ks = static_cast<const uint8_t *>(a.k_scale), *all_vs = static_cast<const uint8_t *>(a.v_scale);
     for (uint32_t tile = p.tile;; ++tile) {
@@ -62,7 +92,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(Atten
         const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
         if (a.splits > 1 && reach.begin >= reach.end) {
             nothing_seen<ROWS>(a, p, tile, D);
-            if (done) return;
+            if (done) return again != 0;
             continue;
         }
         uint4_t q[SETS][KW];
@@ -79,14 +109,18 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(Atten
                 }
             }
             row_sees(a, p, row, from[c], to[c]);
+            to[c] = min(to[c], 0x7FFFFFFFu);
         }
         float4_t acc[SETS][VE];
         float ref[SETS], weight[SETS];
+        bool coarse[SETS];           // (see k_attend_four_many)
+        uint32_t odd = 0;
 #pragma unroll
         for (int c = 0; c < SETS; ++c) {
             for (int j = 0; j < VE; ++j) acc[c][j] = float4_t{0, 0, 0, 0};
             ref[c] = kNone;
             weight[c] = 0.0f;
+            coarse[c] = false;
         }
 
         // Loads are always on their way: a tile's keys are asked for while the tile before it is worked on, its values
@@ -94,147 +128,163 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(Atten
         uint32_t kw[4][KW], vw[16][VW];
         uint4_t ks[KS], vs;
         bool bad = false;
-        auto ask_keys = [&](uint32_t t0, uint32_t entry) {
-            const uint32_t id = (uint32_t)__shfl((int)id_of(a, entry), (int)(m >> 2) << 4), place = (t0 + 16 * (m >> 2)) & (B - 1);
-            const uint64_t head = (uint64_t)id * a.kv_heads + p.h;
+        auto ask_keys = [&](uint32_t t0, uint32_t id) {
+            const uint32_t key_id = (uint32_t)__shfl((int)id, (int)(m >> 2) << 4), place = (t0 + 16 * (m >> 2)) & (B - 1);
+            const uint64_t head = (uint64_t)key_id * a.kv_heads + p.h;
             const uint8_t *keys = all_k + (head * B + place + (m & 3)) * (D / 2) + g * (D / 8);
             const uint8_t *scales = all_ks + (head * GROUPS + g * (D / 4) / 32) * B + place;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const uint8_t *at = keys + 4 * t * (D / 2);
                 if constexpr (D == 64) {
-                    const uint2_t w = *reinterpret_cast<const uint2_t *>(at);
+                    const uint2_t w = codes_at<ONCE, uint2_t>(at);
                     kw[t][0] = w[0]; kw[t][1] = w[1];
                 } else {
                     for (int x = 0; x < KW; x += 4) {
-                        const uint4_t w = *reinterpret_cast<const uint4_t *>(at + 4 * x);
+                        const uint4_t w = codes_at<ONCE, uint4_t>(at + 4 * x);
                         for (int i = 0; i < 4; ++i) kw[t][x + i] = w[i];
                     }
                 }
             }
             for (int x = 0; x < KS; ++x) ks[x] = *reinterpret_cast<const uint4_t *>(scales + x * B);
-            bad = is_bad(a, p, entry);
         };
-        auto ask_values = [&](uint32_t t0, uint32_t entry) {
+        auto ask_values = [&](uint32_t t0, uint32_t id) {
             const uint32_t place = (t0 + 16 * g) & (B - 1);
-            const uint64_t head = (uint64_t)id_of(a, entry) * a.kv_heads + p.h;
+            const uint64_t head = (uint64_t)id * a.kv_heads + p.h;
             const uint8_t *values = all_v + (head * B + place) * (D / 2) + m * (D / 32);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                if constexpr (D == 64) vw[i][0] = *reinterpret_cast<const uint16_t *>(values + i * (D / 2));
-                else if constexpr (D == 128) vw[i][0] = *reinterpret_cast<const uint32_t *>(values + i * (D / 2));
+                if constexpr (D == 64) vw[i][0] = codes_at<ONCE, uint16_t>(values + i * (D / 2));
+                else if constexpr (D == 128) vw[i][0] = codes_at<ONCE, uint32_t>(values + i * (D / 2));
                 else {
-                    const uint2_t w = *reinterpret_cast<const uint2_t *>(values + i * (D / 2));
+                    const uint2_t w = codes_at<ONCE, uint2_t>(values + i * (D / 2));
                     vw[i][0] = w[0]; vw[i][1] = w[1];
                 }
             }
             vs = *reinterpret_cast<const uint4_t *>(all_vs + (head * GROUPS + m * VE / 32) * B + place);
         };
-        uint32_t t0 = reach.begin + 64 * wave, next = 0;
+        uint32_t t0 = reach.begin + 64 * wave;
         if (t0 < reach.end) {
-            const uint32_t entry = table_entry(a, p, t0 + 16 * g, reach.end);
-            next = table_entry(a, p, t0 + 256 + 16 * g, reach.end);
-            ask_keys(t0, entry);
-            ask_values(t0, entry);
-        }
-        for (; t0 < reach.end; t0 += 256) {
-            float4_t s[SETS][4];
+            const uint32_t first = table_entry(a, p, t0 + 16 * g, reach.end);
+            uint32_t next = table_entry(a, p, t0 + 256 + 16 * g, reach.end);
+            bad = is_bad(a, p, first);
+            ask_keys(t0, id_of(a, first));
+            ask_values(t0, id_of(a, first));
+            do {                     // (not a loop that may be left out: its loads would be waited for along with the queries')
+                float4_t s[SETS][4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                for (int c = 0; c < SETS; ++c) s[c][t] = float4_t{0, 0, 0, 0};
-                float scale[KS];
-                for (int x = 0; x < KS; ++x) scale[x] = four_scale(byte_of(ks[x][t], 8 * (m & 3)));
-                for (int j = 0; j < KW; ++j) {
-                    const uint4_t k = four_eight<BF16>(kw[t][j], scale[KS == 1 ? 0 : j / 4]);
-                    for (int c = 0; c < SETS; ++c) s[c][t] = product<BF16>(k, q[c][j], s[c][t]);
+                for (int t = 0; t < 4; ++t) {
+                    for (int c = 0; c < SETS; ++c) s[c][t] = float4_t{0, 0, 0, 0};
+                    float scale[KS];
+                    for (int x = 0; x < KS; ++x) scale[x] = four_scale(byte_of(ks[x][t], 8 * (m & 3)));
+                    for (int j = 0; j < KW; ++j) {
+                        const uint4_t k = four_eight<BF16>(kw[t][j], scale[KS == 1 ? 0 : j / 4]);
+                        for (int c = 0; c < SETS; ++c) s[c][t] = product<BF16>(k, q[c][j], s[c][t]);
+                    }
                 }
-            }
-            const float factor = bad ? __builtin_nanf("") : a.scale_log2;
-            const uint32_t entry = next;
-            ask_keys(t0 + 256, entry);
-            next = table_entry(a, p, t0 + 512 + 16 * g, reach.end);
-            // exponents, and the reference
-            const uint32_t mine = t0 + 16 * g;
-            uint4_t pw[SETS][2], rest[SETS][2];
+                const float all_factor = bad ? __builtin_nanf("") : a.scale_log2;
+                // (the entry is used up before the next one is asked for: a copy of it would wait for that)
+                const uint32_t mine = t0 + 16 * g, id = id_of(a, next);
+                bad = is_bad(a, p, next);
+                next = table_entry(a, p, t0 + 512 + 16 * g, reach.end);
+                ask_keys(t0 + 256, id);
+                // weights, and the reference
+                uint4_t pw[SETS][2], rest[SETS][2];
 #pragma unroll
-            for (int c = 0; c < SETS; ++c) {
-                const bool whole = __ballot(mine < from[c] || mine + 16 > to[c]) == 0;
+                for (int c = 0; c < SETS; ++c) {
+                    float factor = all_factor;
+                    if (coarse[c] || __ballot(mine < from[c] || mine + 16 > to[c])) {
+                        const int first = (int)(from[c] - mine), behind = (int)(to[c] - mine);
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    for (int i = 0; i < 4; ++i) s[c][t][i] *= factor;
-                if (!whole) {
+                        for (int e = 0; e < 16; ++e) s[c][e / 4][e & 3] = e < first || e >= behind ? -INFINITY : s[c][e / 4][e & 3] * factor;
+                        factor = 1.0f;
+                    }
+                    float top = -INFINITY;
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t token = mine + 4 * t + i;
-                            s[c][t][i] = token < from[c] || token >= to[c] ? -INFINITY : s[c][t][i];
-                        }
-                }
-                float top = -INFINITY;
+                        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[c][t][i]);
+                    top = max_across_halves(max_across_sixteen(top * factor));
+                    constexpr float room = Softmaxes<VALUES_BF16>::room, slack = Softmaxes<VALUES_BF16>::slack;
+                    if (__ballot(top > ref[c] + (room + slack))) {
+                        const float now = fmaxf(ref[c], top - room), down = pow2(ref[c] - now);
+                        ref[c] = now;
+                        weight[c] *= down;
+                        for (int j = 0; j < VE; ++j) acc[c][j] *= down;
+                        if (!coarse[c] && __ballot(fabsf(now) > kCoarse && fabsf(now) < -kNone)) {       // from here on
+                            coarse[c] = true;
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[c][t][i]);
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = max_across_halves(top);
-                constexpr float room = Softmaxes<BF16>::room, slack = Softmaxes<BF16>::slack;
-                if (__ballot(top > ref[c] + (room + slack))) {
-                    const float now = fmaxf(ref[c], top - room), down = pow2(ref[c] - now);
-                    ref[c] = now;
-                    weight[c] *= down;
-                    for (int j = 0; j < VE; ++j) acc[c][j] *= down;
-                }
-                float sum = 0.0f;
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    for (int i = 0; i < 4; i += 2) {
-                        const float e0 = pow2(s[c][t][i] - ref[c]), e1 = pow2(s[c][t][i + 1] - ref[c]);
-                        sum += e0 + e1;
-                        const uint32_t w = pack_two<BF16>(e0, e1);
-                        pw[c][t / 2][2 * (t & 1) + i / 2] = w;
-                        if constexpr (BF16) rest[c][t / 2][2 * (t & 1) + i / 2] = pack_two<true>(e0 - widen<true>(w & 0xFFFFu), e1 - widen<true>(w >> 16));
-                    }
-                weight[c] += sum;
-            }
-            // (no value that is not seen may bring NaN or infinity into a sum, whatever stands there: its scale is one of
-            // those that are finite, and its weight is 0.  A token whose values are NaN has keys that are NaN, too)
-            constexpr uint32_t highest = FourScales<BF16>::highest;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float scale[8];
-                for (int e = 0; e < 8; ++e) scale[e] = four_scale(min(byte_of(vs[2 * u + e / 4], 8 * (e & 3)), highest));
-                auto each = [&](auto pair) {             // two elements of the lane's: byte pair % 4 of word pair / 4
-                    constexpr int P = pair();
-                    uint4_t first, second;
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t x = four_pair<BF16, P % 4>(vw[8 * u + 2 * e][P / 4], scale[2 * e]);
-                        const uint32_t y = four_pair<BF16, P % 4>(vw[8 * u + 2 * e + 1][P / 4], scale[2 * e + 1]);
-                        first[e] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                        second[e] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-                    }
-                    for (int c = 0; c < SETS; ++c) {
-                        acc[c][2 * P] = product<BF16>(first, pw[c][u], acc[c][2 * P]);
-                        acc[c][2 * P + 1] = product<BF16>(second, pw[c][u], acc[c][2 * P + 1]);
-                        if constexpr (BF16) {
-                            acc[c][2 * P] = product<BF16>(first, rest[c][u], acc[c][2 * P]);
-                            acc[c][2 * P + 1] = product<BF16>(second, rest[c][u], acc[c][2 * P + 1]);
+                            for (int t = 0; t < 4; ++t)
+                                for (int i = 0; i < 4; ++i) s[c][t][i] *= factor;
+                            factor = 1.0f;
                         }
                     }
-                };
-                each(std::integral_constant<int, 0>{});
-                each(std::integral_constant<int, 1>{});
-                if constexpr (VE >= 8) {
-                    each(std::integral_constant<int, 2>{});
-                    each(std::integral_constant<int, 3>{});
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        for (int i = 0; i < 4; i += 2) {
+                            const float e0 = pow2(__builtin_fmaf(s[c][t][i], factor, -ref[c])), e1 = pow2(__builtin_fmaf(s[c][t][i + 1], factor, -ref[c]));
+                            sum += e0 + e1;
+                            const uint32_t w = pack_two<VALUES_BF16>(e0, e1);
+                            pw[c][t / 2][2 * (t & 1) + i / 2] = w;
+                            if constexpr (VALUES_BF16) rest[c][t / 2][2 * (t & 1) + i / 2] = pack_two<true>(e0 - widen<true>(w & 0xFFFFu), e1 - widen<true>(w >> 16));
+                        }
+                    weight[c] += sum;
                 }
-                if constexpr (VE >= 16) {
-                    each(std::integral_constant<int, 4>{});
-                    each(std::integral_constant<int, 5>{});
-                    each(std::integral_constant<int, 6>{});
-                    each(std::integral_constant<int, 7>{});
+                // No value that is not seen may bring NaN or infinity into a sum with a weight of 0.  (A token whose values are NaN
+                // has keys that are NaN, too.)  Behind the request's end a scale may be anything.
+                if (t0 + 64 > p.seen) {
+                    const int behind = (int)(p.seen - mine);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (e >= behind) vs[e / 4] = (vs[e / 4] & ~(0xFFu << 8 * (e & 3))) | 127u << 8 * (e & 3);
                 }
-            }
-            ask_values(t0 + 256, entry);
+                if constexpr (!CAREFUL) odd |= odd_scales(vs);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float scale[8];
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t w = vs[2 * u + e / 4];
+                        scale[e] = CAREFUL ? four_scale(min(w >> 8 * (e & 3) & 0xFFu, (uint32_t)FourScales<BF16>::highest)) :
+                                   (e & 3) == 0 ? four_scale_at<0>(w) : (e & 3) == 1 ? four_scale_at<1>(w) : (e & 3) == 2 ? four_scale_at<2>(w) : four_scale_at<3>(w);
+                    }
+                    auto each = [&](auto pair) {         // two elements of the lane's: byte pair % 4 of word pair / 4
+                        constexpr int P = pair();
+                        uint4_t one, two;
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t x = four_pair<VALUES_BF16, P % 4>(vw[8 * u + 2 * e][P / 4], scale[2 * e]);
+                            const uint32_t y = four_pair<VALUES_BF16, P % 4>(vw[8 * u + 2 * e + 1][P / 4], scale[2 * e + 1]);
+                            one[e] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                            two[e] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                        }
+                        for (int c = 0; c < SETS; ++c) {
+                            acc[c][2 * P] = product<VALUES_BF16>(one, pw[c][u], acc[c][2 * P]);
+                            acc[c][2 * P + 1] = product<VALUES_BF16>(two, pw[c][u], acc[c][2 * P + 1]);
+                            if constexpr (VALUES_BF16) {
+                                acc[c][2 * P] = product<true>(one, rest[c][u], acc[c][2 * P]);
+                                acc[c][2 * P + 1] = product<true>(two, rest[c][u], acc[c][2 * P + 1]);
+                            }
+                        }
+                    };
+                    each(std::integral_constant<int, 0>{});
+                    each(std::integral_constant<int, 1>{});
+                    if constexpr (VE >= 8) {
+                        each(std::integral_constant<int, 2>{});
+                        each(std::integral_constant<int, 3>{});
+                    }
+                    if constexpr (VE >= 16) {
+                        each(std::integral_constant<int, 4>{});
+                        each(std::integral_constant<int, 5>{});
+                        each(std::integral_constant<int, 6>{});
+                        each(std::integral_constant<int, 7>{});
+                    }
+                }
+                ask_values(t0 + 256, id);
+                t0 += 256;
+                asm volatile("" ::: "memory");           // (the loads are to stay here: at the loop's head they would wait for the keys)
+            } while (t0 < reach.end);
         }
+        const bool any_odd = !CAREFUL && __ballot(odd != 0);
+        if (!CAREFUL && lane == 0) shared.odd[wave] = any_odd;
 
         // the four waves' sums, at one reference
 #pragma unroll
@@ -244,6 +294,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(Atten
             if (c) __syncthreads();
             if (g == 0) { stats[wave][m][0] = ref[c]; stats[wave][m][1] = weight[c]; }
             __syncthreads();
+            if (!CAREFUL && c == 0) again |= shared.odd[0] | shared.odd[1] | shared.odd[2] | shared.odd[3];
             const float all = fmaxf(fmaxf(stats[0][m][0], stats[1][m][0]), fmaxf(stats[2][m][0], stats[3][m][0]));
             const float mine = pow2(ref[c] - all);
             const uint32_t out_row = threadIdx.x >> 4, piece = threadIdx.x & 15, o = tile * ROWS + 16 * c + out_row;
@@ -292,8 +343,34 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(Atten
                 }
             }
         }
-        if (done) return;
+        if (done) return again != 0;
         __syncthreads();
+    }
+}
+
+// The kernel's arguments, in a function that it calls at its end.
+typedef const __attribute__((address_space(4))) void *KernelArgs;
+__device__ __forceinline__ AttendArgs args_of(KernelArgs args) {
+    struct Words { uint32_t w[sizeof(AttendArgs) / 4]; } words;
+    const uint64_t bits = (uint64_t)args;
+    const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)bits);
+    for (uint32_t i = 0; i < sizeof(AttendArgs) / 4; ++i) words.w[i] = ((const __attribute__((address_space(4))) uint32_t *)from)[i];
+    return __builtin_bit_cast(AttendArgs, words);
+}
+
+// All of a workgroup's tiles once more.  Not inlined, and the last thing that it does: what this pass keeps in registers would be
+// taken from the first one's loop.
+template <int D, bool BF16, int SETS>
+__device__ __attribute__((noinline)) void attend_four_few_again(KernelArgs args, __attribute__((address_space(3))) FewShared *shared) {
+    attend_four_few<D, BF16, SETS, false, true>(args_of(args), *(FewShared *)shared);
+}
+
+template <int D, bool BF16, int SETS, bool ONCE>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(AttendArgs a) {
+    __shared__ FewShared shared;
+    if (__builtin_amdgcn_readfirstlane((int)attend_four_few<D, BF16, SETS, ONCE, false>(a, shared))) {
+        __syncthreads();
+        attend_four_few_again<D, BF16, SETS>((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), (__attribute__((address_space(3))) FewShared *)&shared);
     }
 }
 
@@ -560,13 +637,8 @@ __device__ __forceinline__ void attend_four_tiles(const AttendArgs &a, FourTile<
 // All of them once more.  Not inlined, and the last thing that a workgroup does: what this pass keeps in registers would be
 // taken from the first one's loop, which then loads its operands one by one.
 template <int D, int WAVES, int TOKENS>
-__device__ __attribute__((noinline)) void attend_four_again(const __attribute__((address_space(4))) void *args,
-                                                            __attribute__((address_space(3))) FourTile<D, TOKENS> *buffer) {
-    struct Words { uint32_t w[sizeof(AttendArgs) / 4]; } words;
-    const uint64_t bits = (uint64_t)args;
-    const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)bits);
-    for (uint32_t i = 0; i < sizeof(AttendArgs) / 4; ++i) words.w[i] = ((const __attribute__((address_space(4))) uint32_t *)from)[i];
-    attend_four_tiles<D, true, WAVES, TOKENS, true>(__builtin_bit_cast(AttendArgs, words), (FourTile<D, TOKENS> *)buffer, nullptr);
+__device__ __attribute__((noinline)) void attend_four_many_again(KernelArgs args, __attribute__((address_space(3))) FourTile<D, TOKENS> *buffer) {
+    attend_four_tiles<D, true, WAVES, TOKENS, true>(args_of(args), (FourTile<D, TOKENS> *)buffer, nullptr);
 }
 
 template <int D, bool BF16, int WAVES, int TOKENS>
@@ -581,18 +653,27 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_four_many(AttendArgs a
     if constexpr (BF16) {
         __syncthreads();
         if (__builtin_amdgcn_readfirstlane((int)outside))
-            attend_four_again<D, WAVES, TOKENS>((const __attribute__((address_space(4))) void *)__builtin_amdgcn_kernarg_segment_ptr(),
-                                                (__attribute__((address_space(3))) FourTile<D, TOKENS> *)buffer);
+            attend_four_many_again<D, WAVES, TOKENS>((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(),
+                                                     (__attribute__((address_space(3))) FourTile<D, TOKENS> *)buffer);
     }
 }
 
 }  // namespace
 
-void launch_attend_four(const CacheShape &s, uint32_t rows, uint32_t grid, const AttendArgs &a, void *stream) {
+void launch_attend_four(const CacheShape &s, uint32_t rows, bool once, uint32_t grid, const AttendArgs &a, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     by_shape(s, [&](auto d, auto bf16) {
-        if (rows == 16) k_attend_four_few<d(), bf16(), 1><<<grid, 256, 0, st>>>(a);
-        else if (rows == 32) { if constexpr (d() != 256) k_attend_four_few<d(), bf16(), 2><<<grid, 256, 0, st>>>(a); }
+        auto few = [&](auto sets) {
+            // Streaming loads, of heads of 128 alone, whose pieces are whole halves of lines, and where a request has one tile: 64
+            // requests of 1024 to 4096 tokens on 40 heads 166 us against 180; but heads of 64 55 against 39, of 256 88 against 85,
+            // and two tiles of 16 requests of 4096 on 8 heads, which read the cache twice, 43 against 39.
+            if constexpr (d() == 128) {
+                if (once) { k_attend_four_few<d(), bf16(), sets(), true><<<grid, 256, 0, st>>>(a); return; }
+            }
+            k_attend_four_few<d(), bf16(), sets(), false><<<grid, 256, 0, st>>>(a);
+        };
+        if (rows == 16) few(std::integral_constant<int, 1>{});
+        else if (rows == 32) { if constexpr (d() != 256) few(std::integral_constant<int, 2>{}); }
         else if (rows == 128) k_attend_four_many<d(), bf16(), 4, d() == 256 ? 32 : 64><<<grid, 256, 0, st>>>(a);
         else if constexpr (d() != 256) k_attend_four_many<d(), bf16(), 8, 128><<<grid, 512, 0, st>>>(a);
     });

@@ -128,8 +128,8 @@ struct AttendLaunch {
 AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t tokens, uint32_t max_new, uint32_t max_length,
                            uint32_t window);
 int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &a, void *stream);
-// The kernels of a cache in 4 bits, for tiles of `rows` rows of a kv head.
-void launch_attend_four(const CacheShape &s, uint32_t rows, uint32_t grid, const AttendArgs &a, void *stream);
+// The kernels of a cache in 4 bits, for tiles of `rows` rows of a kv head; once: no request has more of few rows.
+void launch_attend_four(const CacheShape &s, uint32_t rows, bool once, uint32_t grid, const AttendArgs &a, void *stream);
 
 // f(head_dim, bfloat16 or not), both as types whose value is known when compiling.
 template <class F> void by_shape(const CacheShape &s, F f) {

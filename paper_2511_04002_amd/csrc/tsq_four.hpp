@@ -24,6 +24,17 @@ template <bool BF16> struct FourScales { static constexpr int lowest = BF16 ? 12
 // Bits of a scale's byte as binary32 (infinity of 255, which the conversions take as NaN).
 __device__ __forceinline__ float four_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
+// ... of a word's byte, in one instruction (the compiler takes two).
+template <int BYTE> __device__ __forceinline__ float four_scale_at(uint32_t w) {
+    float f;
+    const uint32_t by = 23;
+    if constexpr (BYTE == 0) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(f) : "v"(by), "v"(w));
+    else if constexpr (BYTE == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(f) : "v"(by), "v"(w));
+    else if constexpr (BYTE == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(f) : "v"(by), "v"(w));
+    else asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(f) : "v"(by), "v"(w));
+    return f;
+}
+
 // Two elements of a word's byte, in 16 bits each.
 template <bool BF16, int BYTE> __device__ __forceinline__ uint32_t four_pair(uint32_t w, float scale) {
     if constexpr (BF16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, BYTE));
