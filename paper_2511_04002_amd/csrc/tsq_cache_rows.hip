@@ -188,7 +188,7 @@ __global__ __launch_bounds__(kScheduleThreads) void k_schedule(ScheduleArgs a) {
 // together are the lane's own: D / 16 lanes a head, 1024 / D heads a wave.  The sum of squares, the product with the
 // weight and the rotation stay in registers, in binary32; memory is read and written once, and bounds it: 8192 rows of
 // 72 heads of 128 are 306 MB and 54 us, 5.7 TB/s where a copy reaches 6.2.
-template <int D, bool BF16, bool AXES>
+template <int D, bool BF16, bool AXES, bool ONCE>
 __global__ __launch_bounds__(256) void k_norm_rotate(NormRotateArgs a, uint32_t passes, uint32_t waves_each) {
     constexpr int LPH = D / 16, HEADS = 64 / LPH;
     const uint32_t lane = threadIdx.x & 63, wave = blockIdx.x * 4 + wave_in_group();
@@ -216,19 +216,29 @@ __global__ __launch_bounds__(256) void k_norm_rotate(NormRotateArgs a, uint32_t 
         const float *row = a.angles + (uint64_t)position * a.rotary + 8 * j;
         bool together = true;
         if constexpr (AXES) {
-            // the pairs' angles are those of their axes' rows; where a lane's eight have one axis, as most have, in two loads
+            // the pairs' angles are those of their axes' rows; where a lane's eight have several axes, all rows are read and chosen from
             const uint2_t axis = *reinterpret_cast<const uint2_t *>(a.axis + 8 * j);
             auto place_on = [&](uint32_t x) { return x == 0 ? position : x == 1 ? others[0] : x == 2 ? others[1] : others[2]; };
             const uint32_t first = axis[0] & 0xFFu;
             together = axis[0] == axis[1] && axis[0] == first * 0x01010101u && first < a.axes;
             row = a.angles + (uint64_t)(uint32_t)place_on(first) * a.rotary + 8 * j;
-            if (!together)
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t x = axis[i / 4] >> 8 * (i % 4) & 0xFFu;
-                    const float *at = a.angles + (uint64_t)(uint32_t)place_on(x) * a.rotary + 8 * j + i;
-                    c[i] = x < a.axes ? at[0] : __builtin_nanf("");
-                    s[i] = x < a.axes ? at[a.rotary / 2] : __builtin_nanf("");
+            if (!together) {
+                for (int i = 0; i < 8; ++i) c[i] = s[i] = __builtin_nanf("");
+                for (uint32_t x = 0; x < kMaxAxes; ++x) {
+                    if (x >= a.axes) break;
+                    const float *at = a.angles + (uint64_t)(uint32_t)place_on(x) * a.rotary + 8 * j;
+                    float4_t cs[2], sn[2];
+                    for (int i = 0; i < 2; ++i) {
+                        cs[i] = *reinterpret_cast<const float4_t *>(at + 4 * i);
+                        sn[i] = *reinterpret_cast<const float4_t *>(at + a.rotary / 2 + 4 * i);
+                    }
+                    for (int i = 0; i < 8; ++i) {
+                        const bool here = (axis[i / 4] >> 8 * (i % 4) & 0xFFu) == x;
+                        c[i] = here ? cs[i / 4][i % 4] : c[i];
+                        s[i] = here ? sn[i / 4][i % 4] : s[i];
+                    }
                 }
+            }
         }
         if (together)
             for (int i = 0; i < 8; i += 4) {
@@ -248,7 +258,8 @@ __global__ __launch_bounds__(256) void k_norm_rotate(NormRotateArgs a, uint32_t 
         const uint16_t *in = static_cast<const uint16_t *>(is_q ? a.q : a.k) + in_at;
         float x[16];
         if (here) {
-            const uint4_t p0 = *reinterpret_cast<const uint4_t *>(in + e0), p1 = *reinterpret_cast<const uint4_t *>(in + e1);
+            const uint4_t *in0 = reinterpret_cast<const uint4_t *>(in + e0), *in1 = reinterpret_cast<const uint4_t *>(in + e1);
+            const uint4_t p0 = ONCE ? __builtin_nontemporal_load(in0) : *in0, p1 = ONCE ? __builtin_nontemporal_load(in1) : *in1;
             for (int i = 0; i < 4; ++i) {
                 x[2 * i] = widen<BF16>(p0[i] & 0xFFFFu); x[2 * i + 1] = widen<BF16>(p0[i] >> 16);
                 x[8 + 2 * i] = widen<BF16>(p1[i] & 0xFFFFu); x[9 + 2 * i] = widen<BF16>(p1[i] >> 16);
@@ -789,8 +800,12 @@ int launch_norm_rotate(const CacheShape &s, const NormRotateArgs &a, void *strea
     const uint32_t each = (uint64_t)a.tokens * passes <= 4096 ? passes : (passes + 2) / 3;
     if (int e = workgroups((uint64_t)a.tokens * each, &grid)) return e;
     by_shape(s, [&](auto d, auto bf16) {
-        if (a.axes) k_norm_rotate<d(), bf16(), true><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, passes, each);
-        else k_norm_rotate<d(), bf16(), false><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, passes, each);
+        const hipStream_t st = static_cast<hipStream_t>(stream);
+        // Streaming loads, which leave the caches to several axes' rows of angles, where the heads are more than the caches hold: 8192 rows
+        // of 72 heads of 128 by three axes 58.9 us against 59.9, pairs dealt out in turn 62.5 against 66; 2048 rows of 40 13.0 against 10.8.
+        if (a.axes == 0) k_norm_rotate<d(), bf16(), false, false><<<grid, 256, 0, st>>>(a, passes, each);
+        else if (2ull * a.tokens * (a.q_heads + a.kv_heads) * d() >= 64ull << 20) k_norm_rotate<d(), bf16(), true, true><<<grid, 256, 0, st>>>(a, passes, each);
+        else k_norm_rotate<d(), bf16(), true, false><<<grid, 256, 0, st>>>(a, passes, each);
     });
     return (int)hipGetLastError();
 }

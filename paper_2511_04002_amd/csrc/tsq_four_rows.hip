@@ -42,92 +42,143 @@ template <bool BF16> __device__ __forceinline__ uint32_t four_codes(uint4_t w, f
     return c;
 }
 
-// A lane has eight elements of a token's keys of a head, and the values' at the same place: D / 8 lanes a head, 512 / D
-// heads a wave.  No token depends on another.
-template <int D, bool BF16>
-__global__ __launch_bounds__(256) void k_append_four(AppendFourArgs a) {
-    constexpr uint32_t LPH = D / 8, HEADS = 64 / LPH, GROUPS = D / 32;
-    const uint32_t lane = threadIdx.x & 63, piece = lane % LPH, B = 1u << a.block_log2;
-    const uint32_t at = (blockIdx.x * 4 + wave_in_group()) * HEADS + lane / LPH, token = at / a.kv_heads, h = at % a.kv_heads;
-    const bool here = token < a.tokens;
-    const uint32_t slot = here ? (uint32_t)a.slots[token] : ~0u, block = slot >> a.block_log2, place = slot & (B - 1);
-    const bool stored = block < a.blocks;                // (a negative slot's is not)
-    uint4_t k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-    if (stored) {
-        k = *reinterpret_cast<const uint4_t *>(static_cast<const uint16_t *>(a.k) + token * a.k_stride + (uint64_t)h * D + 8 * piece);
-        v = *reinterpret_cast<const uint4_t *>(static_cast<const uint16_t *>(a.v) + token * a.v_stride + (uint64_t)h * D + 8 * piece);
+// 16 rows of some heads a workgroup, as many as 512 elements are: rows are read and written one behind the other, the cache's
+// tokens head after head, and between the two the codes go through LDS.  Both kernels write whole lines where their rows are
+// tokens of a block that follow one another, 256 threads 4 KB of codes.
+constexpr uint32_t kElements = 512;
+template <int D> struct FourRows {
+    static constexpr uint32_t heads = kElements / D, pieces = D / 32, groups = D / 32;    // pieces: of 16 bytes, of a head's row
+    uint8_t codes[2][16][kElements / 2 + 16], scales[2][16][kElements / 32 + 4];
+};
+// The head, row and piece that a thread has of the cache.
+template <int D> struct FourPiece {
+    uint32_t h, r, piece;
+    __device__ __forceinline__ FourPiece() : h(threadIdx.x / (D / 32) / 16), r(threadIdx.x / (D / 32) % 16), piece(threadIdx.x % (D / 32)) {}
+};
+
+// A token does not depend on another.
+template <int D, bool BF16, bool ONCE>
+__global__ __launch_bounds__(256) void k_append_four(AppendFourArgs a, uint32_t groups_each) {
+    typedef FourRows<D> Rows;
+    constexpr uint32_t LPH = D / 8;                      // lanes with eight elements each of a head
+    __shared__ __attribute__((aligned(16))) Rows rows;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, B = 1u << a.block_log2;
+    const uint64_t begin = (uint64_t)(blockIdx.x / groups_each) * 16;
+    const uint32_t h0 = blockIdx.x % groups_each * Rows::heads, heads = min(Rows::heads, a.kv_heads - h0);
+    const uint32_t slot = begin + (lane & 15) < a.tokens ? (uint32_t)a.slots[begin + (lane & 15)] : ~0u;
+    uint4_t x[2][4];
+    const bool there = lane < heads * LPH;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t row = begin + 4 * i + (tid >> 6), at = (uint64_t)h0 * D + 8 * lane;
+        x[0][i] = x[1][i] = uint4_t{0, 0, 0, 0};
+        if (there && row < a.tokens) {
+            const uint4_t *k = reinterpret_cast<const uint4_t *>(static_cast<const uint16_t *>(a.k) + row * a.k_stride + at);
+            const uint4_t *v = reinterpret_cast<const uint4_t *>(static_cast<const uint16_t *>(a.v) + row * a.v_stride + at);
+            x[0][i] = ONCE ? __builtin_nontemporal_load(k) : *k;
+            x[1][i] = ONCE ? __builtin_nontemporal_load(v) : *v;
+        }
     }
-    const uint32_t mk = most_of_four(most_of(k)), mv = most_of_four(most_of(v));
-    const uint64_t odd = __ballot(max(mk, mv) >= (BF16 ? 0x7F80u : 0x7C00u));
-    const bool bad = (odd >> (lane / LPH * LPH) & (~0ull >> (64 - LPH))) != 0;
-    const uint32_t sk = scale_byte<BF16>(mk), sv = scale_byte<BF16>(mv);
-    if (!stored) return;
-    const uint64_t head = (uint64_t)block * a.kv_heads + h;
-    const uint64_t codes = (head * B + place) * (D / 2) + 4 * piece, scale = (head * GROUPS + piece / 4) * B + place;
-    *reinterpret_cast<uint32_t *>(a.k_codes + codes) = four_codes<BF16>(k, four_scale(sk));
-    *reinterpret_cast<uint32_t *>(a.v_codes + codes) = four_codes<BF16>(v, four_scale(sv));
-    if (piece % 4 == 0) {
-        a.k_scale[scale] = (uint8_t)(bad ? kNotANumber : sk);
-        a.v_scale[scale] = (uint8_t)(bad ? kNotANumber : sv);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t r = 4 * i + (tid >> 6), mk = most_of_four(most_of(x[0][i])), mv = most_of_four(most_of(x[1][i]));
+        const uint64_t odd = __ballot(max(mk, mv) >= (BF16 ? 0x7F80u : 0x7C00u));
+        const bool bad = (odd >> (lane / LPH * LPH) & (~0ull >> (64 - LPH))) != 0;
+        for (int y = 0; y < 2; ++y) {
+            const uint32_t byte = scale_byte<BF16>(y ? mv : mk);
+            *reinterpret_cast<uint32_t *>(&rows.codes[y][r][4 * lane]) = four_codes<BF16>(x[y][i], four_scale(byte));
+            if (lane % 4 == 0) rows.scales[y][r][lane / 4] = (uint8_t)(bad ? kNotANumber : byte);
+        }
+    }
+    __syncthreads();
+    uint8_t *const codes[2] = {a.k_codes, a.v_codes}, *const scales[2] = {a.k_scale, a.v_scale};
+    {
+        const FourPiece<D> p;
+        const uint32_t of_row = (uint32_t)__shfl((int)slot, (int)p.r), block = of_row >> a.block_log2, place = of_row & (B - 1);
+        if (block < a.blocks && p.h < heads) {           // (a negative slot's is past all)
+            const uint64_t head = (uint64_t)block * a.kv_heads + h0 + p.h;
+            for (int y = 0; y < 2; ++y)
+                *reinterpret_cast<uint4_t *>(codes[y] + (head * B + place) * (D / 2) + 16 * p.piece) =
+                    *reinterpret_cast<const uint4_t *>(&rows.codes[y][p.r][p.h * (D / 2) + 16 * p.piece]);
+        }
+    }
+    // scales: a group's of 16 rows side by side
+    const uint32_t r = tid % 16, group = tid / 16, h = group / Rows::groups, block = slot >> a.block_log2, place = slot & (B - 1);
+    if (block < a.blocks && h < heads) {
+        const uint64_t head = (uint64_t)block * a.kv_heads + h0 + h;
+        for (int y = 0; y < 2; ++y) scales[y][(head * Rows::groups + group % Rows::groups) * B + place] = rows.scales[y][r][group];
     }
 }
 
-// 16 rows a wave, and a share of their heads: a lane has eight elements, D / 8 lanes a row of a head.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void k_gather_four(GatherArgs a) {
-    constexpr uint32_t LPT = D / 8, TPI = 64 / LPT, LOADS = 16 / TPI, GROUPS = D / 32;
-    const uint32_t lane = threadIdx.x & 63, B = a.block_tokens, piece = lane % LPT, sub = lane / LPT;
-    const uint64_t begin = ((uint64_t)(blockIdx.x / a.waves_each) * 4 + wave_in_group()) * 16;
-    if (begin >= a.tokens) return;
+    typedef FourRows<D> Rows;
+    __shared__ __attribute__((aligned(16))) Rows rows;
+    const uint32_t tid = threadIdx.x, B = a.block_tokens;
+    const uint64_t begin = (uint64_t)(blockIdx.x / a.waves_each) * 16;
+    const uint32_t h0 = blockIdx.x % a.waves_each * Rows::heads, heads = min(Rows::heads, a.kv_heads - h0);
     const GatherRow row = gather_row(a, begin);
-    int32_t block[LOADS];                                // -2: no request's row
-    uint32_t place[LOADS];
-#pragma unroll
-    for (uint32_t t = 0; t < LOADS; ++t) {
-        block[t] = __shfl(row.owned ? row.block : -2, (int)(TPI * t + sub));
-        place[t] = (uint32_t)__shfl((int)row.place, (int)(TPI * t + sub));
-    }
-    for (uint32_t h = blockIdx.x % a.waves_each; h < a.kv_heads; h += a.waves_each) {
-        uint32_t w[2][LOADS], s[2][LOADS];
-#pragma unroll
-        for (uint32_t t = 0; t < LOADS; ++t) {
-            const uint64_t head = (uint64_t)max(block[t], 0) * a.kv_heads + h;
-            const uint64_t codes = (head * B + place[t]) * (D / 2) + 4 * piece, scale = (head * GROUPS + piece / 4) * B + place[t];
-            for (int x = 0; x < 2; ++x) {
-                w[x][t] = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.codes[x]) + codes);
-                s[x][t] = static_cast<const uint8_t *>(a.scale[x])[scale];
-            }
+    {
+        const FourPiece<D> p;
+        const int32_t block = __shfl(row.block, (int)p.r);
+        const uint32_t place = (uint32_t)__shfl((int)row.place, (int)p.r);
+        const uint64_t head = (uint64_t)max(block, 0) * a.kv_heads + h0 + min(p.h, heads - 1);
+        uint4_t w[2];
+        uint32_t s[2];
+        for (int x = 0; x < 2; ++x) {
+            w[x] = *reinterpret_cast<const uint4_t *>(static_cast<const uint8_t *>(a.codes[x]) + (head * B + place) * (D / 2) + 16 * p.piece);
+            s[x] = static_cast<const uint8_t *>(a.scale[x])[(head * Rows::groups + p.piece) * B + place];
         }
-#pragma unroll
-        for (uint32_t t = 0; t < LOADS; ++t) {
-            if (block[t] == -2) continue;
-            for (int x = 0; x < 2; ++x) {
-                const uint4_t y = four_eight<BF16>(w[x][t], four_scale(block[t] < 0 ? kNotANumber : s[x][t]));
-                uint16_t *out = static_cast<uint16_t *>(a.out[x]) + (begin + TPI * t + sub) * a.stride[x] + (uint64_t)h * D + 8 * piece;
-                __builtin_nontemporal_store(y, reinterpret_cast<uint4_t *>(out));
-            }
+        for (int x = 0; x < 2; ++x) {
+            *reinterpret_cast<uint4_t *>(&rows.codes[x][p.r][p.h * (D / 2) + 16 * p.piece]) = w[x];
+            rows.scales[x][p.r][p.h * Rows::groups + p.piece] = (uint8_t)(block < 0 ? kNotANumber : s[x]);
         }
     }
+    __syncthreads();
+    const uint32_t owned = (uint32_t)__ballot(row.owned && (tid & 63) < 16), at = tid & 63;
+    if (at >= heads * (D / 8)) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t r = 4 * i + (tid >> 6);
+        if (!(owned >> r & 1)) continue;
+        for (int x = 0; x < 2; ++x) {
+            const uint4_t y = four_eight<BF16>(*reinterpret_cast<const uint32_t *>(&rows.codes[x][r][4 * at]), four_scale(rows.scales[x][r][at / 4]));
+            uint16_t *out = static_cast<uint16_t *>(a.out[x]) + (begin + r) * a.stride[x] + (uint64_t)h0 * D + 8 * at;
+            __builtin_nontemporal_store(y, reinterpret_cast<uint4_t *>(out));
+        }
+    }
+}
+
+// Workgroups of 16 rows; 0: too many in all.
+uint32_t workgroups_each(const CacheShape &s, uint32_t tokens, uint32_t *grid) {
+    const uint64_t groups = ((uint64_t)tokens + 15) / 16, each = ((uint64_t)s.kv_heads * s.head_dim + kElements - 1) / kElements;
+    if (!fits(groups * each, 256)) return 0;
+    *grid = (uint32_t)(groups * each);
+    return (uint32_t)each;
 }
 
 }  // namespace
 
 int launch_append_four(const CacheShape &s, const AppendFourArgs &a, void *stream) {
-    const uint32_t heads = 512 / s.head_dim;             // a wave
     uint32_t grid;
-    if (int e = workgroups(((uint64_t)a.tokens * s.kv_heads + heads - 1) / heads, &grid)) return e;
-    by_shape(s, [&](auto d, auto bf16) { k_append_four<d(), bf16()><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a); });
+    const uint32_t each = workgroups_each(s, a.tokens, &grid);
+    if (!each) return kTooLarge;
+    // Streaming loads where the rows are more than a program has just made and the caches still hold: 22090 rows of 8 heads of 128
+    // (90 MB) 23.6 us against 26.0, 30000 29.4 against 33.5; 3500 of 32 (57 MB) 18.0 against 16.7.
+    const bool once = 4ull * a.tokens * s.kv_heads * s.head_dim >= 64ull << 20;
+    by_shape(s, [&](auto d, auto bf16) {
+        if (once) k_append_four<d(), bf16(), true><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, each);
+        else k_append_four<d(), bf16(), false><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, each);
+    });
     return (int)hipGetLastError();
 }
 
 int launch_gather_four(const CacheShape &s, const GatherArgs &args, void *stream) {
     GatherArgs a = args;
-    const uint64_t groups = ((uint64_t)a.tokens + 63) / 64;
-    uint64_t each = (4096 + groups - 1) / groups;
-    if (each > s.kv_heads) each = s.kv_heads;
-    a.waves_each = (uint32_t)each;
-    if (!fits(groups * each, 256)) return kTooLarge;
-    by_shape(s, [&](auto d, auto bf16) { k_gather_four<d(), bf16()><<<(uint32_t)(groups * each), 256, 0, static_cast<hipStream_t>(stream)>>>(a); });
+    uint32_t grid;
+    a.waves_each = workgroups_each(s, a.tokens, &grid);
+    if (!a.waves_each) return kTooLarge;
+    by_shape(s, [&](auto d, auto bf16) { k_gather_four<d(), bf16()><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a); });
     return (int)hipGetLastError();
 }
 
