@@ -17,6 +17,8 @@
 // a tile are dealt to the lanes such that nothing has to be moved.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "tsq_attend.hpp"
 
 namespace tsq {
@@ -832,6 +834,10 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
     // little more than one round the ranking costs more than it brings: 20 requests of 250 to 1000 tokens on 32 heads 29
     // against 25).  A wave ranks 64 requests.
     l.by_length = l.tiles_each && requests > 1 && requests <= 64 && units * l.splits >= 4 * slots;
+    if (s.bits == 4 && s.head_dim != 256 && l.rows <= 32 && l.tiles_each == 1 && requests > 1 && requests <= 64 && units * l.splits > 256 && units * l.splits <= 512) {
+        const uint32_t turn = (uint32_t)(256 / (s.kv_heads * l.splits));
+        if (turn >= 1 && turn < requests) l.by_length = turn + 1;
+    }
     return l;
 }
 
@@ -866,6 +872,7 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
         f.rows_to = few_rows(s);
         f.splits = l.few_splits;
         f.chunk = l.few_chunk;
+        f.least = std::max(256u, l.few_chunk / 4 / 128 * 128);
         f.parts = j.few_parts;
         f.part_rows = l.few_part_rows;
         f.slots_each = l.slots_each;

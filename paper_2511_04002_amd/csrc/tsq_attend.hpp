@@ -55,6 +55,11 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
             const uint32_t mine = min((uint32_t)max(lane < a.requests ? a.lengths[lane] : 0, 0), (1u << 26) - 1) << 6 | lane;
             uint32_t below = 0;
             for (uint32_t j = 0; j < a.requests; ++j) below += (uint32_t)__builtin_amdgcn_readlane((int)mine, (int)j) < mine ? 1 : 0;
+            // (or, where all of two rounds run at once, the second round's from the shortest on: a CU has one of each)
+            if (a.by_length > 1) {
+                const uint32_t turn = a.by_length - 1, nth = a.requests - 1 - p.r;
+                if (nth >= turn) p.r = nth - turn;
+            }
             p.r = (uint32_t)__builtin_ctzll(__ballot(lane < a.requests && below == p.r));
         }
     } else {
@@ -89,17 +94,21 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
     return p.tile * (uint64_t)ROWS < rows && rows >= a.rows_from && rows <= a.rows_to;
 }
 
-// Tokens that any row of a tile sees, the part of them that a split has, and what a row sees.
+// Tokens that any row of a tile sees, the part of them that a split has, and what a row sees.  EVEN: the pieces of a tile are
+// alike, down to a.least tokens, instead of a.chunk each.
 struct Reach { uint32_t begin, end; };
-template <int ROWS>
+template <int ROWS, bool EVEN = false>
 __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Place &p, uint32_t tile) {
     const int64_t rows = (int64_t)p.n * a.group, first = (int64_t)tile * ROWS, last = min(first + ROWS, rows) - 1;
     const int64_t p0 = (int64_t)p.length - p.n + first / a.group, p1 = (int64_t)p.length - p.n + last / a.group;
     int64_t lo = a.window ? max(p0 - (int64_t)a.window + 1, (int64_t)0) : 0;
     int64_t hi = a.causal ? min(p1 + 1, (int64_t)p.seen) : (int64_t)p.seen;
     lo &= ~(int64_t)127;             // (a whole tile's, and a block's)
-    const int64_t begin = lo + (int64_t)p.split * a.chunk;
-    if (p.split + 1 < a.splits) hi = min(hi, begin + a.chunk);
+    uint32_t chunk = a.chunk;
+    if constexpr (EVEN)
+        if (a.splits > 1) chunk = max((((uint32_t)max(hi - lo, (int64_t)0) + a.splits - 1) / a.splits + 127u) & ~127u, a.least);
+    const int64_t begin = lo + (int64_t)p.split * chunk;
+    if (p.split + 1 < a.splits) hi = min(hi, begin + chunk);
     Reach w;
     w.begin = (uint32_t)min(begin, (int64_t)0x7FFFFFC0);
     w.end = hi > begin ? (uint32_t)hi : w.begin;

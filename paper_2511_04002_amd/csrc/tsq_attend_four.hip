@@ -88,7 +88,7 @@ __device__ __forceinline__ bool attend_four_few(const AttendArgs &a, FewShared &
     const uint8_t *all_ks = static_cast<const uint8_t *>(a.k_scale), *all_vs = static_cast<const uint8_t *>(a.v_scale);
     for (uint32_t tile = p.tile;; ++tile) {
         const uint32_t rows = p.n * a.group;
-        const Reach reach = reach_of<ROWS>(a, p, tile);
+        const Reach reach = reach_of<ROWS, true>(a, p, tile);
         const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
         if (a.splits > 1 && reach.begin >= reach.end) {
             nothing_seen<ROWS>(a, p, tile, D);
@@ -366,7 +366,7 @@ __device__ __attribute__((noinline)) void attend_four_few_again(KernelArgs args,
 }
 
 template <int D, bool BF16, int SETS, bool ONCE>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_four_few(AttendArgs a) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && SETS == 1 ? 3 : 2) void k_attend_four_few(AttendArgs a) {
     __shared__ FewShared shared;
     if (__builtin_amdgcn_readfirstlane((int)attend_four_few<D, BF16, SETS, ONCE, false>(a, shared))) {
         __syncthreads();
@@ -625,7 +625,7 @@ __device__ __forceinline__ void attend_four_tiles(const AttendArgs &a, FourTile<
     if (!find_place<ROWS>(a, p)) return;
     for (uint32_t tile = p.tile;; ++tile) {
         const uint32_t rows = p.n * a.group;
-        const Reach reach = reach_of<ROWS>(a, p, tile);
+        const Reach reach = reach_of<ROWS, true>(a, p, tile);
         const bool done = !p.last || (uint64_t)(tile + 1) * ROWS >= rows;
         if (a.splits > 1 && reach.begin >= reach.end) nothing_seen<ROWS>(a, p, tile, D);
         else attend_four_tile<D, BF16, WAVES, TOKENS, SPLIT>(a, p, tile, reach, buffer, outside);
@@ -642,7 +642,7 @@ __device__ __attribute__((noinline)) void attend_four_many_again(KernelArgs args
 }
 
 template <int D, bool BF16, int WAVES, int TOKENS>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_four_many(AttendArgs a) {
+__global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_four_many(AttendArgs a) {
     __shared__ FourTile<D, TOKENS> buffer[2];
     __shared__ uint32_t outside;     // (some value is one that halves do not hold)
     if constexpr (BF16) {
@@ -674,7 +674,7 @@ void launch_attend_four(const CacheShape &s, uint32_t rows, bool once, uint32_t 
         };
         if (rows == 16) few(std::integral_constant<int, 1>{});
         else if (rows == 32) { if constexpr (d() != 256) few(std::integral_constant<int, 2>{}); }
-        else if (rows == 128) k_attend_four_many<d(), bf16(), 4, d() == 256 ? 32 : 64><<<grid, 256, 0, st>>>(a);
+        else if (rows == 128) k_attend_four_many<d(), bf16(), 4, 64><<<grid, 256, 0, st>>>(a);
         else if constexpr (d() != 256) k_attend_four_many<d(), bf16(), 8, 128><<<grid, 512, 0, st>>>(a);
     });
 }

@@ -80,7 +80,9 @@ struct AttendArgs {
     uint32_t requests, tokens, q_heads, kv_heads, group, blocks, block_log2, max_blocks;
     uint32_t tiles, tiles_each;  // row tiles of the call; of each request, or 0: they follow one another (see find_place)
     uint32_t splits, chunk;      // pieces of a tile's reach along the cache, and the tokens of a piece (a multiple of 128)
-    uint32_t by_length;          // the requests' workgroups in the order of their lengths, the longest first (2 .. 64 requests)
+    uint32_t least;              // ... the least, where a tile's pieces are alike (a multiple of 128; of a cache in 4 bits)
+    uint32_t by_length;          // the requests' workgroups in the order of their lengths, the longest first (2 .. 64 requests); n + 1: n
+                                 // of them, and then the shortest first
     uint32_t by_tile;            // the requests' first tiles before their second ones
     uint32_t rows_from, rows_to; // a launch is for the requests with so many rows of a kv head: rows_from <= rows <= rows_to
     uint32_t window;
@@ -117,7 +119,7 @@ int launch_gather_four(const CacheShape &s, const GatherArgs &a, void *stream);
 // How an attend call is split: by the shape and the caller's numbers alone, so that the workspace's size and the
 // launch agree.
 struct AttendLaunch {
-    uint32_t rows, tiles, tiles_each, splits, chunk, by_length;
+    uint32_t rows, tiles, tiles_each, splits, chunk, by_length;     // (by_length: as in AttendArgs)
     uint64_t part_rows;
     // a second launch, for the requests of few rows among those of many, with pieces of its own
     uint32_t few_tiles;          // 0: there is none
