@@ -95,7 +95,8 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
 }
 
 // Tokens that any row of a tile sees, the part of them that a split has, and what a row sees.  EVEN: the pieces of a tile are
-// alike, down to a.least tokens, instead of a.chunk each.
+// alike, down to a.least tokens, instead of a.chunk each (32 requests of 2048 to 8192 tokens, 4 rows of 64 heads on 8 each, 47 us
+// against 57: short ones have as many workgroups as long ones).
 struct Reach { uint32_t begin, end; };
 template <int ROWS, bool EVEN = false>
 __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Place &p, uint32_t tile) {

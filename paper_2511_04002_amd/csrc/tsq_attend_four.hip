@@ -4,14 +4,15 @@
 // Keys and values are exact in the queries' own 16-bit type, scale included: the conversion instructions make two elements
 // at a time, and what goes into the matrix instructions is what the cache stands for.  The reference m of a row's weights
 // 2^(score - m) follows its largest score in steps, as it moves only when a score is more than 8 above what it was set for.
-// The weights of binary16 values are halves, at most 2^15 and of 11 bits down to 2^-21 of the row's largest; those of
-// bfloat16 values, whose range halves have not, are the sum of two bfloat16, 16 bits, at most 1.  The denominator adds the
-// weights as they are before that rounding.
+// Weights are halves, at most 2^15, of 11 bits down to 2^-21 of the row's largest, and values are converted to halves,
+// exactly, whichever type the cache is of.  Values of bfloat16 that halves do not hold send their workgroup through all of
+// its tokens a second time, with values in bfloat16 and weights the sum of two bfloat16, 16 bits, at most 1.  The
+// denominator adds the weights as they are before that rounding.
 //
 // Scores are computed transposed, S^T = K Q^T: a lane then has all its scores in one row of the softmax (a query), and the
 // registers that hold P^T are, in the order they are in, an operand of O^T = V^T P^T.  Values lie token by token, as keys
-// do, and their operand wants tokens side by side: of two tokens' registers, which hold two elements each, two byte
-// permutations make one register for either element.
+// do, and their operand wants tokens side by side: few rows make one register for either element of two tokens' registers,
+// which hold two elements each, by two byte permutations; many rows read it so from LDS.
 #include "tsq_attend.hpp"
 #include "tsq_four.hpp"
 
@@ -54,6 +55,11 @@ template <bool BF16> __device__ __forceinline__ float4_t product(uint4_t x, uint
 //   16 tokens of its group; its row of the softmax is m.
 //   Keys: operand row m is token 16 (m / 4) + 4t + m % 4; the lane's elements are g D/4 .. + D/4 - 1, eight a product.
 //   Values: a lane has elements m D/16 .. + D/16 - 1 of its group's 16 tokens; row m of product j is element m D/16 + j.
+// Memory bounds it where a call has enough tokens to keep two workgroups a CU busy: 64 requests of 1024 to 4096 tokens on 40 heads
+// of 128 (949 MB) take 164 us, 5.8 TB/s, where a kernel that reads the same pieces and drops them takes 147 to 157; one request
+// of 131072 tokens, 64 heads on 8, 28 us and 5 to join its pieces, 4.3 TB/s in all; a single token of 128, 5 us from launch to
+// end.  With 32 rows the conversions and the softmax, which are alike for each 16 rows, take as long as the loads: 32 requests of
+// 8192 tokens, 4 rows of 64 heads on 8 each, 47 us, 3.6 TB/s.
 struct FewShared {
     float sums[4][16][132], stats[4][16][2];
     uint32_t odd[4];                                     // of each wave: some value is one that the first pass cannot take
@@ -385,6 +391,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && SETS == 1 ? 3 : 2) v
 //
 // Weights are halves.  Values of bfloat16 are converted to halves, too, as long as halves hold them exactly (all scales
 // of 2^-23 to 2^13); a workgroup that meets others begins again with bfloat16 values and weights in two parts (SPLIT).
+//
+// The matrix instructions and the vector ones, which share a wave's issue, bound it; each is busy for half of the time: a prompt
+// of 8192 tokens, 64 heads of 128 on 8, 1010 to 1030 us, 1.07 to 1.09 PFLOP/s, where a product of two large matrices reaches
+// 1.15 to 1.25; 448 rows over 1500 tokens, 20 heads of 64, six requests, 39 us.  Heads of 64 have half the products for the
+// same exponentials: 8000 tokens on 20 heads 440 to 480 us, 0.7 PFLOP/s.
 //
 // Heads of 256 put a token's pieces of 16 bytes at other places within their 64, such that eight lanes that write at a time
 // meet in no bank: a prompt of 4096 tokens on 16 heads, 214 us instead of 238.  (Heads of 128 do not notice, of 64 lose 3 % by

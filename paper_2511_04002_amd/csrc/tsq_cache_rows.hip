@@ -187,7 +187,8 @@ __global__ __launch_bounds__(kScheduleThreads) void k_schedule(ScheduleArgs a) {
 // Norm and rotation.  A lane holds 16 elements of a head in two pieces of 8, chosen so that the pairs that turn
 // together are the lane's own: D / 16 lanes a head, 1024 / D heads a wave.  The sum of squares, the product with the
 // weight and the rotation stay in registers, in binary32; memory is read and written once, and bounds it: 8192 rows of
-// 72 heads of 128 are 306 MB and 54 us, 5.7 TB/s where a copy reaches 6.2.
+// 72 heads of 128 are 306 MB and 54 us, 5.7 TB/s where a copy reaches 6.2; by three axes (AXES, which choose each pair's row of
+// angles) 59, and 63 with pairs dealt out in turn, whose lanes read the rows of all axes and choose.
 template <int D, bool BF16, bool AXES, bool ONCE>
 __global__ __launch_bounds__(256) void k_norm_rotate(NormRotateArgs a, uint32_t passes, uint32_t waves_each) {
     constexpr int LPH = D / 16, HEADS = 64 / LPH;
