@@ -539,6 +539,23 @@ def test_attend_of_many_heads_and_lengths_in_more_workgroups_than_run_at_once(re
         assert (np.abs(got[:, h:h + 1] - want) <= bound).all(), h
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("requests,heads,longest", [(40, (8, 8, 128), 90), (64, (8, 8, 64), 70), (5, (128, 64, 64), 70), (20, (16, 8, 128), 1500),
+                                                    (32, (64, 8, 128), 700), (3, (24, 24, 64), 1300)])
+def test_attend_where_long_and_short_requests_share_a_compute_unit(dtype, requests, heads, longest):
+    """More than 256 workgroups and no more than 512: they go by the requests' lengths, the second half from the shortest on."""
+    hq, hk, dim = heads
+    b = Both(requests * -(-longest // 16) + 1, 16, hk, dim, dtype, -(-longest // 16), requests, q_heads=hq)
+    lengths = b.g.integers(0, longest + 1, requests)
+    lengths[0] = lengths[requests // 2] = longest
+    counts = np.minimum(b.g.integers(0, 3, requests), lengths)
+    attend_both(b, hq, counts, lengths)
+    attend_both(b, hq, np.ones(requests, int), np.full(requests, longest))
+    lengths[-1] = longest + 40                               # past the table
+    table = b.g.integers(0, len(b.k), (requests, b.max_blocks)).astype(np.int32)
+    attend_both(b, hq, counts, lengths, window=50, table=table)
+
+
 @pytest.mark.parametrize("heads", [(2, 2, 64), (8, 1, 128), (4, 1, 256)])
 def test_attend_one_request_far_longer_than_the_others(heads):
     hq, hk, dim = heads
@@ -756,6 +773,49 @@ def test_a_step_in_a_graph_replayed_with_other_data_between():
         assert torch.equal(captured.y, eager.y) and torch.equal(captured.lengths, eager.lengths) and torch.equal(captured.table, eager.table), i
         assert captured.y.isfinite().all()
     assert int(captured.lengths[0]) == start + 40
+
+
+@pytest.mark.parametrize("dtype,heads", [("f16", (8, 1, 128)), ("bf16", (8, 1, 128)), ("bf16", (4, 2, 64)), ("bf16", (2, 1, 256))])
+def test_calls_at_once_on_two_streams_and_graphs_that_share_a_workspace(dtype, heads):
+    """Each of two memories needs the second pass somewhere, and each call is in pieces; the graphs' calls follow one another."""
+    hq, hk, dim = heads
+    sides = []
+    for seed in (1, 2):
+        b = Both(200, 16, hk, dim, dtype, 190, seed, q_heads=hq)
+        b.vs[seed::7, 0, 0, 3] = 127 - 22
+        b.wrap()
+        table = dev(np.stack([b.g.permutation(200)[:190], b.g.permutation(200)[:190]]).astype(np.int32))
+        for counts, lengths in (((1, 1), (3000, 2900)), ((40, 30), (3000, 1700))):
+            starts = dev(np.array([0, counts[0], sum(counts)], np.int32))
+            q, ws = rows(b.g, sum(counts), hq, dim, dtype), b.c.new_workspace(2, sum(counts), max(counts), 3000)
+            assert ws is not None
+            call = (b.m, q, table, starts, dev(np.array(lengths, np.int32)), max(counts), 3000)
+            sides.append((b, call, ws, b.c.attend(*call, out=torch.empty_like(q), ws=ws)))
+    for one, two in ((sides[0], sides[2]), (sides[1], sides[3]), (sides[0], sides[3])):
+        torch.cuda.synchronize()
+        streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.full_like(x[3], 7.0) for x in (one, two)]
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for (b, call, ws, _), stream, out in zip((one, two), streams, outs):
+                with torch.cuda.stream(stream):
+                    b.c.attend(*call, out=out, ws=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], one[3]) and torch.equal(outs[1], two[3])
+    shared = max((x[2] for x in sides), key=lambda ws: ws.numel())
+    graphs, outs = [], [torch.full_like(x[3], 7.0) for x in sides]
+    for (b, call, _, _), out in zip(sides, outs):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            b.c.attend(*call, out=out, ws=shared)
+        graphs.append(graph)
+    for _ in range(3):
+        for out in outs:
+            out.fill_(7.0)
+        for graph in graphs + graphs[::-1]:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (_, _, _, want), out in zip(sides, outs):
+            assert torch.equal(out, want)
 
 
 def test_calls_of_no_tokens_do_nothing():
