@@ -495,15 +495,16 @@ __device__ __forceinline__ void attend_four_tile(const AttendArgs &a, const Plac
             asked[i] = entry[i];
         }
     };
-    auto put = [&](Tile &t) {
+    auto put = [&](Tile &t, uint32_t t0) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uint32_t e = i * THREADS + tid, token = e / PT, at = e % PT * E;
             const float k_scale = four_scale(is_bad(a, p, asked[i]) ? kNotANumber : ks[i]);
             // (no value may bring NaN or infinity into a sum with a weight of 0: see k_attend_four_few)
             typedef FourScales<VALUES_BF16> Held;
+            // (behind the request's end a scale may be anything)
             if constexpr (BF16 && !SPLIT)
-                if (vs[i] < Held::lowest || vs[i] > Held::highest) *outside = 1;
+                if ((vs[i] < Held::lowest || vs[i] > Held::highest) && t0 + token < p.seen) *outside = 1;
             const float v_scale = four_scale(min(vs[i], (uint32_t)Held::highest));
             const uint32_t turn = turned_by<D>(e % PT);
             for (int j = 0; j < E / 8; ++j) {
@@ -516,7 +517,7 @@ __device__ __forceinline__ void attend_four_tile(const AttendArgs &a, const Plac
         ask_entries(reach.begin);
         ask(reach.begin);
         ask_entries(reach.begin + TOKENS);
-        put(buffer[0]);
+        put(buffer[0], reach.begin);
         ask(reach.begin + TOKENS);
         ask_entries(reach.begin + 2 * TOKENS);
         __syncthreads();
@@ -603,7 +604,7 @@ __device__ __forceinline__ void attend_four_tile(const AttendArgs &a, const Plac
                 if constexpr (!SPLIT) loads_among_products<4 * C * D / 32, 2 * C * D / 32, 1>();
                 __builtin_amdgcn_s_setprio(0);
             }
-            if (t0 + TOKENS < reach.end) put(buffer[at ^ 1]);
+            if (t0 + TOKENS < reach.end) put(buffer[at ^ 1], t0 + TOKENS);
             ask(t0 + 2 * TOKENS);
             ask_entries(t0 + 3 * TOKENS);
             __syncthreads();

@@ -370,6 +370,25 @@ def test_attend_ignores_what_lies_behind_a_request_and_in_blocks_of_nobody(dtype
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("counts,dim", [([1, 1, 1], 64), ([3, 1, 2], 128), ([150, 90, 1], 64), ([150, 90, 1], 128), ([60, 70, 1], 256)])
+def test_attend_gives_the_same_bits_whatever_lies_behind_a_request(dtype, counts, dim):
+    """Scales that have never been written do not decide how a request's own values are treated."""
+    outs = []
+    for behind in (127, 0, 255, 104):
+        b = Both(60, 16, 2, dim, dtype, 20, 77, q_heads=8)
+        table = b.g.permutation(60).reshape(3, 20).astype(np.int32)
+        lengths = [301, 90, 5]
+        for r, n in enumerate(lengths):
+            for x in (b.ks, b.vs):
+                x[table[r, n // 16], ..., n % 16:] = behind
+                x[table[r, n // 16 + 1:]] = behind
+        b.wrap()
+        outs.append(attend_both(b, 8, counts, lengths, table=table, max_length=301)[:2])
+    for out, lse in outs[1:]:
+        assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_attend_one_token_that_takes_all_the_weight_and_queries_far_from_one(dtype):
     b = Both(40, 16, 1, 128, dtype, 20, 20, q_heads=3)
     for n in (3, 40):
