@@ -394,8 +394,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && SETS == 1 ? 3 : 2) v
 //
 // The matrix instructions and the vector ones, which share a wave's issue, bound it; each is busy for half of the time: a prompt
 // of 8192 tokens, 64 heads of 128 on 8, 1000 to 1040 us, 1.06 to 1.10 PFLOP/s (840 on zeros, which cost no clock), where a product
-// of two large matrices reaches 1.15 to 1.25; 448 rows over 1500 tokens, 20 heads of 64, six requests, 39 us.  Heads of 64 have
-// half the products for the same exponentials: 8000 tokens on 20 heads 440 to 480 us, 0.7 PFLOP/s.
+// of two large matrices reaches 1.15 to 1.25; 448 rows over 1500 tokens, 20 heads of 64, six requests, 38 us.  Heads of 64 have
+// half the products for the same exponentials: 8000 tokens on 20 heads, twice, 430 to 440 us, 0.75 PFLOP/s.
 //
 // Heads of 256 put a token's pieces of 16 bytes at other places within their 64, such that eight lanes that write at a time
 // meet in no bank: a prompt of 4096 tokens on 16 heads, 214 us instead of 238.  (Heads of 128 do not notice, of 64 lose 3 % by
@@ -456,6 +456,7 @@ __device__ __forceinline__ void attend_four_tile(const AttendArgs &a, const Plac
     }
     uint32_t from, to;
     row_sees(a, p, row, from, to);
+    if (tile * ROWS + wave * 32 >= rows) to = 0;         // (a wave without rows only helps to stage)
 
     float16_t acc[D / 32];
 #pragma unroll
