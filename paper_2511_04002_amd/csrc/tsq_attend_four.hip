@@ -407,16 +407,17 @@ struct FourTile {
 };
 template <int D> __device__ constexpr uint32_t turned_by(uint32_t part) { return D == 256 ? part >> 1 & 3 : 0; }
 
-// How a block's LOADS loads from LDS and PRODUCTS products are to be issued: a few loads, then the others behind the products.
-template <int LOADS, int PRODUCTS, int GROUP> __device__ __forceinline__ void loads_among_products() {
-    constexpr int kLoad = 0x100, kProduct = 0x8, EACH = LOADS / PRODUCTS;
-    __builtin_amdgcn_sched_group_barrier(kLoad, 4 * EACH, GROUP);
+// How a block's LOADS loads from LDS and PRODUCTS products are to be issued: the loads of some products, then the others behind the products.
+// (Two for heads of 256, which have few registers left: a prompt of 4096 194 us, with four 206, with one 228; the others do not notice.)
+template <int D, int LOADS, int PRODUCTS, int GROUP> __device__ __forceinline__ void loads_among_products() {
+    constexpr int kLoad = 0x100, kProduct = 0x8, EACH = LOADS / PRODUCTS, AHEAD = D == 256 ? 2 : 4;
+    __builtin_amdgcn_sched_group_barrier(kLoad, AHEAD * EACH, GROUP);
 #pragma unroll
-    for (int i = 0; i < PRODUCTS - 4; ++i) {
+    for (int i = 0; i < PRODUCTS - AHEAD; ++i) {
         __builtin_amdgcn_sched_group_barrier(kProduct, 1, GROUP);
         __builtin_amdgcn_sched_group_barrier(kLoad, EACH, GROUP);
     }
-    __builtin_amdgcn_sched_group_barrier(kProduct, 4, GROUP);
+    __builtin_amdgcn_sched_group_barrier(kProduct, AHEAD, GROUP);
 }
 
 // Products of 32 x 32 x 16.
@@ -552,7 +553,7 @@ __device__ __forceinline__ void attend_four_tile(const AttendArgs &a, const Plac
                         s[c] = wide_product<BF16>(*reinterpret_cast<const uint4_t *>(at), q[e], s[c]);
                     }
                 }
-                loads_among_products<C * D / 16, C * D / 16, 0>();
+                loads_among_products<D, C * D / 16, C * D / 16, 0>();
                 ahead<D>(false);
                 const bool whole = __ballot(u0 < from || u0 + SUB > to) == 0;
                 if (!whole) {
@@ -611,7 +612,7 @@ __device__ __forceinline__ void attend_four_tile(const AttendArgs &a, const Plac
                         acc[d] = wide_product<VALUES_BF16>(v, pw[u], acc[d]);
                         if constexpr (SPLIT) acc[d] = wide_product<true>(v, rest[u], acc[d]);
                     }
-                if constexpr (!SPLIT) loads_among_products<4 * C * D / 32, 2 * C * D / 32, 1>();
+                if constexpr (!SPLIT) loads_among_products<D, 4 * C * D / 32, 2 * C * D / 32, 1>();
                 ahead<D>(false);
             }
             if (t0 + TOKENS < reach.end) put(buffer[at ^ 1], t0 + TOKENS);
