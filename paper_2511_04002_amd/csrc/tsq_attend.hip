@@ -837,7 +837,7 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
     // Attention over 4 bits runs two workgroups of few rows a CU, i and i + 256: where that is all there are, a CU's second one
     // goes by length from the other end, the shortest with the longest (64 requests of 1024 to 4096 tokens, 64 heads on 8: 40 us,
     // in the order given 44).
-    if (s.bits == 4 && s.head_dim != 256 && l.rows <= 32 && l.tiles_each == 1 && requests > 1 && requests <= 64 && units * l.splits > 256 && units * l.splits <= 512) {
+    if (s.bits == 4 && l.rows <= 32 && l.tiles_each == 1 && requests > 1 && requests <= 64 && units * l.splits > 256 && units * l.splits <= 512) {
         const uint32_t turn = (uint32_t)(256 / (s.kv_heads * l.splits));
         if (turn >= 1 && turn < requests) l.by_length = turn + 1;
     }

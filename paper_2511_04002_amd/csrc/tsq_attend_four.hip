@@ -371,8 +371,10 @@ __device__ __attribute__((noinline)) void attend_four_few_again(KernelArgs args,
     attend_four_few<D, BF16, SETS, false, true>(args_of(args), *(FewShared *)shared);
 }
 
+// (Two waves a SIMD, whose registers a second set would not fit with heads of 256; three with heads of 64.  64 requests of 1024 to 4096
+// tokens: 16 heads on 8 of 256 77.7 us and 86.0 with one wave, 12 of 64 38.7 and 45.5 with two; heads of 128 lose by a third.)
 template <int D, bool BF16, int SETS, bool ONCE>
-__global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && SETS == 1 ? 3 : 2) void k_attend_four_few(AttendArgs a) {
+__global__ __launch_bounds__(256, D == 64 && SETS == 1 ? 3 : 2) void k_attend_four_few(AttendArgs a) {
     __shared__ FewShared shared;
     if (__builtin_amdgcn_readfirstlane((int)attend_four_few<D, BF16, SETS, ONCE, false>(a, shared))) {
         __syncthreads();
@@ -699,10 +701,10 @@ void launch_attend_four(const CacheShape &s, uint32_t rows, bool once, uint32_t 
     const hipStream_t st = static_cast<hipStream_t>(stream);
     by_shape(s, [&](auto d, auto bf16) {
         auto few = [&](auto sets) {
-            // Streaming loads, of heads of 128 alone, whose pieces are whole halves of lines, and where a request has one tile: 64
-            // requests of 1024 to 4096 tokens on 40 heads 166 us against 180; but heads of 64 55 against 39, of 256 88 against 85,
-            // and two tiles of 16 requests of 4096 on 8 heads, which read the cache twice, 43 against 39.
-            if constexpr (d() == 128) {
+            // Streaming loads, not of heads of 64, whose pieces are less than half a line, and where a request has one tile: 64
+            // requests of 1024 to 4096 tokens on 40 heads of 128 166 us against 180, on 8 of 256 73.7 against 77.5; but heads of 64
+            // 55 against 39, and two tiles of 16 requests of 4096 on 8 heads, which read the cache twice, 43 against 39.
+            if constexpr (d() != 64) {
                 if (once) { k_attend_four_few<d(), bf16(), sets(), true><<<grid, 256, 0, st>>>(a); return; }
             }
             k_attend_four_few<d(), bf16(), sets(), false><<<grid, 256, 0, st>>>(a);
