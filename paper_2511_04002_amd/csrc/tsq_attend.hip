@@ -834,10 +834,10 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
     // little more than one round the ranking costs more than it brings: 20 requests of 250 to 1000 tokens on 32 heads 29
     // against 25).  A wave ranks 64 requests.
     l.by_length = l.tiles_each && requests > 1 && requests <= 64 && units * l.splits >= 4 * slots;
-    // Attention over 4 bits runs two workgroups of few rows a CU, i and i + 256: where that is all there are, a CU's second one
-    // goes by length from the other end, the shortest with the longest (64 requests of 1024 to 4096 tokens, 64 heads on 8: 40 us,
-    // in the order given 44).
-    if (s.bits == 4 && l.rows <= 32 && l.tiles_each == 1 && requests > 1 && requests <= 64 && units * l.splits > 256 && units * l.splits <= 512) {
+    // Attention over 4 bits runs two workgroups of few rows a CU (three with heads of 64), i and i + 256: where that is all there
+    // are, those after the first 256 go by length from the other end, the shortest with the longest (64 requests of 1024 to 4096
+    // tokens, 64 heads on 8: 40 us, in the order given 44; 32 of them, 20 heads of 64, three a CU: 30.5 and 35.8).
+    if (s.bits == 4 && l.rows <= 32 && l.tiles_each == 1 && requests > 1 && requests <= 64 && units * l.splits > 256 && units * l.splits <= std::max<uint64_t>(slots, 512)) {
         const uint32_t turn = (uint32_t)(256 / (s.kv_heads * l.splits));
         if (turn >= 1 && turn < requests) l.by_length = turn + 1;
     }

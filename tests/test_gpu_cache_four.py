@@ -560,9 +560,9 @@ def test_attend_of_many_heads_and_lengths_in_more_workgroups_than_run_at_once(re
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("requests,heads,longest", [(40, (8, 8, 128), 90), (64, (8, 8, 64), 70), (5, (128, 64, 64), 70), (20, (16, 8, 128), 1500),
-                                                    (32, (64, 8, 128), 700), (3, (24, 24, 64), 1300)])
+                                                    (32, (64, 8, 128), 700), (3, (24, 24, 64), 1300), (40, (16, 16, 64), 80), (33, (8, 8, 256), 60)])
 def test_attend_where_long_and_short_requests_share_a_compute_unit(dtype, requests, heads, longest):
-    """More than 256 workgroups and no more than 512: they go by the requests' lengths, the second half from the shortest on."""
+    """More than 256 workgroups, and no more than run at once: they go by the requests' lengths, those after 256 from the shortest on."""
     hq, hk, dim = heads
     b = Both(requests * -(-longest // 16) + 1, 16, hk, dim, dtype, -(-longest // 16), requests, q_heads=hq)
     lengths = b.g.integers(0, longest + 1, requests)
