@@ -834,12 +834,18 @@ AttendLaunch attend_launch(const CacheShape &s, uint32_t requests, uint32_t toke
     // little more than one round the ranking costs more than it brings: 20 requests of 250 to 1000 tokens on 32 heads 29
     // against 25).  A wave ranks 64 requests.
     l.by_length = l.tiles_each && requests > 1 && requests <= 64 && units * l.splits >= 4 * slots;
-    // Attention over 4 bits runs two workgroups of few rows a CU (three with heads of 64), i and i + 256: where that is all there
-    // are, those after the first 256 go by length from the other end, the shortest with the longest (64 requests of 1024 to 4096
-    // tokens, 64 heads on 8: 40 us, in the order given 44; 32 of them, 20 heads of 64, three a CU: 30.5 and 35.8).
-    if (s.bits == 4 && l.rows <= 32 && l.tiles_each == 1 && requests > 1 && requests <= 64 && units * l.splits > 256 && units * l.splits <= std::max<uint64_t>(slots, 512)) {
+    // Workgroups of few rows over 4 bits are done sooner, and the ranking, a microsecond of each, pays from 1024 tokens on, of 16
+    // rows.  Two of them run on a CU at once (three with heads of 64), i and i + 256.  Where that is all there are, those after
+    // the first 256 go by length from the other end, the shortest with the longest (64 requests of 1024 to 4096 tokens, 64 heads
+    // on 8: 40 us, in the order given 44; of 500 to 2000 24.3 and 26.6, of 250 to 1000 17.1 and 16.9, of 125 to 500 13.5 and
+    // 12.3); where there are more, all go from the longest on (32 requests of 1024 to 4096, 32 heads: 64.4 us, in the order given
+    // 70.3; 40 of 375 to 1500 41.5 and 42.9; 60 of 250 to 1000 48.7 and 45.0).
+    if (s.bits == 4 && l.rows <= 32 && l.tiles_each == 1 && requests > 1 && requests <= 64) {
+        const bool pays = reach * l.rows > 16 * 1024;
+        const uint64_t groups = units * l.splits, at_once = std::max<uint64_t>(slots, 512);
         const uint32_t turn = (uint32_t)(256 / (s.kv_heads * l.splits));
-        if (turn >= 1 && turn < requests) l.by_length = turn + 1;
+        l.by_length = pays && groups > at_once ? 1 : 0;
+        if (pays && groups > 256 && groups <= at_once && turn >= 1 && turn < requests) l.by_length = turn + 1;
     }
     return l;
 }

@@ -51,10 +51,13 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
         if (a.by_length) {
             // the longest request first: p.r counts from the shortest here; each lane ranks one request
             const uint32_t lane = threadIdx.x & 63;
-            // (its length and number in one word: they all differ, and lengths past 2^26 may change places)
-            const uint32_t mine = min((uint32_t)max(lane < a.requests ? a.lengths[lane] : 0, 0), (1u << 26) - 1) << 6 | lane;
+            // (its length and number in one word: they all differ, and lengths past 2^25 may change places)
+            // (lanes without a request are above all)
+            const uint32_t mine = lane < a.requests ? min((uint32_t)max(a.lengths[lane], 0), (1u << 25) - 1) << 6 | lane : ~0u;
             uint32_t below = 0;
-            for (uint32_t j = 0; j < a.requests; ++j) below += (uint32_t)__builtin_amdgcn_readlane((int)mine, (int)j) < mine ? 1 : 0;
+            for (uint32_t j = 0; j < a.requests; j += 8)
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) below += (uint32_t)__builtin_amdgcn_readlane((int)mine, (int)(j + i)) < mine ? 1 : 0;
             // (or, where all of two rounds run at once, the second round's from the shortest on: a CU has one of each)
             if (a.by_length > 1) {
                 const uint32_t turn = a.by_length - 1, nth = a.requests - 1 - p.r;

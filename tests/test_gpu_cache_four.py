@@ -568,10 +568,12 @@ def test_attend_where_long_and_short_requests_share_a_compute_unit(dtype, reques
     lengths = b.g.integers(0, longest + 1, requests)
     lengths[0] = lengths[requests // 2] = longest
     counts = np.minimum(b.g.integers(0, 3, requests), lengths)
+    attend_both(b, hq, counts, lengths, max_length=3000)         # (requests that may be short go in the order given)
     attend_both(b, hq, counts, lengths)
-    attend_both(b, hq, np.ones(requests, int), np.full(requests, longest))
+    attend_both(b, hq, np.ones(requests, int), np.full(requests, longest), max_length=1500)
     lengths[-1] = longest + 40                               # past the table
     table = b.g.integers(0, len(b.k), (requests, b.max_blocks)).astype(np.int32)
+    attend_both(b, hq, counts, lengths, table=table, max_length=2000)
     attend_both(b, hq, counts, lengths, window=50, table=table)
 
 
