@@ -56,10 +56,10 @@ template <bool BF16> __device__ __forceinline__ float4_t product(uint4_t x, uint
 //   Keys: operand row m is token 16 (m / 4) + 4t + m % 4; the lane's elements are g D/4 .. + D/4 - 1, eight a product.
 //   Values: a lane has elements m D/16 .. + D/16 - 1 of its group's 16 tokens; row m of product j is element m D/16 + j.
 // Memory bounds it where a call has enough tokens to keep two workgroups a CU busy: 64 requests of 1024 to 4096 tokens on 40 heads
-// of 128 (949 MB) take 164 us, 5.8 TB/s, where a kernel that reads the same pieces and drops them takes 147 to 157; one request
+// of 128 (949 MB) take 160 us, 5.9 TB/s, where a kernel that reads the same pieces and drops them takes 147 to 157; one request
 // of 131072 tokens, 64 heads on 8, 28 us and 5 to join its pieces, 4.3 TB/s in all; a single token of 128, 5 us from launch to
-// end.  With 32 rows the conversions and the softmax, which are alike for each 16 rows, take as long as the loads: 32 requests of
-// 8192 tokens, 4 rows of 64 heads on 8 each, 47 us, 3.6 TB/s.
+// end.  With 32 rows the conversions and the softmax, which is made for each 16 rows, take as long as the loads: 32 requests of
+// 2400 to 8200 tokens, up to 4 queries of 64 heads on 8 each, 46 us, 3.7 TB/s.
 struct FewShared {
     float sums[4][16][132], stats[4][16][2];
     uint32_t odd[4];                                     // of each wave: some value is one that the first pass cannot take
