@@ -100,20 +100,22 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
 // Tokens that any row of a tile sees, the part of them that a split has, and what a row sees.  EVEN: the pieces of a tile are
 // alike, down to a.least tokens, instead of a.chunk each (32 requests of 2048 to 8192 tokens, 4 rows of 64 heads on 8 each, 47 us
 // against 57: short ones have as many workgroups as long ones).
-struct Reach { uint32_t begin, end; };
+// (begin is a whole tile's; first: the first token that some row sees, up to 127 behind it)
+struct Reach { uint32_t begin, end, first; };
 template <int ROWS, bool EVEN = false>
 __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Place &p, uint32_t tile) {
     const int64_t rows = (int64_t)p.n * a.group, first = (int64_t)tile * ROWS, last = min(first + ROWS, rows) - 1;
     const int64_t p0 = (int64_t)p.length - p.n + first / a.group, p1 = (int64_t)p.length - p.n + last / a.group;
     int64_t lo = a.window ? max(p0 - (int64_t)a.window + 1, (int64_t)0) : 0;
     int64_t hi = a.causal ? min(p1 + 1, (int64_t)p.seen) : (int64_t)p.seen;
+    Reach w;
+    w.first = (uint32_t)lo;
     lo &= ~(int64_t)127;             // (a whole tile's, and a block's)
     uint32_t chunk = a.chunk;
     if constexpr (EVEN)
         if (a.splits > 1) chunk = max((((uint32_t)max(hi - lo, (int64_t)0) + a.splits - 1) / a.splits + 127u) & ~127u, a.least);
     const int64_t begin = lo + (int64_t)p.split * chunk;
     if (p.split + 1 < a.splits) hi = min(hi, begin + chunk);
-    Reach w;
     w.begin = (uint32_t)min(begin, (int64_t)0x7FFFFFC0);
     w.end = hi > begin ? (uint32_t)hi : w.begin;
     return w;

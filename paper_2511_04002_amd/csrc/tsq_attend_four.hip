@@ -188,7 +188,8 @@ __device__ __forceinline__ bool attend_four_few(const AttendArgs &a, FewShared &
                         for (int c = 0; c < SETS; ++c) s[c][t] = product<BF16>(k, q[c][j], s[c][t]);
                     }
                 }
-                const float all_factor = bad ? __builtin_nanf("") : a.scale_log2;
+                const bool lost = bad;
+                const float all_factor = lost ? __builtin_nanf("") : a.scale_log2;
                 // (the entry is used up before the next one is asked for: a copy of it would wait for that)
                 const uint32_t mine = t0 + 16 * g, id = id_of(a, next);
                 bad = is_bad(a, p, next);
@@ -237,12 +238,13 @@ __device__ __forceinline__ bool attend_four_few(const AttendArgs &a, FewShared &
                     weight[c] += sum;
                 }
                 // No value that is not seen may bring NaN or infinity into a sum with a weight of 0.  (A token whose values are NaN
-                // has keys that are NaN, too.)  Behind the request's end a scale may be anything.
-                if (t0 + 64 > p.seen) {
-                    const int behind = (int)(p.seen - mine);
+                // has keys that are NaN, too.)  Scales of tokens that no row of the tile sees, and of tokens in no block, may be
+                // anything, and decide nothing.
+                if (t0 + 64 > reach.end || t0 < reach.first || __ballot(lost)) {
+                    const int first = lost ? 16 : (int)(reach.first - mine), behind = (int)(reach.end - mine);
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        if (e >= behind) vs[e / 4] = (vs[e / 4] & ~(0xFFu << 8 * (e & 3))) | 127u << 8 * (e & 3);
+                        if (e < first || e >= behind) vs[e / 4] = (vs[e / 4] & ~(0xFFu << 8 * (e & 3))) | 127u << 8 * (e & 3);
                 }
                 if constexpr (!CAREFUL) odd |= odd_scales(vs);
 #pragma unroll
@@ -508,16 +510,17 @@ __device__ __forceinline__ void attend_four_tile(const AttendArgs &a, const Plac
             asked[i] = entry[i];
         }
     };
-    auto put = [&](Tile &t, uint32_t t0) {
+    auto put = [&](Tile &t, uint32_t t0, uint32_t first) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uint32_t e = i * THREADS + tid, token = e / PT, at = e % PT * E;
-            const float k_scale = four_scale(is_bad(a, p, asked[i]) ? kNotANumber : ks[i]);
+            const bool lost = is_bad(a, p, asked[i]);
+            const float k_scale = four_scale(lost ? kNotANumber : ks[i]);
             // (no value may bring NaN or infinity into a sum with a weight of 0: see k_attend_four_few)
             typedef FourScales<VALUES_BF16> Held;
-            // (behind the request's end a scale may be anything)
+            // (scales of tokens that no row of the tile sees, and of tokens in no block, may be anything, and decide nothing)
             if constexpr (BF16 && !SPLIT)
-                if ((vs[i] < Held::lowest || vs[i] > Held::highest) && t0 + token < p.seen) *outside = 1;
+                if ((vs[i] < Held::lowest || vs[i] > Held::highest) && t0 + token >= first && t0 + token < reach.end && !lost) *outside = 1;
             const float v_scale = four_scale(min(vs[i], (uint32_t)Held::highest));
             const uint32_t turn = turned_by<D>(e % PT);
             for (int j = 0; j < E / 8; ++j) {
@@ -527,14 +530,16 @@ __device__ __forceinline__ void attend_four_tile(const AttendArgs &a, const Plac
         }
     };
     if (reach.begin < reach.end) {
-        ask_entries(reach.begin);
-        ask(reach.begin);
-        ask_entries(reach.begin + TOKENS);
-        put(buffer[0], reach.begin);
-        ask(reach.begin + TOKENS);
-        ask_entries(reach.begin + 2 * TOKENS);
-        __syncthreads();
         uint32_t at = 0, t0 = reach.begin;
+        // (the first token that some row sees is one of the first tile's)
+        if (TOKENS < 128 && t0 + TOKENS <= reach.first && t0 + TOKENS < reach.end) t0 += TOKENS;
+        ask_entries(t0);
+        ask(t0);
+        ask_entries(t0 + TOKENS);
+        put(buffer[0], t0, reach.first);
+        ask(t0 + TOKENS);
+        ask_entries(t0 + 2 * TOKENS);
+        __syncthreads();
         do {                         // (not a loop that may be left out: its loads would be waited for along with the queries')
             const Tile &t = buffer[at];
 #pragma unroll SPLIT ? 1 : TOKENS / SUB
@@ -617,7 +622,7 @@ __device__ __forceinline__ void attend_four_tile(const AttendArgs &a, const Plac
                 if constexpr (!SPLIT) loads_among_products<D, 4 * C * D / 32, 2 * C * D / 32, 1>();
                 ahead<D>(false);
             }
-            if (t0 + TOKENS < reach.end) put(buffer[at ^ 1], t0 + TOKENS);
+            if (t0 + TOKENS < reach.end) put(buffer[at ^ 1], t0 + TOKENS, 0);
             ask(t0 + 2 * TOKENS);
             ask_entries(t0 + 3 * TOKENS);
             __syncthreads();

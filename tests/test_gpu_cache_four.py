@@ -388,6 +388,86 @@ def test_attend_gives_the_same_bits_whatever_lies_behind_a_request(dtype, counts
         assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])
 
 
+ANY_SCALE = (127, 0, 255, 104, 112, 140)                 # what a byte of scales may be that nobody has written
+
+
+def bits_of(b, q, table, starts, lengths, *more):
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    return b.c.attend(b.m, q, dev(table), dev(np.asarray(starts, np.int32)), dev(np.asarray(lengths, np.int32)), *more, lse=lse), lse
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("counts", [[1, 1, 1], [6, 1, 2], [1, 90, 1], [40, 90, 2]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("window,block,causal", [(40, 16, True), (100, 128, True), (70, 32, False)])
+def test_attend_gives_the_same_bits_whatever_lies_before_a_window(dtype, counts, dim, window, block, causal):
+    """Blocks that every row's window has left behind may have been given back, and hold what others write to them."""
+    lengths, starts, outs = [301, 290, 5], np.concatenate(([0], np.cumsum(counts))), []
+    for before in ANY_SCALE + ((37, 250) if dtype == "bf16" else ()):
+        for released in (False, True):
+            b = Both(3 * 20 + 1, block, 2, dim, dtype, 20, 78, q_heads=8)
+            table = 1 + b.g.permutation(60).reshape(3, 20).astype(np.int32)
+            q = rows(b.g, sum(counts), 8, dim, dtype)
+            for x in (b.ks, b.vs):
+                x[0] = before
+                for r, n in enumerate(lengths):
+                    first = max(0, n - counts[r] - window + 1)
+                    x[table[r, :first // block]] = before
+                    x[table[r, first // block], ..., :first % block] = before
+            for r, n in enumerate(lengths) if released else ():
+                table[r, :max(0, n - counts[r] - window + 1) // block] = -1 if r else len(b.ks)
+            b.wrap()
+            outs.append(bits_of(b, q, table, starts, lengths, max(counts), 301, None, causal, window))
+    assert outs[0][0].isfinite().all()
+    for out, lse in outs[1:]:
+        assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])
+    b = Both(3 * 20 + 1, block, 2, dim, dtype, 20, 78, q_heads=8)
+    table = 1 + b.g.permutation(60).reshape(3, 20).astype(np.int32)
+    q = rows(b.g, sum(counts), 8, dim, dtype)
+    got = attend_both(b, 8, counts, lengths, causal, window, table=table, q=q, max_length=301)
+    assert torch.equal(got[0], outs[0][0]) and torch.equal(got[1], outs[0][1])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim,heads,queries,tile", [(64, 8, 8, 4), (128, 8, 8, 4), (256, 4, 8, 4), (64, 1, 600, 256), (128, 8, 200, 32), (256, 4, 90, 32)])
+def test_attend_gives_the_same_bits_whatever_only_later_tiles_see(dtype, dim, heads, queries, tile):
+    """`tile`: queries that one workgroup has; the token behind those of the first ones decides nothing for them."""
+    outs = []
+    for later in ANY_SCALE + ((37, 250) if dtype == "bf16" else ()):
+        b = Both(60, 16, 1, dim, dtype, 60, 79, q_heads=heads)
+        table = b.g.permutation(60)[None].astype(np.int32)
+        q = rows(b.g, queries, heads, dim, dtype)
+        past = 21
+        at = past + tile
+        b.ks[table[0, at // 16], ..., at % 16] = b.vs[table[0, at // 16], ..., at % 16] = later
+        b.wrap()
+        outs.append([x[:tile] for x in bits_of(b, q, table, [0, queries], [past + queries], queries, past + queries)])
+    assert outs[0][0].isfinite().all()
+    for out, lse in outs[1:]:
+        assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("queries", [12, 24, 60, 130])
+def test_attend_gives_the_same_bits_whatever_is_read_for_a_block_that_the_table_does_not_hold(dtype, dim, queries):
+    outs = []
+    for other in ANY_SCALE + ((37, 250) if dtype == "bf16" else ()):
+        b = Both(20, 16, 1, dim, dtype, 19, 80, q_heads=2)
+        table = 1 + b.g.permutation(19)[None].astype(np.int32)
+        q = rows(b.g, queries, 2, dim, dtype)
+        b.ks[0] = b.vs[0] = other
+        b.wrap()
+        length = max(queries, 24)
+        hole = (length - queries) // 16 + 1
+        table[0, hole] = -1
+        outs.append(bits_of(b, q, table, [0, queries], [length], queries, length))
+    before = 16 * hole - (length - queries)                  # rows that see nothing of it
+    assert 0 < before < queries and outs[0][0][:before].isfinite().all() and outs[0][0][before:].isnan().all()
+    for out, lse in outs[1:]:
+        assert torch.equal(out[:before], outs[0][0][:before]) and torch.equal(lse[:before], outs[0][1][:before]) and out[before:].isnan().all()
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_attend_one_token_that_takes_all_the_weight_and_queries_far_from_one(dtype):
     b = Both(40, 16, 1, 128, dtype, 20, 20, q_heads=3)
