@@ -46,7 +46,7 @@ __device__ __forceinline__ Scale scale_at(const AttendArgs &a, const Place &p, u
 }
 struct Block { float c, log_v, back_v; };
 __device__ __forceinline__ Block block_of(Scale s, float row_factor, uint32_t mode) {
-    const float v = s.v == 0.0f ? 0x1p-60f : s.v;
+    const float v = s.v == 0.0f || s.bad ? 0x1p-60f : s.v;         // (what is read for a block that there is not may be anything)
     Block b{s.bad ? __builtin_nanf("") : s.k * row_factor, log2_of(v), 1.0f / v};
     if (mode == kScores) { b.log_v = s.v - s.v; b.back_v = 1.0f; }           // (0, or NaN)
     if (mode == kValues && s.v == 0.0f) b.log_v = -INFINITY;
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
         };
         uint32_t t0 = reach.begin + 64 * wave, next = 0;
         if (t0 < reach.end) {
-            const uint32_t entry = table_entry(a, p, t0 + 16 * g, reach.end);
+            const uint32_t entry = table_entry(a, p, t0 + 16 * g, reach.end, reach.first);
             next = table_entry(a, p, t0 + 256 + 16 * g, reach.end);
             ask_keys(t0, entry);
             ask_values(t0, entry);
@@ -453,10 +453,10 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
             values[i] = static_cast<const int8_t *>(a.v) + (uint64_t)p.h * B * D + (uint64_t)(e / SUBS) * B + (16 * (tid % SUBS) & (B - 1));
         }
         Scale scale = {};
-        auto ask_entries = [&](uint32_t t0) {
+        auto ask_entries = [&](uint32_t t0, uint32_t from) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) key_entry[i] = table_entry(a, p, t0 + (i * THREADS + tid) / (D / 16), reach.end);
-            value_entry = table_entry(a, p, t0 + 16 * (tid % SUBS), reach.end);
+            for (int i = 0; i < N; ++i) key_entry[i] = table_entry(a, p, t0 + (i * THREADS + tid) / (D / 16), reach.end, from);
+            value_entry = table_entry(a, p, t0 + 16 * (tid % SUBS), reach.end, from);
         };
         auto ask = [&](uint32_t t0) {
             const uint32_t half = t0 & (B - 1);
@@ -493,12 +493,12 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
         // What a tile brings is asked for a tile ahead and put into the other buffer when the present one is worked on.
         if (tid == 0) far = 0;       // (the threads that may set it are of this wave)
         if (reach.begin < reach.end) {
-            ask_entries(reach.begin);
+            ask_entries(reach.begin, reach.first);
             ask(reach.begin);
-            ask_entries(reach.begin + TOKENS);
+            ask_entries(reach.begin + TOKENS, TOKENS < 128 ? reach.first : 0);
             put(buffer[0]);
             ask(reach.begin + TOKENS);
-            ask_entries(reach.begin + 2 * TOKENS);
+            ask_entries(reach.begin + 2 * TOKENS, 0);
         }
         __syncthreads();
         uint32_t at = 0;
@@ -601,7 +601,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend_many(At
             }
             if (t0 + TOKENS < reach.end) put(buffer[at ^ 1]);
             ask(t0 + 2 * TOKENS);
-            ask_entries(t0 + 3 * TOKENS);
+            ask_entries(t0 + 3 * TOKENS, 0);
             __syncthreads();
         }
         weight += __shfl_xor(weight, 32);

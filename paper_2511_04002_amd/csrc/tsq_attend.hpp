@@ -138,9 +138,10 @@ __device__ __forceinline__ bool is_lost(const AttendArgs &a, const Place &p, uin
 
 // The table's entry for the 16 tokens from `token` on, as it is (past the end of a reach: its last one, so that what is
 // asked for ahead of need is always there, and costs no new lines).  It is looked at when it is used, by id_of, so that
-// nothing waits for it before.
-__device__ __forceinline__ uint32_t table_entry(const AttendArgs &a, const Place &p, uint32_t token, uint32_t end) {
-    return (uint32_t)a.table[(uint64_t)p.r * a.max_blocks + (min(token, end - 1) >> a.block_log2)];
+// nothing waits for it before.  (`from`: tokens before it are not looked up, but it is in their stead.  A reach begins up to
+// 127 tokens before the first one that some row sees, and of blocks there the table may hold nothing, or others' by now.)
+__device__ __forceinline__ uint32_t table_entry(const AttendArgs &a, const Place &p, uint32_t token, uint32_t end, uint32_t from = 0) {
+    return (uint32_t)a.table[(uint64_t)p.r * a.max_blocks + (min(max(token, from), end - 1) >> a.block_log2)];
 }
 // A block's number, 0 for what is none; is_bad says which tokens are to come out as NaN for that.
 __device__ __forceinline__ uint32_t id_of(const AttendArgs &a, uint32_t entry) { return entry < a.blocks ? entry : 0; }

@@ -960,3 +960,58 @@ def test_tensors_on_another_device_than_the_current_one_are_refused(call, monkey
     monkeypatch.setattr(cachelib, "_device", lambda: torch.cuda.current_device() + 1)
     with pytest.raises(ValueError, match="current"):
         getattr(c, call)(*args)
+
+
+# what the scales of a block may be that nobody has written
+ANY_SCALES = ((0.01, 0.01), (0.0, 0.0), (0.01, 2.0 ** -100), (2.0 ** 100, 2.0 ** 100), (float("nan"), float("inf")), (float("inf"), float("nan")), (-1.0, -2.0 ** -110))
+
+
+def bits_of(b, q, table, starts, lengths, *more):
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    return b.c.attend(b.m, q, dev(table), dev(np.asarray(starts, np.int32)), dev(np.asarray(lengths, np.int32)), *more, lse=lse), lse
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("counts", [[1, 1, 1], [6, 1, 2], [1, 90, 1], [40, 90, 2]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("window,block,causal", [(40, 16, True), (100, 64, True), (70, 32, False)])
+def test_attend_gives_the_same_bits_whatever_lies_before_a_window(dtype, counts, dim, window, block, causal):
+    """Blocks that every row's window has left behind may have been given back, and hold what others write to them."""
+    lengths, starts, outs = [301, 290, 5], np.concatenate(([0], np.cumsum(counts))), []
+    for k_scale, v_scale in ANY_SCALES:
+        for released in (False, True):
+            b = Both(3 * 20 + 1, block, 2, dim, dtype, 20, 78, q_heads=8)
+            table = 1 + b.g.permutation(60).reshape(3, 20).astype(np.int32)
+            q = rows(b.g, sum(counts), 8, dim, dtype)
+            b.ks[0], b.vs[0] = k_scale, v_scale
+            for r, n in enumerate(lengths):
+                behind = max(0, n - counts[r] - window + 1) // block
+                b.ks[table[r, :behind]], b.vs[table[r, :behind]] = k_scale, v_scale
+                if released:
+                    table[r, :behind] = -1 if r else len(b.ks)
+            b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
+            outs.append(bits_of(b, q, table, starts, lengths, max(counts), 301, None, causal, window))
+    assert outs[0][0].isfinite().all()
+    for out, lse in outs[1:]:
+        assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("queries", [12, 24, 60, 130])
+def test_attend_gives_the_same_bits_whatever_is_read_for_a_block_that_the_table_does_not_hold(dtype, dim, queries):
+    outs = []
+    for k_scale, v_scale in ANY_SCALES:
+        b = Both(20, 16, 1, dim, dtype, 19, 80, q_heads=2)
+        table = 1 + b.g.permutation(19)[None].astype(np.int32)
+        q = rows(b.g, queries, 2, dim, dtype)
+        b.ks[0], b.vs[0] = k_scale, v_scale
+        b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
+        length = max(queries, 24)
+        hole = (length - queries) // 16 + 1
+        table[0, hole] = -1
+        outs.append(bits_of(b, q, table, [0, queries], [length], queries, length))
+    before = 16 * hole - (length - queries)                  # rows that see nothing of it
+    assert 0 < before < queries and outs[0][0][:before].isfinite().all() and outs[0][0][before:].isnan().all()
+    for out, lse in outs[1:]:
+        assert torch.equal(out[:before], outs[0][0][:before]) and torch.equal(lse[:before], outs[0][1][:before]) and out[before:].isnan().all()
