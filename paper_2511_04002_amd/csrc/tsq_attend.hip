@@ -881,7 +881,6 @@ int launch_attend(const CacheShape &s, const AttendLaunch &l, const AttendArgs &
         f.rows_to = few_rows(s);
         f.splits = l.few_splits;
         f.chunk = l.few_chunk;
-        f.least = std::max(256u, l.few_chunk / 4 / 128 * 128);
         f.parts = j.few_parts;
         f.part_rows = l.few_part_rows;
         f.slots_each = l.slots_each;

@@ -32,7 +32,7 @@ struct Place {
     bool beyond, last;
 };
 
-template <int ROWS>
+template <int ROWS, bool TURNS = false>
 __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
     uint32_t x = blockIdx.x;
     p.h = x % a.kv_heads;
@@ -59,7 +59,7 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
 #pragma unroll
                 for (uint32_t i = 0; i < 8; ++i) below += (uint32_t)__builtin_amdgcn_readlane((int)mine, (int)(j + i)) < mine ? 1 : 0;
             // (or, where all of two rounds run at once, the second round's from the shortest on: a CU has one of each)
-            if (a.by_length > 1) {
+            if (TURNS && a.by_length > 1) {
                 const uint32_t turn = a.by_length - 1, nth = a.requests - 1 - p.r;
                 if (nth >= turn) p.r = nth - turn;
             }
@@ -98,7 +98,7 @@ __device__ __forceinline__ bool find_place(const AttendArgs &a, Place &p) {
 }
 
 // Tokens that any row of a tile sees, the part of them that a split has, and what a row sees.  EVEN: the pieces of a tile are
-// alike, down to a.least tokens, instead of a.chunk each (32 requests of 2048 to 8192 tokens, 4 rows of 64 heads on 8 each, 47 us
+// alike, down to a quarter of a.chunk (or 256), instead of a.chunk each (32 requests of 2048 to 8192 tokens, 4 rows of 64 heads on 8 each, 47 us
 // against 57: short ones have as many workgroups as long ones).
 // (begin is a whole tile's; first: the first token that some row sees, up to 127 behind it)
 struct Reach { uint32_t begin, end, first; };
@@ -113,7 +113,7 @@ __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Place &p, u
     lo &= ~(int64_t)127;             // (a whole tile's, and a block's)
     uint32_t chunk = a.chunk;
     if constexpr (EVEN)
-        if (a.splits > 1) chunk = max((((uint32_t)max(hi - lo, (int64_t)0) + a.splits - 1) / a.splits + 127u) & ~127u, a.least);
+        if (a.splits > 1) chunk = max((((uint32_t)max(hi - lo, (int64_t)0) + a.splits - 1) / a.splits + 127u) & ~127u, max(256u, a.chunk / 4 & ~127u));
     const int64_t begin = lo + (int64_t)p.split * chunk;
     if (p.split + 1 < a.splits) hi = min(hi, begin + chunk);
     w.begin = (uint32_t)min(begin, (int64_t)0x7FFFFFC0);

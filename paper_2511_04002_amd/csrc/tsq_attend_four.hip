@@ -86,7 +86,7 @@ __device__ __forceinline__ bool attend_four_few(const AttendArgs &a, FewShared &
     auto &sums = shared.sums;
     auto &stats = shared.stats;
     Place p;
-    if (!find_place<ROWS>(a, p)) return false;
+    if (!find_place<ROWS, true>(a, p)) return false;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
     const uint32_t B = 1u << a.block_log2;
     uint32_t again = 0;

@@ -232,7 +232,6 @@ tsq_status tsq_cache_attend(const tsq_cache *c, const tsq_cache_memory *m, uint3
     a.requests = requests; a.tokens = tokens; a.q_heads = c->s.q_heads; a.kv_heads = c->s.kv_heads;
     a.group = c->s.q_heads / c->s.kv_heads; a.blocks = c->s.blocks; a.block_log2 = c->s.block_log2; a.max_blocks = c->s.max_blocks;
     a.tiles = l.tiles; a.tiles_each = l.tiles_each; a.splits = l.splits; a.chunk = l.chunk; a.by_length = l.by_length; a.by_tile = 0;
-    a.least = std::max(256u, l.chunk / 4 / 128 * 128);
     a.rows_from = 0; a.rows_to = ~0u;
     a.window = window; a.causal = causal; a.scale_log2 = scale * 1.44269504088896340736f;
     return hip_rc(launch_attend(c->s, l, a, stream));

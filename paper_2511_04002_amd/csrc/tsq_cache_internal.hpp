@@ -80,7 +80,6 @@ struct AttendArgs {
     uint32_t requests, tokens, q_heads, kv_heads, group, blocks, block_log2, max_blocks;
     uint32_t tiles, tiles_each;  // row tiles of the call; of each request, or 0: they follow one another (see find_place)
     uint32_t splits, chunk;      // pieces of a tile's reach along the cache, and the tokens of a piece (a multiple of 128)
-    uint32_t least;              // ... the least, where a tile's pieces are alike (a multiple of 128; of a cache in 4 bits)
     uint32_t by_length;          // the requests' workgroups in the order of their lengths, the longest first (2 .. 64 requests); n + 1: n
                                  // of them, and then the shortest first
     uint32_t by_tile;            // the requests' first tiles before their second ones
