@@ -53,8 +53,9 @@ tsq_status tsq_plan_direct_launch(const tsq_plan *plan, uint32_t *out);
 
 /*
  * Bounds every device-side wait of the plan's later single-pass calls to `rounds` looks (>= 1; a new
- * plan has 2^20, about a second), so that a test can see what a call does whose waits expire.  Host
- * only.  The one call that writes to a plan: not while another thread uses it.
+ * plan has 2^20, about a second), so that a test can see what a call does whose waits expire.  Of a bound of 1
+ * the one who closes the blob gives up whatever it finds, so that such a call never succeeds; the others do
+ * where their first look comes too early.  Host only.  The one call that writes to a plan: not while another thread uses it.
  */
 tsq_status tsq_plan_limit_waits(tsq_plan *plan, uint32_t rounds);
 

@@ -193,7 +193,8 @@ k_direct(const Params p, const uint16_t *__restrict__ in, uint8_t *__restrict__ 
             default: put_codes<8, FULL>(dst, codes, nd); break;
         }
     }
-    uint32_t ew = 0, ec = 0, bad = 0, spins = 0;
+    uint32_t ew = 0, ec = 0, spins = 0;
+    uint32_t bad = last && gives_up_at_once(p) ? 1u : 0u;
 
     // ---- what lies before the token, 256 words at a time, the lowest first: by the time the next ones are asked for
     //      they have been published, too.  (512 words at a time: 700 x 8192 11.3 us against 9.7;
@@ -506,7 +507,8 @@ k_direct_group(const Params p, const uint16_t *__restrict__ in, uint8_t *__restr
     }
 
     // ---- what lies before the group, a word per thread at a time, the lowest first
-    uint32_t ew = 0, ec = 0, bad = 0, spins = 0;
+    uint32_t ew = 0, ec = 0, spins = 0;
+    uint32_t bad = last && gives_up_at_once(p) ? 1u : 0u;
     const uint32_t u0 = u & ~(kDirectBlock - 1u), none = tag << 30;
     uint64_t base = (uint64_t)none << 32;
     if (u0 && wv == 0) base = prefix_load(pre + u0 + opaque_zero());

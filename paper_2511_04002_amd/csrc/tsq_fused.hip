@@ -214,6 +214,7 @@ __device__ void scan_tokens(const Params &p, uint8_t *blob, uint8_t *ws, uint32_
 
     // ---- wave 0 closes the blob
     uint32_t spins = 0;
+    bad |= gives_up_at_once(p);
     if (!bad) {
         // every computing wave reports once, after its last store has been issued
         for (;;) {

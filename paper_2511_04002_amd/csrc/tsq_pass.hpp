@@ -53,6 +53,9 @@ __device__ __forceinline__ bool keep_waiting(uint32_t &spins, uint32_t limit, co
     __builtin_amdgcn_s_sleep(2);
     return true;
 }
+// A bound of one look, which only tests ask for: whether a look finds what it looks for is a matter of timing, so the one who closes
+// the blob does not look at all.
+__device__ __forceinline__ bool gives_up_at_once(const Params &p) { return p.spin_limit == 1u; }
 __device__ __forceinline__ void raise_error(uint32_t *error_flag) {
     // with its result: the atomic has been performed when the wave goes on
     const uint32_t old = __hip_atomic_fetch_or(error_flag, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

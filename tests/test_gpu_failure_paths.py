@@ -421,3 +421,33 @@ def test_a_decompress_stream_behind_a_compress_stream(tsq, oracle, shape, tokens
         sec = plan.sections(blobs[k])
         assert np.array_equal(sec["payload"], refs[k].payload) and np.array_equal(sec["out_col"], refs[k].out_col)
         assert np.array_equal(outs[k].cpu().numpy().view(np.uint16), oracle.decompress(refs[k], nthreads=8))
+
+
+@pytest.mark.parametrize("T,H,dtype", [(1, 768, "f16"), (8, 768, "bf16"), (9, 2048, "f16"), (1, 4096, "bf16"), (3, 4096, "f16"), (1, 5120, "f16"), (2, 6144, "bf16"),
+                                       (2, 32768, "bf16"), (2047, 2048, "bf16"), (2200, 8192, "bf16"), (5000, 4096, "f16")])
+def test_a_call_whose_waits_have_one_look_never_succeeds(tsq, oracle, T, H, dtype):
+    """Of a bound of one look the one who closes the blob gives up whatever it finds: also where nobody waits, or every first look
+    finds what it looks for."""
+    import torch
+    x = loud_rows(T, H, dtype)
+    ref = oracle.compress(x, {"f16": oracle.F16, "bf16": oracle.BF16}[dtype], 8.0, (2, 3, 4, 6, 8), 0.1, 1, nthreads=8)
+    plan = tsq.Plan(T, H, dtype, 8.0, (2, 3, 4, 6, 8), 0.1, pipeline="fused", max_outliers=max(ref.nnz, 1))
+    xd = torch.from_numpy(x.view(np.int16)).cuda()
+    blob, ws = plan.new_blob(), plan.new_workspace()
+    print("calls with waits of one look", flush=True)
+    for i in range(20):
+        tsq.tsq_workspace_reset(plan.handle, ws.data_ptr(), plan._stream())
+        tsq.tsq_plan_limit_waits(plan.handle, 1)
+        plan.compress(xd, blob, ws)
+        info = plan.info(blob, check=False)
+        assert int(ws.view(torch.int32)[CTL_ERROR]) != 0 and info.return_status == tsq.TSQ_ERR_INTERNAL, i
+    for looks in (2, 1 << 20):                               # (with two, a call may fail or not)
+        tsq.tsq_plan_limit_waits(plan.handle, looks)
+        tsq.tsq_workspace_reset(plan.handle, ws.data_ptr(), plan._stream())
+        plan.compress(xd, blob, ws)
+        if looks == 2 and int(ws.view(torch.int32)[CTL_ERROR]):
+            continue
+        assert plan.info(blob).status == 0
+        sec = plan.sections(blob)
+        for k in SECTIONS:
+            assert np.array_equal(sec[k], getattr(ref, k)), k
