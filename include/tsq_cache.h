@@ -208,8 +208,8 @@ tsq_status tsq_cache_gather(const tsq_cache *cache, const tsq_cache_memory *memo
  * to 11 bits; softmax statistics and all sums are binary32.
  * In 4 bits queries, keys and values are exact in either type; scores, and the sums of weights, at most 1 each, times
  * values of bfloat16 have to stay within binary32's range, and products of weights and values below 2^-126 may count as
- * 0.  A part of the work that meets scales of values below 2^-19 or above 2^12, or marked tokens, is done twice (2.3 to
- * 2.8 times as long).
+ * 0.  A part of the work whose queries see marked tokens, or scales of bfloat16 values below 2^-19 or above 2^12, may be done
+ * twice (2.3 to 2.8 times as long).
  */
 tsq_status tsq_cache_attend(const tsq_cache *cache, const tsq_cache_memory *memory, uint32_t requests, const void *d_table,
                             const void *d_starts, const void *d_lengths, uint32_t tokens, uint32_t max_new,

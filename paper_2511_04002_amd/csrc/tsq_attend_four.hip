@@ -62,17 +62,26 @@ template <bool BF16> __device__ __forceinline__ float4_t product(uint4_t x, uint
 // 2400 to 8200 tokens, up to 4 queries of 64 heads on 8 each, 46 us, 3.7 TB/s.
 struct FewShared {
     float sums[4][16][132], stats[4][16][2];
-    uint32_t odd[4];                                     // of each wave: some value is one that the first pass cannot take
+    uint32_t odd[4];                                     // of each wave: some value is one that the first pass does not take
 };
 
-// Scales of 108 to 139, which the first pass takes (2^-19 to 2^12): the bytes of a word less 108 are below 32 each.  (Where one is
-// not, those above it may be off by its borrow, but it shows itself.)
-__device__ __forceinline__ uint32_t odd_scales(uint4_t s) {
-    constexpr uint32_t lowest = 0x6C6C6C6Cu;
-    return ((s[0] - lowest) | (s[1] - lowest) | (s[2] - lowest) | (s[3] - lowest)) & 0xE0E0E0E0u;
+// Scales that the first pass does not take.  Of bfloat16 values those that are not 108 to 139 (2^-19 to 2^12), of which halves
+// hold the values: the bytes of a word less 108 are below 32 each.  (Where one is not, those above it may be off by its borrow, but it
+// shows itself.)  Of binary16 those above the largest, 140, which is the mark alone: its lower seven bits and 115 pass 127.
+// (A token each of 64 requests of 1024 to 4096 tokens, 40 heads of 128, all scales 104 to 107: 157 us, and 411 with the range of bfloat16.)
+template <bool BF16> __device__ __forceinline__ uint32_t odd_scales(uint4_t s) {
+    if constexpr (BF16) {
+        constexpr uint32_t lowest = 0x6C6C6C6Cu;
+        return ((s[0] - lowest) | (s[1] - lowest) | (s[2] - lowest) | (s[3] - lowest)) & 0xE0E0E0E0u;
+    } else {
+        static_assert(FourScales<false>::highest == 128 + 127 - 115);
+        uint32_t odd = 0;
+        for (int i = 0; i < 4; ++i) odd |= ((s[i] & 0x7F7F7F7Fu) + 0x73737373u) & s[i];
+        return odd & 0x80808080u;
+    }
 }
 
-// CAREFUL: the second pass, for values that halves do not hold, or that are NaN and not seen by all rows.
+// CAREFUL: the second pass, for values that halves do not hold (of bfloat16), or that are NaN and not seen by all rows.
 // -> whether the second pass is wanted.
 template <int D, bool BF16, int SETS, bool ONCE, bool CAREFUL>
 __device__ __forceinline__ bool attend_four_few(const AttendArgs &a, FewShared &shared) {
@@ -246,7 +255,7 @@ __device__ __forceinline__ bool attend_four_few(const AttendArgs &a, FewShared &
                     for (int e = 0; e < 16; ++e)
                         if (e < first || e >= behind) vs[e / 4] = (vs[e / 4] & ~(0xFFu << 8 * (e & 3))) | 127u << 8 * (e & 3);
                 }
-                if constexpr (!CAREFUL) odd |= odd_scales(vs);
+                if constexpr (!CAREFUL) odd |= odd_scales<BF16>(vs);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     float scale[8];
