@@ -122,7 +122,7 @@ template <int D, bool BF16, int SETS>
 __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) void k_attend_few(AttendArgs a) {
     constexpr int F = D / 64;                            // 64-element pieces of a head
     constexpr int ROWS = 16 * SETS;
-    __shared__ float sums[4][16][132];
+    __shared__ alignas(16) float sums[4][16][132];
     __shared__ float stats[4][16][2];
     __shared__ Softmax softmax[ROWS];                    // (of the pass kScores)
     __shared__ uint32_t far[4];
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
 // registers 8u .. 8u + 7 are tokens 4 hi + (0..3) and 8 + 4 hi + (0..3) of the 16, so the values' rows in LDS hold
 // each 16 tokens in the order 0-3, 8-11, 4-7, 12-15.
 template <int D, int TOKENS>
-struct ManyTile {                                        // rows padded by 16 bytes: neighbours begin four banks apart
+struct alignas(16) ManyTile {                            // rows padded by 16 bytes: neighbours begin four banks apart
     _Float16 k[TOKENS][D + 8];
     _Float16 v[D][TOKENS + 8];
     float factor[TOKENS / 16], log_v[TOKENS / 16], back_v[TOKENS / 16];      // of each 16 tokens

@@ -60,9 +60,11 @@ template <bool BF16> __device__ __forceinline__ float4_t product(uint4_t x, uint
 // of 131072 tokens, 64 heads on 8, 28 us and 5 to join its pieces, 4.3 TB/s in all; a single token of 128, 5 us from launch to
 // end.  With 32 rows the conversions and the softmax, which is made for each 16 rows, take as long as the loads: 32 requests of
 // 2400 to 8200 tokens, up to 4 queries of 64 heads on 8 each, 46 us, 3.7 TB/s.
-struct FewShared {
+// (16 bytes at a time: the second pass has no more than the type to go by)
+struct alignas(16) FewShared {
     float sums[4][16][132], stats[4][16][2];
     uint32_t odd[4];                                     // of each wave: some value is one that the first pass does not take
+    static_assert(sizeof sums[0][0] % 16 == 0);
 };
 
 // Scales that the first pass does not take.  Of bfloat16 values those that are not 108 to 139 (2^-19 to 2^12), of which halves
@@ -414,9 +416,10 @@ __global__ __launch_bounds__(256, D == 64 && SETS == 1 ? 3 : 2) void k_attend_fo
 // meet in no bank: a prompt of 4096 tokens on 16 heads, 214 us instead of 238.  (Heads of 128 do not notice, of 64 lose 3 % by
 // it, and readers of values, who would meet nowhere with rows of D + 32, gain nothing by that.)
 template <int D, int TOKENS>
-struct FourTile {
+struct alignas(16) FourTile {
     uint16_t k[TOKENS][D + 8];                           // (neighbours begin four banks apart ...
     uint16_t v[TOKENS][D + 16];                          // ... and eight)
+    static_assert(sizeof k[0] % 16 == 0 && sizeof v[0] % 16 == 0, "rows are read and written 16 bytes at a time");
 };
 template <int D> __device__ constexpr uint32_t turned_by(uint32_t part) { return D == 256 ? part >> 1 & 3 : 0; }
 
