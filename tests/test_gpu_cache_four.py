@@ -522,6 +522,42 @@ def test_attend_of_very_low_scores(counts, dim):
     assert (host(lse) < -1e30).all() and len(starts) == 3
 
 
+@pytest.mark.parametrize("counts", [[1, 1], [3, 2], [40, 90]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype,low,high,size", [
+    ("f16", 104, 107, 2.0 ** 8), ("f16", 138, 141, 2.0 ** -6), ("f16", 104, 141, 1.0), ("f16", 138, 141, 2.0 ** -17),
+    ("bf16", 7, 13, 2.0 ** 100), ("bf16", 240, 253, 2.0 ** -100), ("bf16", 7, 253, 2.0 ** -20), ("bf16", 247, 253, 2.0 ** -128)])
+def test_attend_of_keys_at_the_ends_of_their_range(dtype, low, high, size, dim, counts):
+    """Keys that are below the type's normal range (binary16) or close to its ends, and queries below their type's normal range."""
+    b = Both(40, 16, 1, dim, dtype, 20, 90 + dim, q_heads=3)
+    b.ks[:] = b.g.integers(low, high, b.ks.shape)
+    b.wrap()
+    q = rows(b.g, sum(counts), 3, dim, dtype, size)
+    assert bool((q != 0).any(-1).all())
+    # scores of about 1 where the scales are the largest (the root mean square of the codes is 2.95)
+    attend_both(b, 3, counts, [301, 317], q=q, scale=1.0 / (2.95 * dim ** 0.5 * size * 2.0 ** (high - 128)))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("counts", [[1, 1], [3, 2], [40, 90]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_attend_of_equal_scores_is_the_mean_of_the_values(dtype, counts, dim):
+    """Of very low scores (where the type has them), of 0 and of high ones."""
+    for key, q in ((0xFF, 2.0 ** (60 if dtype == "bf16" else 10)), (0x00, 1.0), (0x77, 2.0 ** (60 if dtype == "bf16" else 10))):
+        b = Both(12, 16, 1, dim, dtype, 6, dim + 1, q_heads=2)
+        b.k[:], b.ks[:], b.vs[:] = key, 127 + (45 if dtype == "bf16" else 10), 126
+        b.wrap()
+        lengths, n = [80, 95], sum(counts)
+        table = b.g.permutation(12).reshape(2, 6).astype(np.int32)
+        out, _ = bits_of(b, torch.full((n, 2, dim), q, dtype=KIND[dtype], device="cuda"), table, [0, counts[0], n], lengths, max(counts), 95, None, False)
+        for r, rows_of in enumerate((slice(0, counts[0]), slice(counts[0], n))):
+            v = O.four_tokens_of(b.v, b.vs, table[r], lengths[r], 16, 6)[:, 0]
+            want = v.mean(0)
+            # equal weights are all rounded alike, by half a unit of 11 bits; a sum of 95 in binary32 and its quotient
+            bound = HALF_ULP[dtype] * np.abs(want) + (2.0 ** -11 + 2.0 ** -24 * 110) * np.abs(v).mean(0) + TINY[dtype]
+            assert (np.abs(host(out)[rows_of] - want) <= bound).all()
+
+
 @pytest.mark.parametrize("kind", ["small", "large", "far apart", "zeros beside large"])
 @pytest.mark.parametrize("heads", [(2, 2, 64), (8, 1, 128), (4, 2, 256)])
 def test_attend_of_values_at_the_ends_of_their_range(kind, heads):
