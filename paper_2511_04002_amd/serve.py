@@ -59,6 +59,14 @@ class Side:
             out += [k, v]
         return out
 
+    def held(self, tokens: List[int]) -> int:
+        """Bytes of the keys (or the values) of a layer that requests of so many tokens have in the cache."""
+        c = self.c
+        elements = sum(tokens) * c.kv_heads * c.head_dim
+        if c.bits == 4:
+            return elements // 2 + elements // 32
+        return elements + 4 * c.kv_heads * sum(-(-n // c.block_tokens) for n in tokens)
+
     def store(self, rows, s) -> None:
         for i, memory in enumerate(self.memory):
             self.c.append(memory, rows[2 * i], rows[2 * i + 1], s.slots)
@@ -107,7 +115,11 @@ class Layers:
 def run(requests: int = 8, prompt: int = 700, layers: int = 4, steps: int = 32, q_heads: int = 32, kv_heads: int = 8,
         dim: int = 128, dtype: str = "bf16", bits=(4, 6, 8), budget: float = 0.01, seed: int = 0, cache_bits: int = 8,
         images: bool = False) -> Dict[str, float]:
-    """-> what was sent, and how far the receiver's steps are from the sender's."""
+    """-> what was sent, and how far the receiver's steps are from the sender's.
+
+    sent_bytes is the blob; cache_bytes the rows that it was made of, in 16 bits, as the sender's caches were read back; held_bytes what
+    those tokens take in the sender's caches, codes and scales.  (The blob holds 16-bit rows within a budget, whatever they were read from: it is
+    larger than caches in 8 bits by 2 % and than such in 4 bits by half, with the numbers given here.)"""
     import torch
 
     from . import tsq
@@ -138,7 +150,8 @@ def run(requests: int = 8, prompt: int = 700, layers: int = 4, steps: int = 32, 
         worst = max(worst, float((got.float() - want.float()).norm() / (want - x).float().norm()))
         times.append(begin.elapsed_time(end) * 1e3)
     assert torch.equal(sender.lengths, receiver.lengths)
-    return {"requests": requests, "tokens_sent": total, "layers": layers, "cache_bytes": 2 * layers * total * m.kv_width * 2, "sent_bytes": int(sent),
+    return {"requests": requests, "tokens_sent": total, "layers": layers, "cache_bytes": 2 * layers * total * m.kv_width * 2,
+            "held_bytes": 2 * layers * sender.held(prompts), "sent_bytes": int(sent),
             "relative_difference": worst, "step_us": sorted(times)[len(times) // 2] if times else 0.0}
 
 

@@ -2,7 +2,7 @@
 used together."""
 import pytest
 
-from paper_2511_04002_amd import serve
+from paper_2511_04002_amd import cache, serve
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +25,14 @@ def test_pictures_in_8_bits_and_one_token():
     assert r["relative_difference"] < 0.08
     r = serve.run(requests=1, prompt=1, layers=1, steps=3, q_heads=4, kv_heads=1, dim=64, dtype="f16", cache_bits=4)
     assert r["tokens_sent"] == 1 and r["relative_difference"] < 0.15
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_what_is_sent_is_set_beside_what_the_caches_hold(bits):
+    r = serve.run(requests=4, prompt=128, layers=2, steps=1, q_heads=8, kv_heads=2, dim=128, dtype="bf16", cache_bits=bits)
+    tokens = 32 + 64 + 96 + 128                              # whole blocks of 16: as many bytes as a cache of so many has
+    c = cache.Cache(tokens // 16, 16, 8, 2, 128, "bf16", 8, bits=bits)
+    sizes = cache.tsq_cache_memory_sizes(c.handle)
+    assert r["tokens_sent"] == tokens and r["held_bytes"] == 2 * 2 * (sizes.code_bytes + sizes.scale_bytes)
+    assert r["cache_bytes"] == 2 * 2 * tokens * 2 * 128 * 2
+    assert 0 < r["sent_bytes"] < r["cache_bytes"]
