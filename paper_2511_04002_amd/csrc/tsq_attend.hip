@@ -113,11 +113,11 @@ __device__ __forceinline__ float query_factor(uint32_t most, float &back) {
 //   Keys: operand row m is token 16 (m / 4) + 4t + m % 4; the lane's k indices are the elements 64f + 16g .. + 15.
 //
 // The cache's bytes bound it: 64 requests of 1024 to 4096 tokens on 40 heads of 128, blocks of 16, are 1.79 GB and
-// 306 us, 5.8 TB/s.  The same 2 KB pieces read and thrown away take 300 us, 283 with the longest request first; a
-// stream of reads reaches 7.0 TB/s.  One query of 64 heads on 8 over 131072 tokens: 269 MB, 46 to 54 us and 5 for the
+// 297 to 303 us, 5.9 to 6.0 TB/s.  The same 2 KB pieces read and thrown away take 300 us, 283 with the longest request first; a
+// stream of reads reaches 7.0 TB/s.  One query of 64 heads on 8 over 131072 tokens: 269 MB, 56 us with the
 // join.  With two sets a wave does twice the exponents, maxima and sums for the same bytes, two waves a SIMD: 4 queries of
 // 32 requests over 8192 tokens, 64 heads on 8, are 537 MB and 130 us, 8 of 16 requests over 4096, in two tiles, 134 MB
-// and 51.
+// and 48.
 template <int D, bool BF16, int SETS>
 __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) void k_attend_few(AttendArgs a) {
     constexpr int F = D / 64;                            // 64-element pieces of a head
@@ -354,11 +354,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 || SETS == 2 ? 2 : 3) 
 // Instruction issue bounds it: a wave's 64 tokens by 32 rows of 128 are 1024 cycles of products, and some 1300 of
 // exponentials, maxima, sums, conversions and addresses, which run beside them only as far as two waves of a SIMD
 // complement each other (a product keeps 12 cycles of issue from the other wave).  8192 queries over as many tokens,
-// causal, 64 heads on 8 of 128: 1.10 PFLOP in 1.12 to 1.15 ms, 0.96 to 0.98 PFLOP/s; a large library product of halves
-// reaches 1.2.  Heads of 64 have the exponentials of 128 for half the products: 0.65 PFLOP/s (two requests of 8000 tokens,
-// 20 heads).  Heads of 256 leave registers for one wave a SIMD, whose products nothing runs beside: 0.58 PFLOP/s (4096
-// tokens, 16 heads on 8).  Chunks: 512 queries after 7680, 64 heads on 8, 168 us, 0.79 PFLOP/s; 300 after 4000 of four
-// requests, 32 on 8, 138 us, 0.59 (160 workgroups for 256 places).
+// causal, 64 heads on 8 of 128: 1.10 PFLOP in 1.12 to 1.14 ms, 0.96 to 0.99 PFLOP/s; a large library product of halves
+// reaches 1.2.  Heads of 64 have the exponentials of 128 for half the products: 0.69 PFLOP/s (two requests of 8000 tokens,
+// 20 heads).  Heads of 256 leave registers for one wave a SIMD, whose products nothing runs beside: 0.59 to 0.63 PFLOP/s (4096
+// tokens, 16 heads on 8).  Chunks: 512 queries after 7680, 64 heads on 8, 154 us, 0.87 PFLOP/s; 300 after 4000 of four
+// requests, 32 on 8, 122 us, 0.67 (160 workgroups for 256 places).
 // The maxima could be left out of nearly all tiles, since the sums of the weights show when the reference is too low;
 // the second pass that this needs costs more registers than there are (spilled, 1.44 ms).
 // Lane (n = lane % 32, hi = lane / 32).  S^T in two 32 x 32 pieces: register i of a piece is token

@@ -56,10 +56,12 @@ template <bool BF16> __device__ __forceinline__ float4_t product(uint4_t x, uint
 //   Keys: operand row m is token 16 (m / 4) + 4t + m % 4; the lane's elements are g D/4 .. + D/4 - 1, eight a product.
 //   Values: a lane has elements m D/16 .. + D/16 - 1 of its group's 16 tokens; row m of product j is element m D/16 + j.
 // Memory bounds it where a call has enough tokens to keep two workgroups a CU busy: 64 requests of 1024 to 4096 tokens on 40 heads
-// of 128 (949 MB) take 160 us, 5.9 TB/s, where a kernel that reads the same pieces and drops them takes 147 to 157; one request
-// of 131072 tokens, 64 heads on 8, 28 us and 5 to join its pieces, 4.3 TB/s in all; a single token of 128, 5 us from launch to
+// of 128 (949 MB) take 156 us, 6.1 TB/s, where a kernel that reads the same pieces and drops them takes 147 to 157; one request
+// of 131072 tokens, 64 heads on 8, 31 us with the join of its pieces, 4.6 TB/s; a single token of 128, 5 us from launch to
 // end.  With 32 rows the conversions and the softmax, which is made for each 16 rows, take as long as the loads: 32 requests of
-// 2400 to 8200 tokens, up to 4 queries of 64 heads on 8 each, 46 us, 3.7 TB/s.
+// 2400 to 8200 tokens, up to 4 queries of 64 heads on 8 each, 43 us with the join, 39 by itself, 4.3 TB/s.
+// Little is left of that where requests are many and short: 256 of 25 to 100 tokens on 40 heads are 20 rounds of workgroups, 106 us,
+// in which one wave of four is busy.
 // (16 bytes at a time: the second pass has no more than the type to go by)
 struct alignas(16) FewShared {
     float sums[4][16][132], stats[4][16][2];
@@ -408,12 +410,12 @@ __global__ __launch_bounds__(256, D == 64 && SETS == 1 ? 3 : 2) void k_attend_fo
 // of 2^-23 to 2^13); a workgroup that meets others begins again with bfloat16 values and weights in two parts (SPLIT).
 //
 // The matrix instructions and the vector ones, which share a wave's issue, bound it; each is busy for half of the time: a prompt
-// of 8192 tokens, 64 heads of 128 on 8, 1000 to 1040 us, 1.06 to 1.10 PFLOP/s (840 on zeros, which cost no clock), where a product
-// of two large matrices reaches 1.15 to 1.25; 448 rows over 1500 tokens, 20 heads of 64, six requests, 38 us.  Heads of 64 have
-// half the products for the same exponentials: 8000 tokens on 20 heads, twice, 430 to 440 us, 0.75 PFLOP/s.
+// of 8192 tokens, 64 heads of 128 on 8, 983 to 1026 us, 1.07 to 1.12 PFLOP/s (840 on zeros, which cost no clock), where a product
+// of two large matrices reaches 1.15 to 1.25; 448 rows over 1500 tokens, 20 heads of 64, six requests, 37 us.  Heads of 64 have
+// half the products for the same exponentials: 8000 tokens on 20 heads, twice, 420 to 427 us, 0.78 PFLOP/s.
 //
 // Heads of 256 put a token's pieces of 16 bytes at other places within their 64, such that eight lanes that write at a time
-// meet in no bank: a prompt of 4096 tokens on 16 heads, 214 us instead of 238.  (Heads of 128 do not notice, of 64 lose 3 % by
+// meet in no bank: a prompt of 4096 tokens on 16 heads, 214 us instead of 238 when that was done, 176 now.  (Heads of 128 do not notice, of 64 lose 3 % by
 // it, and readers of values, who would meet nowhere with rows of D + 32, gain nothing by that.)
 template <int D, int TOKENS>
 struct alignas(16) FourTile {

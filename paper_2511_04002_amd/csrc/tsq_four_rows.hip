@@ -46,7 +46,7 @@ template <bool BF16> __device__ __forceinline__ uint32_t four_codes(uint4_t w, f
 // tokens head after head, and between the two the codes go through LDS.  Both kernels write whole lines where their rows are
 // tokens of a block that follow one another, 256 threads 4 KB of codes.
 // Memory bounds both: 22090 rows of 8 heads of 128 (115 MB) are stored in 23.4 us, 4.9 TB/s, and read back in 21.3, 5.4 TB/s;
-// 477 MB of ragged requests in 86 us, 5.5 TB/s, where a kernel that only reads and writes as much takes 84 to 88.  Straight
+// 477 MB of ragged requests in 84 us, 5.7 TB/s, where a kernel that only reads and writes as much takes 84 to 88.  Straight
 // through registers the first took 25.6 and the last, out of blocks of 64, 112.
 constexpr uint32_t kElements = 512;
 template <int D> struct FourRows {
