@@ -997,6 +997,29 @@ def test_attend_gives_the_same_bits_whatever_lies_before_a_window(dtype, counts,
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("counts", [[1, 1], [5, 2], [70, 60], [1, 1, 1, 1, 1, 90]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_attend_gives_the_same_bits_whatever_lies_before_a_window_in_pieces(dtype, counts, dim):
+    window, lengths, outs = 2500, ([4000, 3333] if len(counts) == 2 else [3000, 9, 0, 2700, 40, 4000]), []
+    starts = np.concatenate(([0], np.cumsum(counts)))
+    for k_scale, v_scale in ANY_SCALES[:5]:
+        b = Both(1501, 16, 1, dim, dtype, 250, 81, q_heads=4)
+        table = 1 + b.g.permutation(1500).reshape(6, 250)[:len(counts)].astype(np.int32)
+        q = rows(b.g, sum(counts), 4, dim, dtype)
+        b.ks[0], b.vs[0] = k_scale, v_scale
+        for r, n in enumerate(lengths):
+            behind = max(0, n - counts[r] - window + 1) // 16
+            b.ks[table[r, :behind]], b.vs[table[r, :behind]] = k_scale, v_scale
+            table[r, :behind] = -1
+        b.m = b.c.wrap(dev(b.k), dev(b.v), dev(b.ks), dev(b.vs))
+        assert cachelib.tsq_cache_attend_workspace_bytes(b.c.handle, len(counts), sum(counts), max(counts), max(lengths), window) > 0
+        outs.append(bits_of(b, q, table, starts, lengths, max(counts), max(lengths), None, True, window))
+    assert outs[0][0].isfinite().all()
+    for out, lse in outs[1:]:
+        assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("dim", [64, 128, 256])
 @pytest.mark.parametrize("queries", [12, 24, 60, 130])
 def test_attend_gives_the_same_bits_whatever_is_read_for_a_block_that_the_table_does_not_hold(dtype, dim, queries):

@@ -429,6 +429,32 @@ def test_attend_gives_the_same_bits_whatever_lies_before_a_window(dtype, counts,
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("counts", [[1, 1], [5, 2], [70, 60], [1, 1, 1, 1, 1, 90]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_attend_gives_the_same_bits_whatever_lies_before_a_window_in_pieces(dtype, counts, dim):
+    window, lengths, outs = 2500, ([4000, 3333] if len(counts) == 2 else [3000, 9, 0, 2700, 40, 4000]), []
+    starts = np.concatenate(([0], np.cumsum(counts)))
+    for before in (127, 255) + ((37,) if dtype == "bf16" else ()):
+        b = Both(1501, 16, 1, dim, dtype, 250, 81, q_heads=4)
+        table = 1 + b.g.permutation(1500).reshape(6, 250)[:len(counts)].astype(np.int32)
+        q = rows(b.g, sum(counts), 4, dim, dtype)
+        for x in (b.ks, b.vs):
+            x[0] = before
+            for r, n in enumerate(lengths):
+                first = max(0, n - counts[r] - window + 1)
+                x[table[r, :first // 16]] = before
+                x[table[r, first // 16], ..., :first % 16] = before
+        for r, n in enumerate(lengths):
+            table[r, :max(0, n - counts[r] - window + 1) // 16] = -1
+        b.wrap()
+        assert cachelib.tsq_cache_attend_workspace_bytes(b.c.handle, len(counts), sum(counts), max(counts), max(lengths), window) > 0
+        outs.append(bits_of(b, q, table, starts, lengths, max(counts), max(lengths), None, True, window))
+    assert outs[0][0].isfinite().all()
+    for out, lse in outs[1:]:
+        assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("dim,heads,queries,tile", [(64, 8, 8, 4), (128, 8, 8, 4), (256, 4, 8, 4), (64, 1, 600, 256), (128, 8, 200, 32), (256, 4, 90, 32)])
 def test_attend_gives_the_same_bits_whatever_only_later_tiles_see(dtype, dim, heads, queries, tile):
     """`tile`: queries that one workgroup has; the token behind those of the first ones decides nothing for them."""
